@@ -7,10 +7,12 @@ by an O(3^m) subset recurrence (Sec. 3.1).  This package runs that recurrence
 in hand-written CUDA kernels behind the C ABI of ``include/mpt.h``:
 
 * ``mpt``        -- the ctypes binding (``mpt.solve(weights, bits)``);
+* ``kv``         -- the ctypes binding of ``include/mpt_kv.h``: the paged key/value
+  cache that serves the laid-out prompts (attention, writes, forks, compaction);
 * ``instances``  -- seeded synthetic instances (RAG-shaped pools, L_n, ...);
 * ``build``      -- compiles ``csrc/`` into ``_build/libmpt.so``.
 
-The binding is imported on first use so that ``instances`` stays usable
+The bindings are imported on first use so that ``instances`` stays usable
 without the compiled library.
 """
 
@@ -18,10 +20,10 @@ import importlib
 
 from . import instances
 
-__all__ = ["instances", "mpt", "build"]
+__all__ = ["instances", "mpt", "kv", "build"]
 
 
 def __getattr__(name):
-    if name in ("mpt", "build"):
+    if name in ("mpt", "kv", "build"):
         return importlib.import_module(f".{name}", __name__)
     raise AttributeError(name)

@@ -19,7 +19,7 @@ LIB = BUILD / "libmpt.so"
 BOUNDS_BUILD = PKG / "_build_bounds"
 BOUNDS_LIB = BOUNDS_BUILD / "libmpt.so"
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-SOURCES = ["k_scatter_zeta.cu", "k_dp_general.cu", "k_dp_blocked.cu", "k_walk.cu", "mpt_api.cu", "mpt_noalloc.cu", "k_batch.cu", "mpt_batch.cu", "k_greedy.cu", "k_sched.cu", "k_probe.cu", "k_tables.cu", "k_dp_wide.cu", "k_dp_pruned.cu", "k_dp_tile0.cu"]
+SOURCES = ["k_scatter_zeta.cu", "k_dp_general.cu", "k_dp_blocked.cu", "k_walk.cu", "mpt_api.cu", "mpt_noalloc.cu", "k_batch.cu", "mpt_batch.cu", "k_greedy.cu", "k_sched.cu", "k_probe.cu", "k_tables.cu", "k_dp_wide.cu", "k_dp_pruned.cu", "k_dp_tile0.cu", "mpt_kv.cu", "k_kv_pages.cu", "k_attend_few.cu"]
 
 
 def nvcc() -> str:
@@ -41,7 +41,7 @@ def build(force: bool = False, verbose: bool = False, bounds: bool = False) -> P
     (with bounds=True the bounds-checked variant, in its own directory)."""
     out_dir, lib = (BOUNDS_BUILD, BOUNDS_LIB) if bounds else (BUILD, LIB)
     out_dir.mkdir(exist_ok=True)
-    headers = [CSRC / "mpt_internal.cuh", ROOT / "include" / "mpt.h"]
+    headers = [*CSRC.glob("*.cuh"), *(ROOT / "include").glob("*.h")]
     flags = ["-std=c++17", "-O3", "-lineinfo", *ARCH, "-Xcompiler", "-fPIC", "-I", str(ROOT / "include")]
     if bounds:
         flags.append("-DMPT_BOUNDS")

@@ -1,0 +1,563 @@
+// Pages of a key/value cache (include/mpt_kv.h): merge of attention parts,
+// writes into pages, page bookkeeping and page copies.  All of them move bytes
+// and are bound by the memory, or by latency where there is little to move.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "kv_pages.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace mpt {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Merge: out = sum_p exp(lse_p - lse) out_p
+// ---------------------------------------------------------------------------
+
+// One thread per 16 bytes of the result; the parts' loads are issued together.
+// The weights are recomputed by each of a row's threads (n_parts reads that hit
+// L1, n_parts exponentials): cheaper than handing them round.
+template <int kType>
+struct Vec;  // 16 bytes as 32-bit floats and back
+template <>
+struct Vec<MPT_KV_F32> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ void load(const uint4& u, float* f) {
+    f[0] = __uint_as_float(u.x), f[1] = __uint_as_float(u.y), f[2] = __uint_as_float(u.z), f[3] = __uint_as_float(u.w);
+  }
+  static __device__ __forceinline__ uint4 store(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+template <>
+struct Vec<MPT_KV_BF16> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void load(const uint4& u, float* f) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(w[i] << 16), f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+  static __device__ __forceinline__ uint4 store(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Vec<MPT_KV_F16> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void load(const uint4& u, float* f) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __half2float(__ushort_as_half((unsigned short)w[i]));
+      f[2 * i + 1] = __half2float(__ushort_as_half((unsigned short)(w[i] >> 16)));
+    }
+  }
+  static __device__ __forceinline__ uint4 store(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+template <int kType, int kParts>
+__global__ void __launch_bounds__(256) k_kv_merge(const __grid_constant__ MergeParams p) {
+  using V = Vec<kType>;
+  const int n = kParts ? kParts : p.n;
+  const int64_t all = p.rows * p.vecs;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+    const int64_t row = all < (1ll << 32) ? (int64_t)((uint32_t)at / (uint32_t)p.vecs) : at / p.vecs;
+    uint4 u[kParts ? kParts : 1];
+    float s[kParts ? kParts : 1];
+    float top = -INFINITY, sum = 0.f, acc[V::kN];
+#pragma unroll
+    for (int i = 0; i < V::kN; ++i) acc[i] = 0.f;
+    if constexpr (kParts > 0) {
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) u[k] = ((const uint4*)p.outs[k])[at];
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) s[k] = p.lses[k][row];
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) top = fmaxf(top, s[k]);
+    } else {
+      for (int k = 0; k < n; ++k) top = fmaxf(top, p.lses[k][row]);
+    }
+    const float safe = top == -INFINITY ? 0.f : top;
+#pragma unroll(kParts ? kParts : 4)
+    for (int k = 0; k < n; ++k) {
+      const float lse = kParts ? s[kParts ? k : 0] : p.lses[k][row];
+      const float f = expf(lse - safe);
+      float x[V::kN];
+      V::load(kParts ? u[kParts ? k : 0] : ((const uint4*)p.outs[k])[at], x);
+      sum += f;
+      if (lse != -INFINITY) {  // an empty part's out has no say, whatever it holds
+#pragma unroll
+        for (int i = 0; i < V::kN; ++i) acc[i] = fmaf(f, x[i], acc[i]);
+      }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < V::kN; ++i) acc[i] *= inv;
+    ((uint4*)p.out)[at] = V::store(acc);
+    if (p.lse && at == row * p.vecs) p.lse[row] = top + logf(sum);
+  }
+}
+
+template <int kType>
+cudaError_t merge_of(const MergeParams& p, cudaStream_t stream) {
+  const int64_t blocks = (p.rows * p.vecs + 255) / 256;
+  const unsigned grid = (unsigned)(blocks < (1 << 30) ? blocks : 1 << 30);
+  switch (p.n) {
+    case 2: k_kv_merge<kType, 2><<<grid, 256, 0, stream>>>(p); break;
+    case 3: k_kv_merge<kType, 3><<<grid, 256, 0, stream>>>(p); break;
+    case 4: k_kv_merge<kType, 4><<<grid, 256, 0, stream>>>(p); break;
+    default: k_kv_merge<kType, 0><<<grid, 256, 0, stream>>>(p);
+  }
+  return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Write: a warp per new token and tensor (keys or values)
+// ---------------------------------------------------------------------------
+
+__global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ WriteParams p) {
+  const int lane = threadIdx.x & 31;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (t >= p.tokens) return;
+  // the request: how many of q_offsets[1..batch] are at most t, 32 probes at a time
+  int lo = 0, hi = p.batch;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, j = lo + (lane + 1) * step;
+    const int n = __popc(__ballot_sync(~0u, j <= hi && p.q_offsets[j] <= t));
+    hi = min(hi, lo + (n + 1) * step - 1);
+    lo += n * step;
+  }
+  if (lo >= p.batch) return;
+  const int64_t q0 = p.q_offsets[lo], q1 = p.q_offsets[lo + 1];
+  if (t < q0) return;
+  const int64_t pos = (int64_t)p.kv_lens[lo] - (q1 - q0) + (t - q0);
+  if (pos < 0 || pos >> p.page_log2 >= p.width) return;
+  const int page = p.table[(int64_t)lo * p.table_stride + (pos >> p.page_log2)];
+  if (page < 0 || page >= p.n_pages) return;
+  const int64_t slot = pos & ((1 << p.page_log2) - 1);
+  const uint4* from;
+  uint4* to;
+  int64_t from_head, to_head;
+  if (blockIdx.y == 0) {
+    from = (const uint4*)p.k_new + t * p.k_new_tok, from_head = p.k_new_head;
+    to = (uint4*)p.k + page * p.k_page + slot * p.k_slot, to_head = p.k_head;
+  } else {
+    from = (const uint4*)p.v_new + t * p.v_new_tok, from_head = p.v_new_head;
+    to = (uint4*)p.v + page * p.v_page + slot * p.v_slot, to_head = p.v_head;
+  }
+  const int n = p.kv_heads * p.vecs;
+#pragma unroll 4
+  for (int c = lane; c < n; c += 32) {
+    const int head = c / p.vecs, v = c - head * p.vecs;
+    to[head * to_head + v] = from[head * from_head + v];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Page copies: units of up to 16 KB of one page and plane, dealt out to the
+// blocks in turn; a block looks up 256 of its units at once and drops those
+// without a pair, so that a list that is mostly -1 costs little
+// ---------------------------------------------------------------------------
+
+constexpr int kCopyThreads = 256, kCopyVecs = 4, kCopySeg = kCopyThreads * kCopyVecs * 16;
+
+__global__ void __launch_bounds__(kCopyThreads) k_kv_copy_pages(const __grid_constant__ CopyParams p) {
+  __shared__ int64_t from[kCopyThreads], to[kCopyThreads];
+  __shared__ int left[kCopyThreads], count;
+  const int tid = threadIdx.x;
+  const int64_t segs = (p.page_bytes + kCopySeg - 1) / kCopySeg, units = (int64_t)p.n * p.planes * segs;
+  for (int64_t first = blockIdx.x; first < units; first += (int64_t)gridDim.x * kCopyThreads) {
+    if (tid == 0) count = 0;
+    __syncthreads();
+    const int64_t unit = first + (int64_t)tid * gridDim.x;
+    if (unit < units) {
+      const int64_t seg = unit % segs, pp = unit / segs;
+      const int plane = (int)(pp % p.planes), j = (int)(pp / p.planes);
+      const int s = p.src[j], d = p.dst[j];
+      if (s >= 0 && s < p.n_pages && d >= 0 && d < p.n_pages && s != d) {
+        const int at = atomicAdd(&count, 1);  // any order: each unit has bytes of its own
+        const int64_t base = plane * p.plane_stride + seg * kCopySeg, rest = p.page_bytes - seg * kCopySeg;
+        from[at] = base + s * p.page_stride;
+        to[at] = base + d * p.page_stride;
+        left[at] = rest < kCopySeg ? (int)rest : kCopySeg;
+      }
+    }
+    __syncthreads();
+    const int n = count;
+    for (int k = 0; k < n; ++k) {
+      uint4 v[kCopyVecs];
+#pragma unroll
+      for (int i = 0; i < kCopyVecs; ++i) {
+        const int o = (i * kCopyThreads + tid) * 16;
+        if (o < left[k]) v[i] = *(const uint4*)(p.pool + from[k] + o);
+      }
+#pragma unroll
+      for (int i = 0; i < kCopyVecs; ++i) {
+        const int o = (i * kCopyThreads + tid) * 16;
+        if (o < left[k]) *(uint4*)(p.pool + to[k] + o) = v[i];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Bookkeeping: one cluster of eight blocks per call, so that counting the free
+// pages, ranking them and handing them out are one launch with cluster
+// barriers in between.  A warp owns a run of page ids; ranks are its count
+// before it (a prefix over the cluster's warps, read from the other blocks'
+// shared memory) plus its own ballots.  The counts are whole, so the ranks and
+// everything that follows do not depend on the order of anything.
+// ---------------------------------------------------------------------------
+
+constexpr int kCluster = 8, kBookThreads = 1024, kBookWarps = kBookThreads / 32;
+constexpr int kScanWarps = kCluster * kBookWarps;
+
+struct Scan {
+  int lo, hi;  // page ids of this warp
+};
+
+__device__ __forceinline__ Scan my_run(int n_pages, int warp_of_all, int* per_out = nullptr) {
+  const int per = (int)((((int64_t)n_pages + kScanWarps - 1) / kScanWarps + 31) / 32 * 32);
+  if (per_out) *per_out = per;
+  const int64_t lo = (int64_t)warp_of_all * per;
+  Scan s;
+  s.lo = lo < n_pages ? (int)lo : n_pages;
+  s.hi = lo + per < n_pages ? (int)(lo + per) : n_pages;
+  return s;
+}
+
+// Whole-block exclusive prefix of one value per thread; *total gets the sum.
+__device__ int64_t block_prefix(int64_t v, int64_t* scratch, int64_t* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t inc = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t o = __shfl_up_sync(~0u, inc, d);
+    if (lane >= d) inc += o;
+  }
+  __syncthreads();
+  if (lane == 31) scratch[warp] = inc;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+  for (int w = 0; w < kBookWarps; ++w) {
+    if (w < warp) before += scratch[w];
+    all += scratch[w];
+  }
+  *total = all;
+  return before + inc - v;
+}
+
+// Prefix over all warps of the cluster of one count per warp.  `mine` and `all`
+// are shared; every thread of the cluster calls it.
+__device__ int cluster_prefix(cg::cluster_group& cl, int count, int* mine, int* all, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) mine[warp] = count;
+  cl.sync();
+  if (threadIdx.x < kScanWarps) all[threadIdx.x] = cl.map_shared_rank(mine, threadIdx.x / kBookWarps)[threadIdx.x % kBookWarps];
+  __syncthreads();
+  const int me = (int)cl.block_rank() * kBookWarps + warp;
+  int before = 0, sum = 0;
+  for (int i = lane; i < kScanWarps; i += 32) {
+    const int v = all[i];
+    sum += v;
+    if (i < me) before += v;
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) {
+    before += __shfl_xor_sync(~0u, before, d);
+    sum += __shfl_xor_sync(~0u, sum, d);
+  }
+  *total = sum;
+  return before;
+}
+
+struct BookShared {
+  int64_t scratch[kBookWarps];
+  int mine[kBookWarps], all[kScanWarps];
+  int flags;
+  int64_t need;
+  int partial;
+};
+
+// Whether row r was marked before (marks are bits in the block's shared memory).
+__device__ __forceinline__ bool mark(uint32_t* marks, int r) { return atomicOr(&marks[r >> 5], 1u << (r & 31)) >> (r & 31) & 1u; }
+
+template <int OP>
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads) k_kv_book(const __grid_constant__ BookParams p) {
+  extern __shared__ uint32_t marks[];
+  __shared__ BookShared sh;
+  cg::cluster_group cl = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = (int)cl.block_rank(), gw = rank * kBookWarps + warp;
+  const mpt_kv_book& b = p.b;
+  const int mask = (1 << p.page_log2) - 1;
+  int32_t* fresh = p.ws + kBookHeader;
+  int32_t* ranks = fresh + b.n_pages;
+  const Scan run = my_run(b.n_pages, gw);
+  auto is_page = [&](int id) { return id >= 0 && id < b.n_pages; };
+  const int64_t room = (int64_t)b.width << p.page_log2;  // tokens of a full row
+
+  // Free pages of this warp's run.
+  int free_here = 0;
+  if (OP != kBookFree) {
+#pragma unroll 4
+    for (int at = run.lo; at < run.hi; at += 32) free_here += __popc(__ballot_sync(~0u, at + lane < run.hi && b.refs[at + lane] <= 0));
+  }
+
+  // The first block looks the list over: what each entry needs, and what is wrong.
+  if (rank == 0) {
+    if (tid == 0) sh.flags = 0;
+    for (int i = tid; i < (b.rows + 31) / 32; i += kBookThreads) marks[i] = 0;
+    __syncthreads();
+    int64_t need_before = 0;
+    int flags = 0;
+    for (int base = 0; base < p.n; base += kBookThreads) {
+      const int j = base + tid;
+      int64_t need = 0;
+      if (j < p.n) {
+        if (OP == kBookFork) {
+          const int src = p.l0[j], dst = p.l1[j], keep = p.l2[j];
+          if (src < 0 || src >= b.rows || dst < 0 || dst >= b.rows || mark(marks, dst) || b.lens[dst] != 0 || keep < 0 ||
+              keep > b.lens[src] || keep > room)
+            flags |= MPT_KV_BAD_ROW;
+          else
+            need = (keep & mask) != 0 && is_page(b.table[(int64_t)src * b.table_stride + (keep >> p.page_log2)]);
+        } else {
+          const int row = p.l0[j];
+          if (row < 0 || row >= b.rows || mark(marks, row)) {
+            flags |= MPT_KV_BAD_ROW;
+          } else {
+            const int64_t len = b.lens[row], more = OP == kBookExtend ? p.l1[j] : 0;
+            if (len < 0 || len > room || more < 0)
+              flags |= MPT_KV_BAD_ROW;
+            else if (len + more > room)
+              flags |= MPT_KV_ROW_FULL;
+            else
+              need = ((len + more + mask) >> p.page_log2) - ((len + mask) >> p.page_log2);
+          }
+        }
+      }
+      if (OP != kBookFree) {
+        int64_t all;
+        const int64_t at = need_before + block_prefix(need, sh.scratch, &all);
+        if (j < p.n) ranks[j] = (int)(at < b.n_pages ? at : b.n_pages);
+        need_before += all;
+      }
+    }
+    if (flags) atomicOr(&sh.flags, flags);
+    if (tid == 0) sh.need = need_before;
+  }
+  int free_all = 0;
+  const int before = cluster_prefix(cl, free_here, sh.mine, sh.all, &free_all);  // a cluster barrier: sh is written
+  const BookShared* lead = cl.map_shared_rank(&sh, 0);
+  const int64_t need = lead->need;
+  int flags = lead->flags;
+  if (need > free_all) flags |= MPT_KV_NO_PAGES;
+  if (OP == kBookFree) flags &= ~MPT_KV_NO_PAGES;
+  if (flags == 0 && OP != kBookFree) {
+    int at = before;
+    for (int id = run.lo; id < run.hi && at < need; id += 32) {
+      const unsigned f = __ballot_sync(~0u, id + lane < run.hi && b.refs[id + lane] <= 0);
+      const int r = at + __popc(f & ((1u << lane) - 1u));
+      if ((f >> lane & 1u) && r < need) fresh[r] = id + lane;
+      at += __popc(f);
+    }
+  }
+  cl.sync();  // the fresh pages are known; nobody reads the first block's shared memory any more
+  if (flags == 0) {
+    for (int j = gw; j < p.n; j += kScanWarps) {
+      if (OP == kBookFork) {
+        const int src = p.l0[j], dst = p.l1[j], keep = p.l2[j];
+        const int32_t* from = b.table + (int64_t)src * b.table_stride;
+        int32_t* to = b.table + (int64_t)dst * b.table_stride;
+        const int full = keep >> p.page_log2;
+        for (int i = lane; i < b.width; i += 32) {
+          int id = -1, old = -1;
+          if (i < full) {
+            id = from[i];
+            if (is_page(id)) atomicAdd(&b.refs[id], 1);
+            else id = -1;
+          } else if (i == full && (keep & mask)) {
+            old = from[i];
+            if (is_page(old)) {
+              id = fresh[ranks[j]];
+              b.refs[id] = 1;
+            }
+          }
+          to[i] = id;
+          if (i == full || (full == b.width && i == b.width - 1)) {
+            const bool copy = i == full && id >= 0;
+            p.copy_src[j] = copy ? old : -1;
+            p.copy_dst[j] = copy ? id : -1;
+          }
+        }
+        if (lane == 0) b.lens[dst] = keep;
+      } else {
+        const int row = p.l0[j], len = b.lens[row];
+        int32_t* to = b.table + (int64_t)row * b.table_stride;
+        const int have = (int)(((int64_t)len + mask) >> p.page_log2);
+        if (OP == kBookExtend) {
+          const int more = p.l1[j], want = (int)(((int64_t)len + more + mask) >> p.page_log2), first = ranks[j];
+          for (int i = have + lane; i < want; i += 32) {
+            const int id = fresh[first + i - have];
+            to[i] = id;
+            b.refs[id] = 1;
+          }
+          __syncwarp();
+          if (lane == 0) b.lens[row] = len + more;
+        } else {
+          for (int i = lane; i < b.width; i += 32) {
+            if (i < have && is_page(to[i])) atomicSub(&b.refs[to[i]], 1);
+            to[i] = -1;
+          }
+          __syncwarp();
+          if (lane == 0) b.lens[row] = 0;
+        }
+      }
+    }
+  } else if (OP == kBookFork) {
+    for (int j = gw * 32 + lane; j < p.n; j += kScanWarps * 32) p.copy_src[j] = p.copy_dst[j] = -1;
+  }
+  if (OP == kBookFree) {  // the pages that this call freed are counted too
+    cl.sync();
+    int n = 0, all;
+#pragma unroll 4
+    for (int at = run.lo; at < run.hi; at += 32) n += __popc(__ballot_sync(~0u, at + lane < run.hi && b.refs[at + lane] <= 0));
+    cluster_prefix(cl, n, sh.mine, sh.all, &all);
+    if (gw == 0 && lane == 0) {
+      p.status[0] = flags;
+      p.status[1] = all;
+    }
+    cl.sync();
+  } else if (gw == 0 && lane == 0) {
+    p.status[0] = flags;
+    p.status[1] = free_all - (flags ? 0 : (int)need);
+  }
+}
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads) k_kv_compact(const __grid_constant__ BookParams p) {
+  __shared__ BookShared sh;
+  cg::cluster_group cl = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = (int)cl.block_rank(), gw = rank * kBookWarps + warp, all_threads = kCluster * kBookThreads;
+  const mpt_kv_book& b = p.b;
+  int32_t* to = p.ws + kBookHeader;
+  int per;
+  const Scan run = my_run(b.n_pages, gw, &per);
+  int live = 0, n_live;
+#pragma unroll 4
+  for (int at = run.lo; at < run.hi; at += 32) live += __popc(__ballot_sync(~0u, at + lane < run.hi && b.refs[at + lane] > 0));
+  int before = cluster_prefix(cl, live, sh.mine, sh.all, &n_live);
+  // live pages of id < n_live: those of the warps before the one whose run holds n_live, and a part of its own
+  const int border = n_live / per;  // may be past the last warp
+  if (warp == 0) {
+    int sum = 0;
+    for (int i = lane; i < border && i < kScanWarps; i += 32) sum += sh.all[i];
+    for (int at = border * per; at < n_live; at += 32) {
+      const int c = __popc(__ballot_sync(~0u, at + lane < n_live && b.refs[at + lane] > 0));
+      if (lane == 0) sum += c;
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+    if (lane == 0) sh.partial = sum;
+  }
+  __syncthreads();
+  const int stay = sh.partial, moves = n_live - stay, half = b.n_pages / 2;
+  for (int id0 = run.lo; id0 < run.hi; id0 += 32) {
+    const int id = id0 + lane;
+    const bool in = id < run.hi, on = in && b.refs[id] > 0;
+    const unsigned f = __ballot_sync(~0u, on);
+    const int ahead = before + __popc(f & ((1u << lane) - 1u));  // live pages of a lower id
+    if (in && !on && id < n_live) p.copy_dst[id - ahead] = id;
+    if (on && id >= n_live) p.copy_src[ahead - stay] = id;
+    if (in && !on && id >= n_live) to[id] = id;
+    before += __popc(f);
+  }
+  for (int k = moves + rank * kBookThreads + tid; k < half; k += all_threads) p.copy_src[k] = p.copy_dst[k] = -1;
+  cl.sync();
+  for (int k = rank * kBookThreads + tid; k < moves; k += all_threads) {
+    const int s = p.copy_src[k], d = p.copy_dst[k];
+    to[s] = d;
+    b.refs[d] = b.refs[s];
+    b.refs[s] = 0;
+  }
+  if (gw == 0 && lane == 0) {
+    p.ws[0] = n_live;
+    p.status[0] = 0;
+    p.status[1] = b.n_pages - n_live;
+  }
+}
+
+// Table entries of moved pages (id >= the number of live ones).
+__global__ void __launch_bounds__(256) k_kv_remap(const __grid_constant__ BookParams p) {
+  wait_for_primary();
+  const int n_live = p.ws[0];
+  const int32_t* to = p.ws + kBookHeader;
+  for (int row = blockIdx.y; row < p.b.rows; row += gridDim.y)
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.b.width; i += (int64_t)gridDim.x * 256) {
+      int32_t* at = p.b.table + (int64_t)row * p.b.table_stride + i;
+      const int id = *at;
+      if (id >= n_live && id < p.b.n_pages) *at = to[id];
+    }
+}
+
+template <int OP>
+cudaError_t book(const BookParams& p, cudaStream_t stream) {
+  const size_t smem = (size_t)(p.b.rows + 31) / 32 * 4;
+  cudaError_t e = cudaSuccess;
+  if (smem > 40 * 1024) e = cudaFuncSetAttribute(k_kv_book<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  k_kv_book<OP><<<kCluster, kBookThreads, smem, stream>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv_merge(const MergeParams& p, int type, cudaStream_t stream) {
+  if (type == MPT_KV_F32) return merge_of<MPT_KV_F32>(p, stream);
+  return type == MPT_KV_F16 ? merge_of<MPT_KV_F16>(p, stream) : merge_of<MPT_KV_BF16>(p, stream);
+}
+
+cudaError_t launch_kv_write(const WriteParams& p, cudaStream_t stream) {
+  k_kv_write<<<dim3((unsigned)((p.tokens + 3) / 4), 2), 128, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_copy_pages(const CopyParams& p, cudaStream_t stream) {
+  const int64_t segs = (p.page_bytes + kCopySeg - 1) / kCopySeg, units = (int64_t)p.n * p.planes * segs;
+  const int64_t most = sm_count() * 8;
+  k_kv_copy_pages<<<(unsigned)(units < most ? units : most), kCopyThreads, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_book(const BookParams& p, BookOp op, cudaStream_t stream) {
+  if (op == kBookFork) return book<kBookFork>(p, stream);
+  if (op == kBookExtend) return book<kBookExtend>(p, stream);
+  if (op == kBookFree) return book<kBookFree>(p, stream);
+  k_kv_compact<<<kCluster, kBookThreads, 0, stream>>>(p);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || p.b.rows == 0) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((p.b.width + 255) / 256, p.b.rows < 32768 ? p.b.rows : 32768);
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_kv_remap, p);
+}
+
+}  // namespace mpt

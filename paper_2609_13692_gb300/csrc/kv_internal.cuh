@@ -1,0 +1,151 @@
+// Internal declarations of the paged-cache operators (include/mpt_kv.h).
+#pragma once
+
+#include <cuda.h>
+
+#include "../../include/mpt_kv.h"
+#include "mpt_internal.cuh"
+
+namespace mpt {
+
+// Attention over a paged cache, as both kernels take it.  The tensor maps are
+// 4-d: (element of the head, slot of the page, KV head, page).
+struct alignas(128) AttnParams {
+  CUtensorMap map_k, map_v, map_q;
+  const char* q;
+  char* out;
+  float* lse;  // [tokens][heads] or nullptr
+  int64_t q_tok, q_head, out_tok, out_head;  // strides in elements
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* q_offsets;
+  const int32_t* kv_lens;
+  float* part;  // partial results, see each kernel
+  int4* desc;   // one per block: what its last, unfinished item is
+  int64_t tokens;
+  int32_t width, n_pages, page_log2, batch, heads, kv_heads, group, dim, causal, box;  // box: page slots per copy
+  float scale_log2;  // scale * log2(e)
+};
+
+// One request's lengths, clamped to what the token axis and the table hold.
+struct AttnReq {
+  int q0, ql, kvl;  // first token, new tokens, keys
+};
+
+__device__ __forceinline__ AttnReq attn_req(const AttnParams& p, int i) {
+  AttnReq r;
+  const int64_t a = p.q_offsets[i], b = p.q_offsets[i + 1];
+  const int64_t q0 = a < 0 ? 0 : a > p.tokens ? p.tokens : a;
+  const int64_t q1 = b < q0 ? q0 : b > p.tokens ? p.tokens : b;
+  const int64_t most = (int64_t)p.width << p.page_log2;
+  const int64_t l = p.kv_lens[i];
+  r.q0 = (int)q0;
+  r.ql = (int)(q1 - q0);
+  r.kvl = (int)(l < 0 ? 0 : l > most ? most : l);
+  return r;
+}
+
+// Keys that token t of the request may see: j < the returned value.
+__device__ __forceinline__ int attn_limit(const AttnParams& p, const AttnReq& r, int t) {
+  if (!p.causal) return r.kvl;
+  const int64_t lim = (int64_t)r.kvl - r.ql + t + 1;
+  return lim < 0 ? 0 : lim > r.kvl ? r.kvl : (int)lim;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w,
+                                            unsigned long long* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
+      "[%6];" ::"r"(smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      : "memory");
+}
+
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Work of both attention kernels is a line of units: the requests in order,
+// the items of each (a KV head and a tile of query rows), and the key tiles of
+// an item.  Block c of nc takes units [total c / nc, total (c + 1) / nc), so
+// every block reads the same number of key tiles whatever the lengths; an item
+// cut by a block's border leaves partial results, which a second kernel joins.
+struct AttnRange {
+  int64_t total, begin, end;
+  int nc;       // blocks that have work
+  int req;      // request of unit `begin`
+  int64_t off;  // its place in that request
+};
+
+// All threads of the block call it; `scratch` holds 40 int64.  units(i): units
+// of request i.
+template <int kThreads, typename Units>
+__device__ AttnRange attn_range(int batch, int block, int blocks, int64_t* scratch, Units units) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int kWarps = kThreads / 32;
+  const int per = (batch + kThreads - 1) / kThreads;
+  const int lo = tid * per < batch ? tid * per : batch, hi = lo + per < batch ? lo + per : batch;
+  int64_t sum = 0;
+  for (int i = lo; i < hi; ++i) sum += units(i);
+  int64_t inc = sum;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t v = __shfl_up_sync(~0u, inc, d);
+    if (lane >= d) inc += v;
+  }
+  if (lane == 31) scratch[warp] = inc;
+  __syncthreads();
+  int64_t before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += scratch[w];
+    total += scratch[w];
+  }
+  AttnRange r;
+  r.total = total;
+  r.nc = total < blocks ? (int)total : blocks;
+  r.begin = r.end = 0;
+  r.req = 0;
+  r.off = 0;
+  if (block >= r.nc) return r;  // uniform
+  r.begin = total * block / r.nc;
+  r.end = total * (block + 1) / r.nc;
+  int64_t at = before + inc - sum;
+  if (at <= r.begin && r.begin < at + sum) {
+    int i = lo;
+    for (; i < hi - 1; ++i) {
+      const int64_t u = units(i);
+      if (r.begin < at + u) break;
+      at += u;
+    }
+    scratch[38] = i;
+    scratch[39] = r.begin - at;
+  }
+  __syncthreads();
+  r.req = (int)scratch[38];
+  r.off = scratch[39];
+  return r;
+}
+
+// The block that unit u belongs to.
+__device__ __forceinline__ int attn_block_of(const AttnRange& r, int64_t u) {
+  return (int)(((u + 1) * r.nc + r.total - 1) / r.total) - 1;
+}
+
+// Few query rows per KV head (k_attend_few.cu): bytes of workspace and launch.
+size_t attend_few_workspace(int sms);
+cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, cudaStream_t stream);
+// Flags of the kernels since the last call (waits for the stream).
+cudaError_t attend_few_flags(cudaStream_t stream, int* flags);
+
+// Whole tiles of query rows on tcgen05 (k_attend_tile.cu); head_dim <= 128.
+size_t attend_tile_workspace(int sms);
+cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, cudaStream_t stream);
+cudaError_t attend_tile_flags(cudaStream_t stream, int* flags);
+
+}  // namespace mpt

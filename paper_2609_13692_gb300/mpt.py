@@ -46,7 +46,9 @@ EXPORTED = [
     "mpt_batch_results", "mpt_batch_tables", "mpt_batch_destroy", "mpt_greedy", "mpt_serve_order",
     "mpt_cache_costs", "mpt_layout_pinned", "mpt_solve_steps", "mpt_solve_begin", "mpt_solve_layers",
     "mpt_solve_end", "mpt_solve_resume", "mpt_set_tables", "mpt_tables32", "mpt_gather_bandwidth",
-    "mpt_alu_addmin_peak", "mpt_build_info",
+    "mpt_alu_addmin_peak", "mpt_build_info", "mpt_kv_attend_workspace_bytes", "mpt_kv_attend", "mpt_kv_merge",
+    "mpt_kv_write", "mpt_kv_pages_workspace_bytes", "mpt_kv_fork", "mpt_kv_extend", "mpt_kv_free", "mpt_kv_compact",
+    "mpt_kv_copy_pages", "mpt_kv_check",
 ]
 
 
@@ -137,6 +139,18 @@ def load() -> ctypes.CDLL:
         "mpt_gather_bandwidth": ([i32, i64, vp, ctypes.POINTER(ctypes.c_double)], ctypes.c_int),
         "mpt_alu_addmin_peak": ([i64, vp, ctypes.POINTER(ctypes.c_double)], ctypes.c_int),
         "mpt_build_info": ([i32p], ctypes.c_int),
+        # include/mpt_kv.h; structures and device arrays as plain pointers
+        "mpt_kv_attend_workspace_bytes": ([i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "mpt_kv_attend": ([vp, vp, vp, i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "mpt_kv_merge": ([vp, vp, i32, i64, i32, i32, vp, vp, vp], ctypes.c_int),
+        "mpt_kv_write": ([vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
+        "mpt_kv_pages_workspace_bytes": ([vp, ctypes.POINTER(sz)], ctypes.c_int),
+        "mpt_kv_fork": ([vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "mpt_kv_extend": ([vp, vp, vp, i32, vp, vp, sz, vp], ctypes.c_int),
+        "mpt_kv_free": ([vp, vp, i32, vp, vp, sz, vp], ctypes.c_int),
+        "mpt_kv_compact": ([vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "mpt_kv_copy_pages": ([vp, i32, i64, i32, i64, i64, vp, vp, i32, vp], ctypes.c_int),
+        "mpt_kv_check": ([vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
