@@ -1,0 +1,794 @@
+// Attention over a paged cache for many query rows per KV head (include/mpt_kv.h,
+// mpt_kv_attend): chunks of new tokens, on tcgen05 with accumulators in tensor
+// memory; head sizes up to 128.
+//
+// The running form over key tiles is that of k_attend_few.cu.  An item is a KV
+// head and two tiles of up to 128 query rows (row = token t, query head g of
+// the group), so both products of a key tile, S = Q K^T and O += P V, are
+// 128 x 128 x 128 and every key tile read serves 256 rows.
+//
+// Bound: 4 d operations per visible pair, on the tensor cores; per key tile two
+// S and two PV products (512 cycles each), beside which 2 x 128 x 128
+// exponentials have to fit.  So the two row tiles alternate: while one's
+// products run, the other's probabilities are computed.
+//
+//   warps 0-3, 4-7  one row tile each, one thread per row (no exchange between
+//                   threads): S from tensor memory, running maximum, P back
+//                   over S, O rescaled where the maximum grew, O out at the end
+//   warp 8          issues the products
+//   warp 9          copies: queries once an item, then keys and values of each
+//                   tile page by page into a ring of slots
+//   warps 10, 11    look at the values of tiles with masked keys (below)
+//
+// Rescaling O costs a pass over its 128 columns, so it waits until the maximum
+// has grown by 2^8: any reference below the maximum gives the same quotient,
+// and with 2^8 of room neither P nor its sum can overflow.
+//
+// A masked key's probability is 0, but 0 times an infinite or NaN value is NaN.
+// Tiles with masked keys are few (the last of an item); warps 10 and 11 look at
+// the values that some row of the item must not see, blank those that are not
+// finite, and note the ones that other rows do see; these rows add them at the
+// item's end, key by key.
+#include "kv_internal.cuh"
+
+namespace mpt {
+namespace {
+
+__device__ int g_tile_flags;
+
+constexpr int kKeys = 128;     // keys of a tile
+constexpr int kRows = 256;     // rows of a slot of partial results
+constexpr int kThreads = 384;
+constexpr int kOddSets = 8;    // items whose notes are kept apart (ring depth in items + 2)
+constexpr int kHeldSets = 16;  // key tiles whose page marks are kept apart
+
+template <int HDP>
+struct TileCfg {
+  static constexpr int kBlk = HDP / 64;
+  static constexpr int kSlot = kKeys * HDP * 2;
+  static constexpr int kQ = 2 * 128 * HDP * 2;
+  static constexpr int kSlots = HDP == 64 ? 8 : 5;
+  static constexpr int kSmem = 1024 + kQ + kSlots * kSlot + 2048;
+};
+
+struct TileShared {
+  unsigned long long full[8], empty[8], asked[8], checked[8], q_full, q_empty, s_full[2], p_ready[2], o_full[2], drain;
+  uint32_t tmem;
+  int gave_up;
+  uint32_t held[kHeldSets];
+  uint32_t odd[kOddSets][2][9];  // per checking warp: 8 words of keys from the item's first ambiguous one, and whether any is set
+  int64_t scratch[40];
+};
+static_assert(sizeof(TileShared) <= 2048);
+
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+
+// Bounded wait: false once the block has given up, or after four seconds.
+__device__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const unsigned long long start = now_ns();
+  for (;;) {
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (*(volatile int*)gave_up) return false;
+    if (now_ns() - start > 4000000000ull) {
+      *(volatile int*)gave_up = 1;
+      atomicOr(&g_tile_flags, kErrTimeout);
+      return false;
+    }
+  }
+}
+
+// Shared-memory operand of tcgen05.mma, 128-byte swizzle: `lead` and `stride`
+// are the byte distances of 64-element blocks along the contiguous axis (used
+// where that axis is not the summed one) and of groups of 8 rows.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32_t stride) {
+  return (uint64_t)(addr >> 4 & 0x3FFF) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((int)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((int)add)
+      : "memory");
+}
+__device__ __forceinline__ void commit(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_ld32(float* r, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+        "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]),
+        "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
+        "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, unsigned long long* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (F16)
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool F16>
+__device__ __forceinline__ float2 unpack2(uint32_t x) {
+  if (F16) {
+    float2 f;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(x));
+    return f;
+  }
+  return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+}
+template <bool F16>
+__device__ __forceinline__ bool not_finite2(uint32_t x) {
+  constexpr uint32_t e = F16 ? 0x7C00u : 0x7F80u;
+  return (x & e) == e || (x >> 16 & e) == e;
+}
+
+// sum over k < n of floor((a + b k) / 128), a, b >= 0: after the whole parts are
+// taken out, the points under the line are counted by the other axis, as in
+// Euclid's algorithm.
+__device__ int64_t floor_sum(uint32_t n, uint32_t b, uint32_t a) {
+  int64_t sum = 0;
+  uint32_t m = 128;
+  while (n > 0) {
+    sum += (int64_t)n * (n - 1) / 2 * (b / m) + (int64_t)n * (a / m);
+    b %= m;
+    a %= m;
+    const uint32_t y = b * n + a;  // b < 256, n < 2^24
+    if (y < m) break;
+    n = y / m;
+    a = y % m;
+    const uint32_t t = m;
+    m = b;
+    b = t;
+  }
+  return sum;
+}
+
+// One request's items: its pairs of row tiles and their key tiles.
+struct TileReq {
+  AttnReq r;
+  int toks, pairs;  // tokens of a row tile; pairs of row tiles
+  __device__ __forceinline__ int cost(const AttnParams& p, int pair) const {
+    int lim = r.kvl;
+    if (p.causal) {
+      const int64_t tok = (int64_t)2 * toks * (pair + 1);
+      lim = r.kvl - r.ql + (tok < r.ql ? (int)tok : r.ql);  // > -2^31 + 1
+    }
+    return lim <= kKeys ? 1 : (lim - 1) / kKeys + 1;
+  }
+  // key tiles of the pairs before `pair` (pair <= pairs)
+  __device__ int64_t before(const AttnParams& p, int pair) const {
+    if (!p.causal || pair == 0) return (int64_t)pair * cost(p, 0);
+    const int last = pair == pairs ? cost(p, pairs - 1) : 0;
+    const int n = pair == pairs ? pair - 1 : pair;
+    // cost(q) = max(1, floor((a + b q) / 128))
+    const int b = 2 * toks;
+    const int64_t a = (int64_t)r.kvl - r.ql + b + 127;
+    int64_t one = a >= 128 ? 0 : (128 - a + b - 1) / b;
+    if (one > n) one = n;
+    return one + floor_sum((uint32_t)(n - one), (uint32_t)b, n > one ? (uint32_t)(a + b * one) : 0u) + last;
+  }
+};
+
+__device__ __forceinline__ TileReq tile_req(const AttnParams& p, int i) {
+  TileReq t;
+  t.r = attn_req(p, i);
+  t.toks = 128 / p.group;
+  t.pairs = (int)(((int64_t)t.r.ql + 2 * t.toks - 1) / (2 * t.toks));
+  return t;
+}
+
+// A walk over the block's items; every role makes it on its own.
+struct TileWalk {
+  int req, head, pair, t0, cost, seg;
+  int64_t left;
+  TileReq x;
+  int tok0, n[2], tiles;  // first token; key tiles of each row tile from t0; their maximum
+  int lim_first;          // what the item's first row sees
+  bool starts, ends;
+
+  // By whole warps.
+  __device__ void begin(const AttnParams& p, const AttnRange& range) {
+    req = range.req;
+    left = range.end - range.begin;
+    x = tile_req(p, req);
+    const int64_t per_head = x.before(p, x.pairs);
+    head = (int)(range.off / per_head);
+    const int64_t rest = range.off % per_head;
+    int lo = 0, hi = x.pairs - 1;  // the last pair that begins at or before rest
+    const int lane = threadIdx.x & 31;
+    while (lo < hi) {
+      const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+      const int k = __popc(__ballot_sync(~0u, at <= hi && x.before(p, at) <= rest));
+      lo += k * step;
+      hi = min(hi, lo + step - 1);
+    }
+    pair = lo;
+    t0 = (int)(rest - x.before(p, pair));
+    enter(p);
+  }
+  __device__ __forceinline__ void enter(const AttnParams& p) {
+    cost = x.cost(p, pair);
+    seg = (int)(left < cost - t0 ? left : cost - t0);
+    starts = t0 == 0;
+    ends = t0 + seg == cost;
+    tok0 = pair * 2 * x.toks;
+    lim_first = attn_limit(p, x.r, tok0);
+    tiles = 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int64_t first = (int64_t)tok0 + s * x.toks;
+      n[s] = 0;
+      if (first < x.r.ql) {
+        const int end = (int)(first + x.toks < x.r.ql ? first + x.toks : x.r.ql);
+        const int lim = attn_limit(p, x.r, end - 1), need = lim == 0 ? 0 : (lim - 1) / kKeys + 1;
+        const int stop = t0 + seg < need ? t0 + seg : need;
+        n[s] = stop > t0 ? stop - t0 : 0;
+      }
+      tiles = n[s] > tiles ? n[s] : tiles;
+    }
+  }
+  // False after the last item.
+  __device__ bool next(const AttnParams& p) {
+    left -= seg;
+    if (left <= 0) return false;
+    t0 = 0;
+    if (++pair == x.pairs) {
+      pair = 0;
+      if (++head == p.kv_heads) {
+        head = 0;
+        do {
+          if (++req >= p.batch) return false;
+          x = tile_req(p, req);
+        } while (x.pairs == 0);
+      }
+    }
+    enter(p);
+    return true;
+  }
+  // Whether some row of the item does not see every key of tile t0 + j.
+  __device__ __forceinline__ bool partly(int j) const { return (int64_t)(t0 + j + 1) * kKeys > lim_first; }
+  // Whether the item has such a tile (its last is one if any is).
+  __device__ __forceinline__ bool any_partly() const { return tiles > 0 && partly(tiles - 1); }
+};
+
+template <int HDP, bool F16>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_constant__ AttnParams p) {
+  using C = TileCfg<HDP>;
+  extern __shared__ char raw[];
+  char* base = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+  char* qbuf = base;
+  char* ring = base + C::kQ;
+  TileShared& sh = *(TileShared*)(ring + C::kSlots * C::kSlot);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  if (tid == 0) {
+    for (int s = 0; s < C::kSlots; ++s) {
+      mbar_init(&sh.full[s], 1);
+      mbar_init(&sh.empty[s], 1);
+      mbar_init(&sh.asked[s], 1);
+      mbar_init(&sh.checked[s], 2);
+    }
+    mbar_init(&sh.q_full, 1);
+    mbar_init(&sh.q_empty, 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sh.s_full[s], 1);
+      mbar_init(&sh.p_ready[s], 4);
+      mbar_init(&sh.o_full[s], 1);
+    }
+    mbar_init(&sh.drain, 1);
+    sh.gave_up = 0;
+    mbar_init_fence();
+  }
+  launch_dependents();
+  const AttnRange range = attn_range<kThreads>(p.batch, blockIdx.x, gridDim.x, sh.scratch, [&](int i) -> int64_t {
+    const TileReq t = tile_req(p, i);
+    return t.pairs == 0 ? 0 : p.kv_heads * t.before(p, t.pairs);
+  });
+  if (tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+  if (range.begin >= range.end) return;
+
+  // rows that no copy fills (whole tokens only in a tile) stay 0
+  for (int e = tid; e < C::kQ / 16; e += kThreads) ((uint4*)qbuf)[e] = make_uint4(0, 0, 0, 0);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem;  // S0/P0 at 0, S1/P1 at 128, O0 at 256, O1 at 384
+  int* const gave_up = &sh.gave_up;
+
+  TileWalk w;
+  w.begin(p, range);
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");  // 2 x 224 + 56 = 3 x 168
+    if (warp == 9) {
+      // ---- copies ----
+      const int box = p.box, per = kKeys / box, mine = lane % per, blk = lane / per;
+      uint32_t idx = 0, item = 0, gt = 0;
+      bool ok = true;
+      auto load = [&](char* dst, const CUtensorMap* map, int t, int id, unsigned long long* bar) {
+        const int slot = (t * kKeys) & ((1 << p.page_log2) - 1);
+        if (lane < per * C::kBlk)
+          tma_load_4d(dst + blk * kKeys * 128 + mine * box * 128, map, blk * 64, slot, w.head, id, bar);
+      };
+      do {
+        if (w.tiles == 0) continue;
+        // queries
+        if (item > 0) ok = ok && __all_sync(~0u, wait_bar(&sh.q_empty, (item - 1) & 1, gave_up));
+        if (!ok) break;
+        if (lane == 0) {
+          const int tiles = w.n[1] > 0 ? 2 : 1;  // the second row tile sees at least what the first does
+          mbar_arrive_expect_tx(&sh.q_full, tiles * w.x.toks * p.group * 128 * C::kBlk);
+          for (int s = 0; s < tiles; ++s)
+            for (int b = 0; b < C::kBlk; ++b)
+              tma_load_3d(qbuf + (s * C::kBlk + b) * 128 * 128, &p.map_q, b * 64, w.head * p.group,
+                          w.x.r.q0 + w.tok0 + s * w.x.toks, &sh.q_full);
+        }
+        ++item;
+        const int32_t* row = p.table + (int64_t)w.req * p.table_stride;
+        auto page_of = [&](int j) -> int {
+          const int64_t key = (int64_t)(w.t0 + j) * kKeys + mine * box;
+          if (j >= w.tiles || key >= w.x.r.kvl) return -1;
+          const int id = row[key >> p.page_log2];
+          return id < 0 || id >= p.n_pages ? -1 : id;
+        };
+        int next = page_of(0);
+        for (int j = 0; j < w.tiles; ++j, ++gt) {
+          const int id = next;
+          next = page_of(j + 1);
+          const unsigned held = __ballot_sync(~0u, id >= 0);
+#pragma unroll
+          for (int v = 0; v < 2; ++v, ++idx) {
+            const int s = idx % C::kSlots;
+            if (idx >= C::kSlots) ok = ok && __all_sync(~0u, wait_bar(&sh.empty[s], (idx / C::kSlots - 1) & 1, gave_up));
+            if (!ok) break;
+            if (lane == 0) {
+              if (v == 0) {
+                uint32_t m = 0;
+                for (int g = 0; g < kKeys / 8; ++g) m |= (held >> (g * 8 / box) & 1u) << g;
+                sh.held[gt % kHeldSets] = m;
+              }
+              mbar_arrive_expect_tx(&sh.full[s], C::kSlot);
+            }
+            __syncwarp();
+            load(ring + s * C::kSlot, v ? &p.map_v : &p.map_k, w.t0 + j, id, &sh.full[s]);
+            if (v == 1 && w.partly(j)) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.asked[s]);
+            }
+          }
+          if (!ok) break;
+        }
+      } while (ok && w.next(p));
+      if (!ok) {  // copies in flight land before the block ends
+        for (uint32_t k = idx > C::kSlots ? idx - C::kSlots : 0; k < idx; ++k)
+          for (int i = 0; i < 1 << 16 && !mbar_try_wait(&sh.full[k % C::kSlots], (k / C::kSlots) & 1); ++i) {
+          }
+      }
+    } else if (warp == 8) {
+      // ---- products ----
+      if (lane == 0) {
+        const int steps = (p.dim + 15) / 16;  // of 16 elements of a head; columns of O likewise
+        const uint32_t kind = 1u << 4 | (F16 ? 0u : 1u << 7 | 1u << 10) | 8u << 24;  // 32-bit sums, 128 rows
+        const uint32_t desc_s = kind | (kKeys >> 3) << 17, desc_o = kind | 1u << 16 | (uint32_t)(steps * 16 >> 3) << 17;
+        const uint32_t q_at = smem_u32(qbuf), ring_at = smem_u32(ring);
+        uint32_t idx = 0, item = 0, checks = 0, ready[2] = {0, 0};
+        bool ok = true;
+        auto scores = [&](int s, uint32_t k_at) {
+          for (int k = 0; k < steps; ++k) {
+            const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
+            mma_ss(tmem + s * 128, operand(q_at + s * C::kBlk * 128 * 128 + off, 16, 1024), operand(k_at + off, 16, 1024), desc_s, k > 0);
+          }
+          commit(&sh.s_full[s]);
+        };
+        do {
+          if (w.tiles == 0) continue;
+          ok = wait_bar(&sh.q_full, item & 1, gave_up);
+          ++item;
+          if (!ok) break;
+          // idx: slot number of tile j's keys; its values are idx + 1
+          int s0 = idx % C::kSlots;
+          ok = wait_bar(&sh.full[s0], (idx / C::kSlots) & 1, gave_up);
+          if (!ok) break;
+          fence_after();
+          for (int s = 0; s < 2; ++s)
+            if (w.n[s] > 0) scores(s, ring_at + s0 * C::kSlot);
+          commit(&sh.empty[s0]);
+          for (int j = 0; j < w.tiles && ok; ++j, idx += 2) {
+            const bool more = j + 1 < w.tiles;
+            if (!more) commit(&sh.q_empty);
+            const uint32_t vi = idx + 1, ki = idx + 2;
+            const int sv = vi % C::kSlots, sk = ki % C::kSlots;
+            ok = wait_bar(&sh.full[sv], (vi / C::kSlots) & 1, gave_up);
+            if (ok && w.partly(j)) {
+              ok = wait_bar(&sh.checked[sv], checks >> sv & 1, gave_up);
+              checks ^= 1u << sv;
+            }
+            if (ok && more) ok = wait_bar(&sh.full[sk], (ki / C::kSlots) & 1, gave_up);
+            for (int s = 0; s < 2 && ok; ++s) {
+              if (j >= w.n[s]) continue;
+              ok = wait_bar(&sh.p_ready[s], ready[s] & 1, gave_up);
+              ++ready[s];
+              if (!ok) break;
+              fence_after();
+              for (int k = 0; k < kKeys / 16; ++k)
+                mma_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, operand(ring_at + sv * C::kSlot + k * 2048, kKeys * 128, 1024),
+                       desc_o, j > 0 || k > 0);
+              if (s == 1 || j >= w.n[1]) commit(&sh.empty[sv]);
+              if (j + 1 == w.n[s]) commit(&sh.o_full[s]);
+              else scores(s, ring_at + sk * C::kSlot);
+            }
+            if (!ok) break;
+            if (more) commit(&sh.empty[sk]);
+          }
+        } while (ok && w.next(p));
+        // nothing in flight when the tensor memory goes
+        commit(&sh.drain);
+        for (int i = 0; i < 1 << 20 && !mbar_try_wait(&sh.drain, 0); ++i) {
+        }
+      }
+      __syncwarp();
+    } else {
+      // ---- values that some row must not see ----
+      uint32_t idx = 0, item = 0, asks = 0;
+      bool ok = true;
+      do {
+        if (w.tiles == 0) continue;
+        if (!w.any_partly()) {
+          idx += 2 * w.tiles;
+          continue;
+        }
+        uint32_t* odd = sh.odd[item % kOddSets][warp - 10];
+        ++item;
+        if (lane < 9) odd[lane] = 0;
+        __syncwarp();
+        for (int j = 0; j < w.tiles && ok; ++j, idx += 2) {
+          if (!w.partly(j)) continue;
+          const uint32_t vi = idx + 1;
+          const int s = vi % C::kSlots;
+          // the copy of this use of the slot is under way once it is asked for, so the wait for it is for this use
+          ok = __all_sync(~0u, wait_bar(&sh.asked[s], asks >> s & 1, gave_up));
+          asks ^= 1u << s;
+          ok = ok && __all_sync(~0u, wait_bar(&sh.full[s], (vi / C::kSlots) & 1, gave_up));
+          if (!ok) break;
+          const uint32_t at = smem_u32(ring + s * C::kSlot);
+          const int key0 = (w.t0 + j) * kKeys;
+          const int from = w.lim_first > key0 ? w.lim_first - key0 : 0;
+          bool wrote = false;
+          for (int row = from + (warp - 10); row < kKeys; row += 2) {
+            bool bad = false;
+            for (int ch = lane; ch < HDP / 8; ch += 32) {
+              uint4 v;
+              asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                           : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                           : "r"(at + (ch >> 3) * (kKeys * 128) + row * 128 + ((ch & 7) << 4)));
+              bad |= not_finite2<F16>(v.x) || not_finite2<F16>(v.y) || not_finite2<F16>(v.z) || not_finite2<F16>(v.w);
+            }
+            if (!__any_sync(~0u, bad)) continue;
+            wrote = true;
+            for (int ch = lane; ch < HDP / 8; ch += 32)
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at + (ch >> 3) * (kKeys * 128) + row * 128 + ((ch & 7) << 4)), "r"(0)
+                           : "memory");
+            const int a = key0 + row - w.lim_first;  // at most one per token of the item
+            if (lane == 0 && key0 + row < w.x.r.kvl && a < 256) {
+              odd[a >> 5] |= 1u << (a & 31);
+              odd[8] = 1;
+            }
+          }
+          if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.checked[s]);
+        }
+      } while (ok && w.next(p));
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // ---- one row per thread ----
+    const int s = warp >> 2, r = tid & 127, r_tok = r / p.group, sub = r % p.group;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + s * 128 + lanes, t_o = tmem + 256 + s * 128 + lanes;
+    uint32_t scored = 0, done = 0, item = 0, gt = 0;
+    bool ok = true;
+    do {
+      const int64_t first_tok = (int64_t)w.tok0 + s * w.x.toks;
+      const bool valid = r_tok < w.x.toks && first_tok + r_tok < w.x.r.ql;
+      const int tok = valid ? (int)first_tok + r_tok : 0;
+      const int lim = valid ? attn_limit(p, w.x.r, tok) : INT32_MAX;
+      const int lim_tile = first_tok < w.x.r.ql ? attn_limit(p, w.x.r, (int)first_tok) : 0;  // what every row of the tile sees
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < w.n[s]; ++j) {
+        ok = __all_sync(~0u, wait_bar(&sh.s_full[s], scored & 1, gave_up));
+        ++scored;
+        if (!ok) break;
+        fence_after();
+        float f[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(f + 32 * c, t_s + 32 * c);
+        wait_ld();
+        const uint32_t held = sh.held[(gt + j) % kHeldSets];
+        const int key0 = (w.t0 + j) * kKeys;
+        if (key0 + kKeys > lim_tile || held != 0xFFFFu) {
+          const int sees = lim - key0;
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c >= sees || !(held >> (c >> 3) & 1u)) f[c] = -INFINITY;
+        }
+        float mx[4] = {f[0], f[1], f[2], f[3]};
+#pragma unroll
+        for (int c = 4; c < 128; c += 8)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) mx[q] = c + 4 + q < 128 ? fmaxf(fmaxf(mx[q], f[c + q]), f[c + 4 + q]) : fmaxf(mx[q], f[c + q]);
+        const float top = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2);
+        if (j == 0) {
+          m = top;
+        } else if (__any_sync(~0u, top - m > 8.f)) {
+          const float safe = top == -INFINITY ? 0.f : top;
+          const bool grows = top - m > 8.f;
+          const float a = grows ? ex2(m - safe) : 1.f;
+          m = grows ? top : m;
+          l *= a;
+          for (int c = 0; c < HDP / 32; ++c) {
+            float o[32];
+            uint32_t u[32];
+            tmem_ld32(o, t_o + 32 * c);
+            wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(o[e] * a);
+            tmem_st32(t_o + 32 * c, u);
+          }
+          wait_st();
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 128; ++c) {
+          f[c] = ex2(fmaf(f[c], p.scale_log2, -ref));
+          sum[c & 3] += f[c];
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        // P, rounded to the cache's type (the operand's), over S
+        uint32_t x[64];
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[c] = pack2<F16>(f[2 * c], f[2 * c + 1]);
+        tmem_st32(t_s, x);
+        tmem_st32(t_s + 32, x + 32);
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_ready[s]);
+      }
+      if (!ok) break;
+      gt += w.tiles;
+      const uint32_t(*odd)[9] = nullptr;
+      if (w.any_partly()) odd = sh.odd[item++ % kOddSets];
+      if (w.n[s] > 0) {
+        ok = __all_sync(~0u, wait_bar(&sh.o_full[s], done & 1, gave_up));
+        ++done;
+        if (!ok) break;
+        fence_after();
+      }
+      // ---- out ----
+      const bool whole = w.starts && w.ends;
+      if (first_tok < w.x.r.ql) {
+        const bool extra = odd && w.n[s] > 0 && (odd[0][8] || odd[1][8]);
+        const float inv = l == 0.f ? 0.f : 1.f / l, scale = whole ? inv : 1.f;
+        const int64_t tok_at = (int64_t)w.x.r.q0 + tok, head = (int64_t)w.head * p.group + sub;
+        char* out = p.out + 2 * (tok_at * p.out_tok + head * p.out_head);
+        float* part = p.part + ((int64_t)blockIdx.x * 2 + (w.starts ? 1 : 0)) * (kRows * HDP + 2 * kRows);
+        for (int c = 0; c < HDP / 32; ++c) {
+          float o[32];
+          if (w.n[s] > 0) {
+            tmem_ld32(o, t_o + 32 * c);
+            wait_ld();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          }
+          if (extra && valid) {
+            // seen keys whose values were blanked for the other rows
+            const char* q = p.q + 2 * (tok_at * p.q_tok + head * p.q_head);
+            for (int a = 0; a < 256; ++a) {
+              const int key = w.lim_first + a;
+              if (!((odd[0][a >> 5] | odd[1][a >> 5]) >> (a & 31) & 1u) || key >= lim) continue;
+              const int64_t id = p.table[(int64_t)w.req * p.table_stride + (key >> p.page_log2)];
+              if (id < 0 || id >= p.n_pages) continue;
+              const int64_t slot = key & ((1 << p.page_log2) - 1);
+              const char* kp = p.k + 2 * (id * p.k_page + slot * p.k_slot + w.head * p.k_head);
+              const char* vp = p.v + 2 * (id * p.v_page + slot * p.v_slot + w.head * p.v_head);
+              float dot = 0.f;
+              for (int d = 0; d < p.dim; d += 2) {
+                const float2 a2 = unpack2<F16>(*(const uint32_t*)(q + 2 * d)), b2 = unpack2<F16>(*(const uint32_t*)(kp + 2 * d));
+                dot = fmaf(a2.x, b2.x, fmaf(a2.y, b2.y, dot));
+              }
+              const float pr = ex2(fmaf(dot, p.scale_log2, -(m == -INFINITY ? 0.f : m)));
+#pragma unroll
+              for (int e = 0; e < 32; e += 2)
+                if (32 * c + e < p.dim) {
+                  const float2 v2 = unpack2<F16>(*(const uint32_t*)(vp + 2 * (32 * c + e)));
+                  o[e] = fmaf(pr, v2.x, o[e]);
+                  o[e + 1] = fmaf(pr, v2.y, o[e + 1]);
+                }
+            }
+          }
+          if (whole) {
+            if (valid) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 8)
+                if (32 * c + e < p.dim) {
+                  uint4 v;
+                  v.x = pack2<F16>(o[e] * scale, o[e + 1] * scale);
+                  v.y = pack2<F16>(o[e + 2] * scale, o[e + 3] * scale);
+                  v.z = pack2<F16>(o[e + 4] * scale, o[e + 5] * scale);
+                  v.w = pack2<F16>(o[e + 6] * scale, o[e + 7] * scale);
+                  *(uint4*)(out + 2 * (32 * c + e)) = v;
+                }
+            }
+          } else {
+            // [column / 4][row][4]: a warp's 32 rows are 512 contiguous bytes
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *(float4*)(part + ((int64_t)(8 * c + e / 4) * kRows + s * 128 + r) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+        }
+        if (whole) {
+          if (valid && p.lse) p.lse[tok_at * p.heads + head] = (m + log2f(l)) * 0.6931471805599453f;
+        } else {
+          part[kRows * HDP + s * 128 + r] = m;
+          part[kRows * HDP + kRows + s * 128 + r] = l;
+        }
+      }
+      if (w.starts && !w.ends && tid == 0) {
+        const int64_t first = range.end - w.seg;  // the item's first unit
+        p.desc[blockIdx.x] = make_int4(w.req, w.head, w.pair, attn_block_of(range, first + w.cost - 1) - (int)blockIdx.x + 1);
+      }
+      fence_before();  // O is read before the next item's first product may write it
+    } while (w.next(p));
+  }
+
+  __syncthreads();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// Joins the parts of the item that block c began and did not end: a block per
+// (c, 32 rows), a lane per row, a warp per eighth of the columns.
+template <int HDP, bool F16>
+__global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant__ AttnParams p) {
+  wait_for_primary();
+  const int4 d = p.desc[blockIdx.x];
+  if (d.w == 0) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const TileReq x = tile_req(p, d.x);
+  const int slot_row = blockIdx.y * 32 + lane, s = slot_row >> 7, r = slot_row & 127;
+  const int64_t row_tok = ((int64_t)d.z * 2 + s) * x.toks + r / p.group;
+  if (r >= x.toks * p.group || row_tok >= x.r.ql) return;
+  constexpr int64_t kSlot = kRows * HDP + 2 * kRows;
+  constexpr int kCols = HDP / 8;
+  const float* first = p.part + ((int64_t)blockIdx.x * 2 + 1) * kSlot;
+  const float* rest = p.part + ((int64_t)blockIdx.x * 2 + 2) * kSlot;  // then every second slot
+  float top = -INFINITY, sum = 0.f, acc[kCols];
+#pragma unroll
+  for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < d.w; ++k) top = fmaxf(top, (k ? rest + 2 * (k - 1) * kSlot : first)[kRows * HDP + slot_row]);
+  const float safe = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+  for (int k = 0; k < d.w; ++k) {
+    const float* at = k ? rest + 2 * (k - 1) * kSlot : first;
+    const float f = ex2(at[kRows * HDP + slot_row] - safe);
+    sum = fmaf(f, at[kRows * HDP + kRows + slot_row], sum);
+#pragma unroll
+    for (int c = 0; c < kCols; c += 4) {
+      const float4 v = *(const float4*)(at + ((int64_t)(warp * kCols + c) / 4 * kRows + slot_row) * 4);
+      acc[c] = fmaf(f, v.x, acc[c]);
+      acc[c + 1] = fmaf(f, v.y, acc[c + 1]);
+      acc[c + 2] = fmaf(f, v.z, acc[c + 2]);
+      acc[c + 3] = fmaf(f, v.w, acc[c + 3]);
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int64_t tok = x.r.q0 + row_tok, head = (int64_t)d.y * p.group + r % p.group;
+#pragma unroll
+  for (int c = 0; c < kCols; c += 8) {
+    const int col = warp * kCols + c;
+    if (col >= p.dim) break;
+    uint4 v;
+    v.x = pack2<F16>(acc[c] * inv, acc[c + 1] * inv);
+    v.y = pack2<F16>(acc[c + 2] * inv, acc[c + 3] * inv);
+    v.z = pack2<F16>(acc[c + 4] * inv, acc[c + 5] * inv);
+    v.w = pack2<F16>(acc[c + 6] * inv, acc[c + 7] * inv);
+    *(uint4*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) = v;
+  }
+  if (p.lse && warp == 0) p.lse[tok * p.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+template <int HDP, bool F16>
+cudaError_t launch(const AttnParams& p, int sms, cudaStream_t stream) {
+  using C = TileCfg<HDP>;
+  // the warpgroups' shares (2 x 224 + 56) have to fit the registers of the launch, or they would wait for ever
+  static const cudaError_t fits = [] {
+    cudaFuncAttributes a;
+    const cudaError_t e = cudaFuncGetAttributes(&a, k_attend_tile<HDP, F16>);
+    return e != cudaSuccess ? e : a.numRegs * 3 >= 2 * 224 + 56 ? cudaSuccess : cudaErrorInvalidConfiguration;
+  }();
+  if (fits != cudaSuccess) return fits;
+  cudaError_t e = cudaFuncSetAttribute(k_attend_tile<HDP, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  if (e != cudaSuccess) return e;
+  k_attend_tile<HDP, F16><<<sms, kThreads, C::kSmem, stream>>>(p);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(sms, kRows / 32);
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_attend_tile_join<HDP, F16>, p);
+}
+
+}  // namespace
+
+size_t attend_tile_workspace(int sms) {
+  return (size_t)sms * sizeof(int4) + 256 + (size_t)sms * 2 * (kRows * 128 + 2 * kRows) * sizeof(float);
+}
+
+cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, cudaStream_t stream) {
+  if (p.dim <= 64) return f16 ? launch<64, true>(p, sms, stream) : launch<64, false>(p, sms, stream);
+  return f16 ? launch<128, true>(p, sms, stream) : launch<128, false>(p, sms, stream);
+}
+
+cudaError_t attend_tile_flags(cudaStream_t stream, int* flags) {
+  void* at = nullptr;
+  cudaError_t e = cudaGetSymbolAddress(&at, g_tile_flags);
+  if (e != cudaSuccess) return e;
+  if ((e = cudaMemcpyAsync(flags, at, sizeof(int), cudaMemcpyDeviceToHost, stream)) != cudaSuccess) return e;
+  if ((e = cudaMemsetAsync(at, 0, sizeof(int), stream)) != cudaSuccess) return e;
+  return cudaStreamSynchronize(stream);
+}
+
+}  // namespace mpt

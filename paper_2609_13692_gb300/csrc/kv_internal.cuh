@@ -12,10 +12,11 @@ namespace mpt {
 // 4-d: (element of the head, slot of the page, KV head, page).
 struct alignas(128) AttnParams {
   CUtensorMap map_k, map_v, map_q;
-  const char* q;
+  const char *q, *k, *v;
   char* out;
   float* lse;  // [tokens][heads] or nullptr
   int64_t q_tok, q_head, out_tok, out_head;  // strides in elements
+  int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
   const int32_t* table;
   int64_t table_stride;
   const int32_t* q_offsets;

@@ -71,9 +71,22 @@ bool make_map(CUtensorMap* map, const mpt_kv_cache& c, const void* at, const int
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-size_t attend_workspace() {
-  const int sms = (int)sm_count();
-  return attend_few_workspace(sms);
+// (element, query head, token) of the queries, copied as whole tokens' heads
+// of one KV head, at most 128 rows at a time.
+bool make_query_map(CUtensorMap* map, const AttnParams& p, bool f16) {
+  const EncodeTiled fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)p.dim, (cuuint64_t)p.heads, (cuuint64_t)p.tokens};
+  const cuuint64_t strides[2] = {p.heads > 1 ? (cuuint64_t)p.q_head * 2 : 16, p.tokens > 1 ? (cuuint64_t)p.q_tok * 2 : 16};
+  const cuuint32_t boxes[3] = {64, (cuuint32_t)p.group, (cuuint32_t)(128 / p.group)}, ones[3] = {1, 1, 1};
+  return fn(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<char*>(p.q), dims,
+            strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+size_t attend_workspace(int head_dim, int sms) {
+  const size_t few = attend_few_workspace(sms), tile = attend_tile_workspace(sms);
+  return head_dim > 128 || few > tile ? few : tile;
 }
 
 }  // namespace
@@ -83,7 +96,7 @@ extern "C" {
 
 mpt_status mpt_kv_attend_workspace_bytes(int32_t head_dim, size_t* bytes) {
   if (!bytes || head_dim < 8 || head_dim > 256 || head_dim % 8 != 0) return MPT_ERR_INVALID_ARG;
-  *bytes = mpt::attend_workspace();
+  *bytes = mpt::attend_workspace(head_dim, (int)mpt::sm_count());
   return MPT_OK;
 }
 
@@ -103,7 +116,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   if (!q || !out || !mpt::aligned(q, 16) || !mpt::aligned(out, 16) || !mpt::aligned(lse, 4)) return MPT_ERR_INVALID_ARG;
   const int sms = (int)mpt::sm_count();
   if (!workspace || !mpt::aligned(workspace, 256)) return MPT_ERR_INVALID_ARG;
-  if (workspace_bytes < mpt::attend_workspace()) return MPT_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < mpt::attend_workspace(c->head_dim, sms)) return MPT_ERR_WORKSPACE_TOO_SMALL;
 
   mpt::AttnParams p;
   std::memset((void*)&p, 0, sizeof(p));
@@ -129,11 +142,22 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   p.causal = causal != 0;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t stream = (cudaStream_t)stream_ptr;
-  p.box = c->page_size < 64 ? c->page_size : 64;
-  if (!mpt::make_map(&p.map_k, *c, c->k, c->k_stride, p.box) || !mpt::make_map(&p.map_v, *c, c->v, c->v_stride, p.box))
+  const bool f16 = c->type == MPT_KV_F16;
+  p.k = (const char*)c->k, p.v = (const char*)c->v;
+  p.k_page = c->k_stride[0], p.k_slot = c->k_stride[1], p.k_head = c->k_stride[2];
+  p.v_page = c->v_stride[0], p.v_slot = c->v_stride[1], p.v_head = c->v_stride[2];
+  // Few rows per KV head: 16 of them fill the smaller kernel's products.  Where
+  // the caller does not say, as many tokens as requests are taken for one each.
+  const int64_t most = max_q_len > 0 ? max_q_len : tokens <= c->batch ? 1 : 129;
+  const bool tile = c->head_dim <= 128 && most * p.group > 16;
+  const int keys = tile ? 128 : 64;
+  p.box = c->page_size < keys ? c->page_size : keys;
+  if (!mpt::make_map(&p.map_k, *c, c->k, c->k_stride, p.box) || !mpt::make_map(&p.map_v, *c, c->v, c->v_stride, p.box) ||
+      (tile && !mpt::make_query_map(&p.map_q, p, f16)))
     return MPT_ERR_CUDA;
-  const int64_t rows = max_q_len > 0 ? (int64_t)max_q_len * p.group : 16;
-  return mpt::launch_attend_few(p, c->type == MPT_KV_F16, rows < 16 ? (int)rows : 16, sms, stream) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
+  const cudaError_t e = tile ? mpt::launch_attend_tile(p, f16, sms, stream)
+                             : mpt::launch_attend_few(p, f16, most * p.group < 16 ? (int)(most * p.group) : 16, sms, stream);
+  return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 
 mpt_status mpt_kv_merge(const void* const* outs, const float* const* lses, int32_t n_parts, int64_t rows,
@@ -275,9 +299,11 @@ mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, i
 }
 
 mpt_status mpt_kv_check(void* stream) {
-  int flags = 0;
-  if (mpt::attend_few_flags((cudaStream_t)stream, &flags) != cudaSuccess) return MPT_ERR_CUDA;
-  return flags ? MPT_ERR_TIMEOUT : MPT_OK;
+  int few = 0, tile = 0;
+  if (mpt::attend_few_flags((cudaStream_t)stream, &few) != cudaSuccess ||
+      mpt::attend_tile_flags((cudaStream_t)stream, &tile) != cudaSuccess)
+    return MPT_ERR_CUDA;
+  return few | tile ? MPT_ERR_TIMEOUT : MPT_OK;
 }
 
 }  // extern "C"
