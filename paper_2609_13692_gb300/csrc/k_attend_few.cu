@@ -582,9 +582,10 @@ __global__ void __launch_bounds__(512) k_attend_few_join(const __grid_constant__
 }
 
 template <int HDP, bool F16>
-cudaError_t launch(const AttnParams& p, int rows_hint, int sms, cudaStream_t stream) {
+cudaError_t launch(const AttnParams& p, int rows_hint, int sms, int device, cudaStream_t stream) {
   using C = FewCfg<HDP>;
-  cudaError_t e = cudaFuncSetAttribute(k_attend_few<HDP, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  static std::atomic<uint64_t> allowed;
+  cudaError_t e = kv_allow_smem(k_attend_few<HDP, F16>, C::kSmem, device, allowed);
   if (e != cudaSuccess) return e;
   k_attend_few<HDP, F16><<<sms, C::kThreads, C::kSmem, stream>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
@@ -606,11 +607,11 @@ size_t attend_few_workspace(int sms) {
   return (size_t)sms * sizeof(int4) + 256 + (size_t)sms * 2 * (kRows * 256 + 2 * kRows) * sizeof(float);
 }
 
-cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, cudaStream_t stream) {
-  if (p.dim <= 64) return f16 ? launch<64, true>(p, rows_hint, sms, stream) : launch<64, false>(p, rows_hint, sms, stream);
+cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, int device, cudaStream_t stream) {
+  if (p.dim <= 64) return f16 ? launch<64, true>(p, rows_hint, sms, device, stream) : launch<64, false>(p, rows_hint, sms, device, stream);
   if (p.dim <= 128)
-    return f16 ? launch<128, true>(p, rows_hint, sms, stream) : launch<128, false>(p, rows_hint, sms, stream);
-  return f16 ? launch<256, true>(p, rows_hint, sms, stream) : launch<256, false>(p, rows_hint, sms, stream);
+    return f16 ? launch<128, true>(p, rows_hint, sms, device, stream) : launch<128, false>(p, rows_hint, sms, device, stream);
+  return f16 ? launch<256, true>(p, rows_hint, sms, device, stream) : launch<256, false>(p, rows_hint, sms, device, stream);
 }
 
 cudaError_t attend_few_flags(cudaStream_t stream, int* flags) {

@@ -746,7 +746,7 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
 }
 
 template <int HDP, bool F16>
-cudaError_t launch(const AttnParams& p, int sms, cudaStream_t stream) {
+cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream) {
   using C = TileCfg<HDP>;
   // the warpgroups' shares (2 x 224 + 56) have to fit the registers of the launch, or they would wait for ever
   static const cudaError_t fits = [] {
@@ -755,7 +755,8 @@ cudaError_t launch(const AttnParams& p, int sms, cudaStream_t stream) {
     return e != cudaSuccess ? e : a.numRegs * 3 >= 2 * 224 + 56 ? cudaSuccess : cudaErrorInvalidConfiguration;
   }();
   if (fits != cudaSuccess) return fits;
-  cudaError_t e = cudaFuncSetAttribute(k_attend_tile<HDP, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  static std::atomic<uint64_t> allowed;
+  cudaError_t e = kv_allow_smem(k_attend_tile<HDP, F16>, C::kSmem, device, allowed);
   if (e != cudaSuccess) return e;
   k_attend_tile<HDP, F16><<<sms, kThreads, C::kSmem, stream>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
@@ -777,9 +778,9 @@ size_t attend_tile_workspace(int sms) {
   return (size_t)sms * sizeof(int4) + 256 + (size_t)sms * 2 * (kRows * 128 + 2 * kRows) * sizeof(float);
 }
 
-cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, cudaStream_t stream) {
-  if (p.dim <= 64) return f16 ? launch<64, true>(p, sms, stream) : launch<64, false>(p, sms, stream);
-  return f16 ? launch<128, true>(p, sms, stream) : launch<128, false>(p, sms, stream);
+cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int device, cudaStream_t stream) {
+  if (p.dim <= 64) return f16 ? launch<64, true>(p, sms, device, stream) : launch<64, false>(p, sms, device, stream);
+  return f16 ? launch<128, true>(p, sms, device, stream) : launch<128, false>(p, sms, device, stream);
 }
 
 cudaError_t attend_tile_flags(cudaStream_t stream, int* flags) {

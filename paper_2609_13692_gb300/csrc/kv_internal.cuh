@@ -1,6 +1,8 @@
 // Internal declarations of the paged-cache operators (include/mpt_kv.h).
 #pragma once
 
+#include <atomic>
+
 #include <cuda.h>
 
 #include "../../include/mpt_kv.h"
@@ -27,6 +29,31 @@ struct alignas(128) AttnParams {
   int32_t width, n_pages, page_log2, batch, heads, kv_heads, group, dim, causal, box;  // box: page slots per copy
   float scale_log2;  // scale * log2(e)
 };
+
+// Multiprocessors of the current device, asked once per device.
+inline int kv_sm_count(int* device) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    *device = 0;
+    return (int)sm_count();
+  }
+  *device = dev;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) known[dev].store(n = (int)sm_count(), std::memory_order_relaxed);
+  return n;
+}
+
+// A kernel's limit of dynamic shared memory, raised once per device.  `done` is
+// the kernel's own, a bit per device.
+template <typename Kernel>
+cudaError_t kv_allow_smem(Kernel kernel, int bytes, int device, std::atomic<uint64_t>& done) {
+  const uint64_t bit = 1ull << (device & 63);
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 // One request's lengths, clamped to what the token axis and the table hold.
 struct AttnReq {
@@ -140,13 +167,13 @@ __device__ __forceinline__ int attn_block_of(const AttnRange& r, int64_t u) {
 
 // Few query rows per KV head (k_attend_few.cu): bytes of workspace and launch.
 size_t attend_few_workspace(int sms);
-cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, cudaStream_t stream);
+cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, int device, cudaStream_t stream);
 // Flags of the kernels since the last call (waits for the stream).
 cudaError_t attend_few_flags(cudaStream_t stream, int* flags);
 
 // Whole tiles of query rows on tcgen05 (k_attend_tile.cu); head_dim <= 128.
 size_t attend_tile_workspace(int sms);
-cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, cudaStream_t stream);
+cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int device, cudaStream_t stream);
 cudaError_t attend_tile_flags(cudaStream_t stream, int* flags);
 
 }  // namespace mpt

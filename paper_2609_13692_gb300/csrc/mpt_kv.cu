@@ -96,7 +96,8 @@ extern "C" {
 
 mpt_status mpt_kv_attend_workspace_bytes(int32_t head_dim, size_t* bytes) {
   if (!bytes || head_dim < 8 || head_dim > 256 || head_dim % 8 != 0) return MPT_ERR_INVALID_ARG;
-  *bytes = mpt::attend_workspace(head_dim, (int)mpt::sm_count());
+  int device = 0;
+  *bytes = mpt::attend_workspace(head_dim, mpt::kv_sm_count(&device));
   return MPT_OK;
 }
 
@@ -114,7 +115,8 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
     if (!mpt::stride_ok(q_stride[i], entries[i]) || !mpt::stride_ok(out_stride[i], entries[i])) return MPT_ERR_INVALID_ARG;
   if (tokens == 0 || c->batch == 0) return MPT_OK;
   if (!q || !out || !mpt::aligned(q, 16) || !mpt::aligned(out, 16) || !mpt::aligned(lse, 4)) return MPT_ERR_INVALID_ARG;
-  const int sms = (int)mpt::sm_count();
+  int device = 0;
+  const int sms = mpt::kv_sm_count(&device);
   if (!workspace || !mpt::aligned(workspace, 256)) return MPT_ERR_INVALID_ARG;
   if (workspace_bytes < mpt::attend_workspace(c->head_dim, sms)) return MPT_ERR_WORKSPACE_TOO_SMALL;
 
@@ -155,8 +157,8 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   if (!mpt::make_map(&p.map_k, *c, c->k, c->k_stride, p.box) || !mpt::make_map(&p.map_v, *c, c->v, c->v_stride, p.box) ||
       (tile && !mpt::make_query_map(&p.map_q, p, f16)))
     return MPT_ERR_CUDA;
-  const cudaError_t e = tile ? mpt::launch_attend_tile(p, f16, sms, stream)
-                             : mpt::launch_attend_few(p, f16, most * p.group < 16 ? (int)(most * p.group) : 16, sms, stream);
+  const cudaError_t e = tile ? mpt::launch_attend_tile(p, f16, sms, device, stream)
+                             : mpt::launch_attend_few(p, f16, most * p.group < 16 ? (int)(most * p.group) : 16, sms, device, stream);
   return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 

@@ -13,10 +13,10 @@ that other streams write have to be ready in it, as for any torch operation.
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
-from typing import Optional, Sequence
+import struct
+from typing import Optional
 
 import torch
 
@@ -25,94 +25,77 @@ from . import mpt as _mpt
 MPT_KV_BF16, MPT_KV_F16, MPT_KV_F32 = 0, 1, 2
 MPT_KV_BAD_ROW, MPT_KV_NO_PAGES, MPT_KV_ROW_FULL = 1, 2, 4
 _TYPES = {torch.bfloat16: MPT_KV_BF16, torch.float16: MPT_KV_F16, torch.float32: MPT_KV_F32}
+_INT = torch.int32
+
+# The structures of mpt_kv.h as packed bytes (native sizes and alignment): a
+# call's host time is a good part of a small call, and filling a ctypes
+# structure field by field costs as much as the call itself.
+_CACHE = struct.Struct("@2P6q6iPqi2P")  # mpt_kv_cache
+_BOOK = struct.Struct("@Pq2i2P2i")      # mpt_kv_book
+_PAIR = struct.Struct("@2q")            # two strides
+
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-class mpt_kv_cache(ctypes.Structure):
-    _fields_ = [
-        ("k", ctypes.c_void_p),
-        ("v", ctypes.c_void_p),
-        ("k_stride", ctypes.c_int64 * 3),
-        ("v_stride", ctypes.c_int64 * 3),
-        ("type", ctypes.c_int32),
-        ("n_pages", ctypes.c_int32),
-        ("page_size", ctypes.c_int32),
-        ("kv_heads", ctypes.c_int32),
-        ("head_dim", ctypes.c_int32),
-        ("batch", ctypes.c_int32),
-        ("page_table", ctypes.c_void_p),
-        ("table_stride", ctypes.c_int64),
-        ("table_width", ctypes.c_int32),
-        ("q_offsets", ctypes.c_void_p),
-        ("kv_lens", ctypes.c_void_p),
-    ]
-
-
-class mpt_kv_book(ctypes.Structure):
-    _fields_ = [
-        ("table", ctypes.c_void_p),
-        ("table_stride", ctypes.c_int64),
-        ("width", ctypes.c_int32),
-        ("rows", ctypes.c_int32),
-        ("lens", ctypes.c_void_p),
-        ("refs", ctypes.c_void_p),
-        ("n_pages", ctypes.c_int32),
-        ("page_size", ctypes.c_int32),
-    ]
-
-
-@contextlib.contextmanager
-def _on(tensor, stream):
-    """The tensor's device, and `stream` as torch's current stream there, so that
-    what the call allocates belongs to it; yields the stream's address."""
-    if tensor.device.index == torch.cuda.current_device() and stream is None:
-        yield torch.cuda.current_stream().cuda_stream
-        return
-    with torch.cuda.device(tensor.device):
+def _run(index: int, stream: Optional[int], call, *args):
+    """call(stream address, *args) with device `index` current and `stream` as torch's current
+    stream there, so that what the call allocates belongs to it."""
+    if stream is None and index == torch.cuda.current_device():
+        return call(_raw_stream(index), *args)
+    with torch.cuda.device(index):
         if stream is None:
-            yield torch.cuda.current_stream().cuda_stream
-        else:
-            with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=tensor.device)):
-                yield int(stream)
+            return call(_raw_stream(index), *args)
+        with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=index)):
+            return call(int(stream), *args)
 
 
-def _same_device(first, *others):
-    for t in (first, *others):
-        if not t.is_cuda or t.device != first.device:
-            raise ValueError("every tensor must be on the same CUDA device")
+def _device(first, *others) -> int:
+    index = first.get_device()
+    for t in others:
+        if t.get_device() != index:
+            index = -1
+    if index < 0:
+        raise ValueError("every tensor must be on the same CUDA device")
+    return index
 
 
 def _ints(t, name: str, dims: int = 1):
-    if t.dtype != torch.int32 or t.dim() != dims or (t.numel() > 0 and t.stride(-1) != 1):
+    if t.dtype is not _INT or t.dim() != dims or (t.stride(-1) != 1 and t.numel() > 0):
         raise ValueError(f"{name} must be a {dims}-d int32 tensor with contiguous rows")
 
 
-def _cache(k_pages, v_pages, page_table, q_offsets, kv_lens) -> mpt_kv_cache:
-    _same_device(k_pages, v_pages, page_table, q_offsets, kv_lens)
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
+def _cache(k_pages, v_pages, page_table, q_offsets, kv_lens):
+    """The packed mpt_kv_cache, and (type, kv_heads, head_dim)."""
+    shape, dtype = k_pages.shape, k_pages.dtype
+    if len(shape) != 4 or shape != v_pages.shape or dtype is not v_pages.dtype:
         raise ValueError("k_pages and v_pages must be [n_pages, page_size, kv_heads, head_dim] of one type")
-    if k_pages.dtype not in (torch.bfloat16, torch.float16):
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
         raise ValueError("the cache must be bfloat16 or float16")
-    if k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
+    kp, ks, kh, ke = k_pages.stride()
+    vp, vs, vh, ve = v_pages.stride()
+    if ke != 1 or ve != 1:
         raise ValueError("the elements of a head must be contiguous")
     _ints(page_table, "page_table", 2)
     _ints(q_offsets, "q_offsets")
     _ints(kv_lens, "kv_lens")
-    batch = int(page_table.shape[0])
+    batch, width = page_table.shape
     if q_offsets.shape[0] != batch + 1 or kv_lens.shape[0] != batch:
         raise ValueError("q_offsets needs batch + 1 entries, kv_lens batch")
-    n_pages, page_size, kv_heads, dim = k_pages.shape
-    c = mpt_kv_cache(k_pages.data_ptr(), v_pages.data_ptr())
-    c.k_stride[:] = k_pages.stride()[:3]
-    c.v_stride[:] = v_pages.stride()[:3]
-    c.type, c.n_pages, c.page_size, c.kv_heads, c.head_dim = _TYPES[k_pages.dtype], n_pages, page_size, kv_heads, dim
-    c.batch, c.table_width = batch, page_table.shape[1]
-    c.table_stride = max(page_table.stride(0), page_table.shape[1]) if batch < 2 else page_table.stride(0)
-    c.page_table, c.q_offsets, c.kv_lens = page_table.data_ptr(), q_offsets.data_ptr(), kv_lens.data_ptr()
-    return c
+    n_pages, page_size, kv_heads, dim = shape
+    stride = page_table.stride(0) if batch > 1 else max(width, 1)
+    return _CACHE.pack(k_pages.data_ptr(), v_pages.data_ptr(), kp, ks, kh, vp, vs, vh, _TYPES[dtype], n_pages, page_size,
+                       kv_heads, dim, batch, page_table.data_ptr(), stride, width, q_offsets.data_ptr(),
+                       kv_lens.data_ptr()), dtype, kv_heads, dim
 
 
-def _strides(t):
-    return (ctypes.c_int64 * 2)(t.stride(0), t.stride(1))
+def _strides(t) -> bytes:
+    return _PAIR.pack(t.stride(0), t.stride(1))
+
+
+def _check_workspace(workspace, index: int):
+    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != index:
+        raise ValueError("workspace must be a contiguous CUDA uint8 tensor on the same device")
 
 
 _workspace_bytes: dict = {}
@@ -135,35 +118,42 @@ def mpt_kv_attend(q, k_pages, v_pages, page_table, q_offsets, kv_lens, *, max_q_
     request with n new tokens and L keys sees keys j <= L - n + t (causal) or all L.  max_q_len: the
     most new tokens of a request, where known (a hint).  scale: default 1 / sqrt(head_dim).
     out: [tokens, heads, head_dim] of q's type; lse: float32[tokens, heads], natural logarithm.
-    A row that sees no key gets out = 0, lse = -inf."""
-    _same_device(q, k_pages)
-    c = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
-    if q.dim() != 3 or q.dtype != k_pages.dtype or q.shape[2] != c.head_dim or (q.numel() > 0 and q.stride(2) != 1):
+    A row that sees no key gets out = 0, lse = -inf; tokens of no request are not written."""
+    index = _device(q, k_pages, v_pages, page_table, q_offsets, kv_lens)
+    cache, dtype, _, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
+    shape = q.shape
+    if len(shape) != 3 or q.dtype is not dtype or shape[2] != dim or (q.stride(2) != 1 and q.numel() > 0):
         raise ValueError("q must be [tokens, heads, head_dim] of the cache's type with contiguous heads")
-    tokens, heads = int(q.shape[0]), int(q.shape[1])
-    with _on(q, stream) as s:
-        if out is None:
-            # rows that belong to no request are not written
-            out = torch.empty((tokens, heads, c.head_dim), dtype=q.dtype, device=q.device)
-        if lse is None:
-            lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device)
-        if out.shape != q.shape or out.dtype != q.dtype or (out.numel() > 0 and out.stride(2) != 1):
+    if out is not None:
+        _device(q, out)
+        if out.shape != shape or out.dtype is not dtype or (out.stride(2) != 1 and out.numel() > 0):
             raise ValueError("out must have q's shape and type, with contiguous heads")
-        if lse.shape != (tokens, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
+    if lse is not None:
+        _device(q, lse)
+        if lse.shape != shape[:2] or lse.dtype is not torch.float32 or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous float32[tokens, heads]")
-        _same_device(q, out, lse)
-        if workspace is None:
-            key = (q.device.index, c.head_dim)
-            if key not in _workspace_bytes:
-                _workspace_bytes[key] = mpt_kv_attend_workspace_bytes(c.head_dim)
-            workspace = torch.empty(_workspace_bytes[key], dtype=torch.uint8, device=q.device)
-        if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous CUDA uint8 tensor")
-        _same_device(q, workspace)
-        _mpt._check(_mpt.load().mpt_kv_attend(
-            ctypes.byref(c), q.data_ptr(), _strides(q), tokens, heads, int(max_q_len), 1 if causal else 0,
-            1.0 / math.sqrt(c.head_dim) if scale is None else float(scale), out.data_ptr(), _strides(out),
-            lse.data_ptr(), workspace.data_ptr(), workspace.numel(), s), "mpt_kv_attend")
+    if workspace is not None:
+        _check_workspace(workspace, index)
+    return _run(index, stream, _attend, index, cache, q, int(max_q_len), 1 if causal else 0,
+                1.0 / math.sqrt(dim) if scale is None else float(scale), out, lse, workspace)
+
+
+def _attend(s, index, cache, q, max_q_len, causal, scale, out, lse, workspace):
+    (tokens, heads, dim), device = q.shape, q.device
+    if out is None:
+        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=device)
+    if lse is None:
+        lse = torch.empty((tokens, heads), dtype=torch.float32, device=device)
+    if workspace is None:
+        size = _workspace_bytes.get((index, dim))
+        if size is None:
+            size = _workspace_bytes[index, dim] = mpt_kv_attend_workspace_bytes(dim)
+        workspace = torch.empty(size, dtype=torch.uint8, device=device)
+    status = _mpt.load().mpt_kv_attend(cache, q.data_ptr(), _strides(q), tokens, heads, max_q_len, causal, scale,
+                                       out.data_ptr(), _strides(out), lse.data_ptr(), workspace.data_ptr(),
+                                       workspace.numel(), s)
+    if status:
+        _mpt._check(status, "mpt_kv_attend")
     return out, lse
 
 
@@ -172,160 +162,204 @@ def mpt_kv_merge(outs, lses, *, out=None, lse=None, stream: Optional[int] = None
 
     outs: a sequence of [.., head_dim] tensors (or one tensor of them along its first axis), bf16,
     f16 or f32; lses: likewise, float32 [..].  Parts with lse = -inf have no part in a row."""
-    outs, lses = list(outs), list(lses)
-    if not outs or len(outs) != len(lses):
-        raise ValueError("outs and lses must be non-empty and of one length")
-    o = outs[0]
-    _same_device(o, *outs, *lses)
-    if o.dtype not in _TYPES or o.dim() < 1:
-        raise ValueError("outs must be bfloat16, float16 or float32")
-    for a, b in zip(outs, lses):
-        if a.shape != o.shape or a.dtype != o.dtype or not a.is_contiguous():
-            raise ValueError("outs must be contiguous and of one shape and type")
-        if b.shape != o.shape[:-1] or b.dtype != torch.float32 or not b.is_contiguous():
-            raise ValueError("lses must be contiguous float32 of outs' shape without the last axis")
-    n, dim = len(outs), int(o.shape[-1])
-    with _on(o, stream) as s:
-        out = torch.empty_like(o) if out is None else out
-        lse = torch.empty_like(lses[0]) if lse is None else lse
-        _same_device(o, out, lse)
-        if out.shape != o.shape or out.dtype != o.dtype or not out.is_contiguous():
+    po, shape, dtype, o = _parts(outs, "outs")
+    pl, lshape, ldtype, z = _parts(lses, "lses")
+    if len(po) != len(pl) or lshape != shape[:-1] or ldtype is not torch.float32:
+        raise ValueError("lses must be as many float32 tensors as outs, of their shape without the last axis")
+    if dtype not in _TYPES or not shape:
+        raise ValueError("outs must be bfloat16, float16 or float32 with heads of a last axis")
+    index = _device(o, z)
+    if out is not None:
+        _device(o, out)
+        if out.shape != shape or out.dtype is not dtype or not out.is_contiguous():
             raise ValueError("out must be contiguous, of outs' shape and type")
-        if lse.shape != o.shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous():
+    if lse is not None:
+        _device(o, lse)
+        if lse.shape != lshape or lse.dtype is not torch.float32 or not lse.is_contiguous():
             raise ValueError("lse must be contiguous float32 of lses' shape")
-        ps = (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs])
-        pl = (ctypes.c_void_p * n)(*[t.data_ptr() for t in lses])
-        _mpt._check(_mpt.load().mpt_kv_merge(ps, pl, n, lse.numel(), dim, _TYPES[o.dtype], out.data_ptr(),
-                                             lse.data_ptr(), s), "mpt_kv_merge")
+    return _run(index, stream, _merge, po, pl, shape, dtype, o.device, out, lse)
+
+
+def _parts(parts, name: str):
+    """(addresses, shape, type, a tensor) of equal contiguous parts."""
+    if isinstance(parts, torch.Tensor):
+        if parts.dim() < 1 or parts.shape[0] < 1 or not parts.is_contiguous():
+            raise ValueError(f"{name} must be contiguous parts, one at least")
+        n, at = parts.shape[0], parts.data_ptr()
+        step = parts.stride(0) * parts.element_size()
+        return [at + i * step for i in range(n)], parts.shape[1:], parts.dtype, parts
+    parts = list(parts)
+    if not parts:
+        raise ValueError(f"{name} must not be empty")
+    first = parts[0]
+    _device(first, *parts)
+    for t in parts:
+        if t.shape != first.shape or t.dtype is not first.dtype or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous and of one shape and type")
+    return [t.data_ptr() for t in parts], first.shape, first.dtype, first
+
+
+def _merge(s, po, pl, shape, dtype, device, out, lse):
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    if lse is None:
+        lse = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+    n = len(po)
+    status = _mpt.load().mpt_kv_merge(struct.pack("%dP" % n, *po), struct.pack("%dP" % n, *pl), n, lse.numel(), shape[-1],
+                                      _TYPES[dtype], out.data_ptr(), lse.data_ptr(), s)
+    if status:
+        _mpt._check(status, "mpt_kv_merge")
     return out, lse
 
 
 def mpt_kv_write(k_new, v_new, k_pages, v_pages, page_table, q_offsets, kv_lens, *, stream: Optional[int] = None) -> None:
     """Write the new tokens' keys and values ([tokens, kv_heads, head_dim], the cache's type) into
     their pages: the last q_offsets[i+1] - q_offsets[i] of request i's kv_lens[i] positions."""
-    c = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
-    _same_device(k_pages, k_new, v_new)
+    index = _device(k_pages, v_pages, page_table, q_offsets, kv_lens, k_new, v_new)
+    cache, dtype, kv_heads, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
+    tokens = k_new.shape[0] if k_new.dim() else 0
     for t in (k_new, v_new):
-        if t.shape != (k_new.shape[0], c.kv_heads, c.head_dim) or t.dtype != k_pages.dtype or (t.numel() > 0 and t.stride(2) != 1):
+        if t.shape != (tokens, kv_heads, dim) or t.dtype is not dtype or (t.stride(2) != 1 and t.numel() > 0):
             raise ValueError("k_new and v_new must be [tokens, kv_heads, head_dim] of the cache's type with contiguous heads")
-    with _on(k_pages, stream) as s:
-        _mpt._check(_mpt.load().mpt_kv_write(ctypes.byref(c), k_new.data_ptr(), _strides(k_new), v_new.data_ptr(),
-                                             _strides(v_new), int(k_new.shape[0]), s), "mpt_kv_write")
+    _run(index, stream, _write, cache, k_new, v_new, tokens)
+
+
+def _write(s, cache, k_new, v_new, tokens):
+    status = _mpt.load().mpt_kv_write(cache, k_new.data_ptr(), _strides(k_new), v_new.data_ptr(), _strides(v_new), tokens, s)
+    if status:
+        _mpt._check(status, "mpt_kv_write")
 
 
 # ---------------------------------------------------------------------------
 # Bookkeeping of pages
 # ---------------------------------------------------------------------------
 
-def _book(table, lens, refs, page_size: int) -> mpt_kv_book:
-    _same_device(table, lens, refs)
+def _book(table, lens, refs, page_size: int, *lists):
+    """The packed mpt_kv_book, the device, (rows, n_pages) and the length of the lists."""
+    index = _device(table, lens, refs, *lists)
     _ints(table, "table", 2)
     _ints(lens, "lens")
     _ints(refs, "refs")
-    if lens.shape[0] != table.shape[0]:
-        raise ValueError("lens needs one entry per table row")
     rows, width = table.shape
-    stride = max(table.stride(0), width) if rows < 2 else table.stride(0)
-    return mpt_kv_book(table.data_ptr(), stride, width, rows, lens.data_ptr(), refs.data_ptr(), refs.shape[0], int(page_size))
-
-
-def _lists(table, *lists):
-    _same_device(table, *lists)
+    if lens.shape[0] != rows:
+        raise ValueError("lens needs one entry per table row")
+    n = lists[0].shape[0] if lists and lists[0].dim() else 0
     for t in lists:
         _ints(t, "a list of rows or lengths")
-        if t.shape != lists[0].shape:
+        if t.shape[0] != n:
             raise ValueError("the lists must be of one length")
+    n_pages = refs.shape[0]
+    stride = table.stride(0) if rows > 1 else max(width, 1)
+    return _BOOK.pack(table.data_ptr(), stride, width, rows, lens.data_ptr(), refs.data_ptr(), n_pages,
+                      int(page_size)), index, rows, n_pages, n
+
+
+def _pages_workspace(workspace, index, rows, n_pages, device):
+    if workspace is None:  # what mpt_kv_pages_workspace_bytes says: a header, one int per page and per row
+        return torch.empty(4 * (16 + n_pages + rows), dtype=torch.uint8, device=device)
+    _check_workspace(workspace, index)
+    return workspace
 
 
 def mpt_kv_pages_workspace_bytes(table, lens, refs, page_size: int) -> int:
     """Bytes of workspace of the bookkeeping calls."""
-    b = _book(table, lens, refs, page_size)
+    book = _book(table, lens, refs, page_size)[0]
     out = ctypes.c_size_t()
-    _mpt._check(_mpt.load().mpt_kv_pages_workspace_bytes(ctypes.byref(b), ctypes.byref(out)), "mpt_kv_pages_workspace_bytes")
+    _mpt._check(_mpt.load().mpt_kv_pages_workspace_bytes(book, ctypes.byref(out)), "mpt_kv_pages_workspace_bytes")
     return int(out.value)
-
-
-def _pages_workspace(table, refs, workspace):
-    if workspace is None:  # what mpt_kv_pages_workspace_bytes says: a header, one int per page and per row
-        workspace = torch.empty(4 * (16 + refs.shape[0] + table.shape[0]), dtype=torch.uint8, device=table.device)
-    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous CUDA uint8 tensor")
-    _same_device(table, workspace)
-    return workspace
 
 
 def mpt_kv_fork(table, lens, refs, page_size: int, src, dst, keep, *, workspace=None, stream: Optional[int] = None):
     """Row dst[j] (empty) gets the first keep[j] tokens of row src[j]: full pages shared, a part page
     copied to a fresh one.  Returns (old, fresh, status): int32[n] page pairs for
     :func:`mpt_kv_copy_pages` (-1 where nothing is to copy), and the device int32[2] status."""
-    b = _book(table, lens, refs, page_size)
-    _lists(table, src, dst, keep)
-    n = int(src.shape[0])
-    with _on(table, stream) as s:
-        got = torch.empty(2 * n + 2, dtype=torch.int32, device=table.device)
-        old, fresh, status = got[:n], got[n:2 * n], got[2 * n:]
-        ws = _pages_workspace(table, refs, workspace)
-        _mpt._check(_mpt.load().mpt_kv_fork(ctypes.byref(b), src.data_ptr(), dst.data_ptr(), keep.data_ptr(), n,
-                                            old.data_ptr(), fresh.data_ptr(), status.data_ptr(), ws.data_ptr(),
-                                            ws.numel(), s), "mpt_kv_fork")
+    book = _book(table, lens, refs, page_size, src, dst, keep)
+    return _run(book[1], stream, _fork, *book, table.device, src, dst, keep, workspace)
+
+
+def _fork(s, book, index, rows, n_pages, n, device, src, dst, keep, workspace):
+    old, fresh, status = torch.empty(2 * n + 2, dtype=_INT, device=device).split((n, n, 2))
+    ws = _pages_workspace(workspace, index, rows, n_pages, device)
+    st = _mpt.load().mpt_kv_fork(book, src.data_ptr(), dst.data_ptr(), keep.data_ptr(), n, old.data_ptr(), fresh.data_ptr(),
+                                 status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    if st:
+        _mpt._check(st, "mpt_kv_fork")
     return old, fresh, status
 
 
 def mpt_kv_extend(table, lens, refs, page_size: int, rows, more, *, workspace=None, stream: Optional[int] = None):
     """Row rows[j] grows by more[j] tokens onto fresh pages; returns the device int32[2] status."""
-    b = _book(table, lens, refs, page_size)
-    _lists(table, rows, more)
-    with _on(table, stream) as s:
-        status = torch.empty(2, dtype=torch.int32, device=table.device)
-        ws = _pages_workspace(table, refs, workspace)
-        _mpt._check(_mpt.load().mpt_kv_extend(ctypes.byref(b), rows.data_ptr(), more.data_ptr(), int(rows.shape[0]),
-                                              status.data_ptr(), ws.data_ptr(), ws.numel(), s), "mpt_kv_extend")
+    book = _book(table, lens, refs, page_size, rows, more)
+    return _run(book[1], stream, _extend, *book, table.device, rows, more, workspace)
+
+
+def _extend(s, book, index, n_rows, n_pages, n, device, rows, more, workspace):
+    status = torch.empty(2, dtype=_INT, device=device)
+    ws = _pages_workspace(workspace, index, n_rows, n_pages, device)
+    st = _mpt.load().mpt_kv_extend(book, rows.data_ptr(), more.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    if st:
+        _mpt._check(st, "mpt_kv_extend")
     return status
 
 
 def mpt_kv_free(table, lens, refs, page_size: int, rows, *, workspace=None, stream: Optional[int] = None):
     """The pages of the listed rows lose a reference, the rows are emptied; returns the device int32[2] status."""
-    b = _book(table, lens, refs, page_size)
-    _lists(table, rows)
-    with _on(table, stream) as s:
-        status = torch.empty(2, dtype=torch.int32, device=table.device)
-        ws = _pages_workspace(table, refs, workspace)
-        _mpt._check(_mpt.load().mpt_kv_free(ctypes.byref(b), rows.data_ptr(), int(rows.shape[0]), status.data_ptr(),
-                                            ws.data_ptr(), ws.numel(), s), "mpt_kv_free")
+    book = _book(table, lens, refs, page_size, rows)
+    return _run(book[1], stream, _free, *book, table.device, rows, workspace)
+
+
+def _free(s, book, index, n_rows, n_pages, n, device, rows, workspace):
+    status = torch.empty(2, dtype=_INT, device=device)
+    ws = _pages_workspace(workspace, index, n_rows, n_pages, device)
+    st = _mpt.load().mpt_kv_free(book, rows.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    if st:
+        _mpt._check(st, "mpt_kv_free")
     return status
 
 
 def mpt_kv_compact(table, lens, refs, page_size: int, *, workspace=None, stream: Optional[int] = None):
     """Moves the live pages to the lowest ids; returns (old, fresh, status): int32[n_pages // 2] page
     pairs for :func:`mpt_kv_copy_pages` (the moves, then -1), and the device int32[2] status."""
-    b = _book(table, lens, refs, page_size)
-    n = int(refs.shape[0]) // 2
-    with _on(table, stream) as s:
-        got = torch.empty(2 * n + 2, dtype=torch.int32, device=table.device)
-        old, fresh, status = got[:n], got[n:2 * n], got[2 * n:]
-        ws = _pages_workspace(table, refs, workspace)
-        _mpt._check(_mpt.load().mpt_kv_compact(ctypes.byref(b), old.data_ptr(), fresh.data_ptr(), status.data_ptr(),
-                                               ws.data_ptr(), ws.numel(), s), "mpt_kv_compact")
+    book = _book(table, lens, refs, page_size)
+    return _run(book[1], stream, _compact, *book, table.device, workspace)
+
+
+def _compact(s, book, index, rows, n_pages, _, device, workspace):
+    n = n_pages // 2
+    old, fresh, status = torch.empty(2 * n + 2, dtype=_INT, device=device).split((n, n, 2))
+    ws = _pages_workspace(workspace, index, rows, n_pages, device)
+    st = _mpt.load().mpt_kv_compact(book, old.data_ptr(), fresh.data_ptr(), status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    if st:
+        _mpt._check(st, "mpt_kv_compact")
     return old, fresh, status
 
 
 def mpt_kv_copy_pages(pool, src, dst, *, stream: Optional[int] = None) -> None:
     """Copy pages src[j] -> dst[j] in every plane of ``pool`` ([planes, n_pages, ...], a page
     contiguous); pairs with an id out of range (-1) are skipped.  No dst may be a page of another pair."""
-    _lists(src, src, dst)
-    _same_device(pool, src)
-    if pool.dim() < 3:
-        raise ValueError("pool must be [planes, n_pages, ...]")
-    page = pool[0, 0] if pool.shape[0] and pool.shape[1] else None
-    if page is None or not page.is_contiguous():
-        raise ValueError("the pool must not be empty and its pages must be contiguous")
+    index = _device(pool, src, dst)
+    _ints(src, "src")
+    _ints(dst, "dst")
+    if src.shape != dst.shape:
+        raise ValueError("the lists must be of one length")
+    shape, strides = pool.shape, pool.stride()
+    if len(shape) < 3 or 0 in shape:
+        raise ValueError("pool must be [planes, n_pages, ...] and not empty")
+    size = 1
+    for n, step in zip(shape[:1:-1], strides[:1:-1]):
+        if n > 1 and step != size:
+            raise ValueError("a page of the pool must be contiguous")
+        size *= n
     e = pool.element_size()
-    planes, n_pages, size = int(pool.shape[0]), int(pool.shape[1]), page.numel() * e
-    with _on(pool, stream) as s:
-        _mpt._check(_mpt.load().mpt_kv_copy_pages(pool.data_ptr(), planes, pool.stride(0) * e if planes > 1 else 0,
-                                                  n_pages, pool.stride(1) * e if n_pages > 1 else size, size,
-                                                  src.data_ptr(), dst.data_ptr(), int(src.shape[0]), s),
-                    "mpt_kv_copy_pages")
+    _run(index, stream, _copy_pages, pool, shape[0], strides[0] * e if shape[0] > 1 else 0, shape[1],
+         (strides[1] if shape[1] > 1 else size) * e, size * e, src, dst)
+
+
+def _copy_pages(s, pool, planes, plane_stride, n_pages, page_stride, page_bytes, src, dst):
+    st = _mpt.load().mpt_kv_copy_pages(pool.data_ptr(), planes, plane_stride, n_pages, page_stride, page_bytes, src.data_ptr(),
+                                       dst.data_ptr(), src.shape[0], s)
+    if st:
+        _mpt._check(st, "mpt_kv_copy_pages")
 
 
 def mpt_kv_check(stream: Optional[int] = None) -> None:
