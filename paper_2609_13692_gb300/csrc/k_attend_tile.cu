@@ -16,18 +16,19 @@
 //                   threads): S from tensor memory, running maximum, P back
 //                   over S, O rescaled where the maximum grew, O out at the end
 //   warp 8          issues the products
-//   warp 9          copies: queries once an item, then keys and values of each
-//                   tile page by page into a ring of slots
-//   warps 10, 11    look at the values of tiles with masked keys (below)
+//   warps 9, 10     copies: queries once an item and keys, and values, of each
+//                   tile page by page into a ring of slots (with pages of 16 one
+//                   warp's 32 copies a tile take longer than its products)
+//   warp 11         looks at the values of tiles with masked keys (below)
 //
 // Rescaling O costs a pass over its 128 columns, so it waits until the maximum
 // has grown by 2^8: any reference below the maximum gives the same quotient,
 // and with 2^8 of room neither P nor its sum can overflow.
 //
 // A masked key's probability is 0, but 0 times an infinite or NaN value is NaN.
-// Tiles with masked keys are few (the last of an item); warps 10 and 11 look at
-// the values that some row of the item must not see, blank those that are not
-// finite, and note the ones that other rows do see; these rows add them at the
+// Tiles with masked keys are few (the last of an item); warp 11 looks at the
+// values that some row of the item must not see, blanks those that are not
+// finite, and notes the ones that other rows do see; these rows add them at the
 // item's end, key by key.
 #include "kv_internal.cuh"
 
@@ -56,7 +57,7 @@ struct TileShared {
   uint32_t tmem;
   int gave_up;
   uint32_t held[kHeldSets];
-  uint32_t odd[kOddSets][2][9];  // per checking warp: 8 words of keys from the item's first ambiguous one, and whether any is set
+  uint32_t odd[kOddSets][9];  // 8 words of keys from the item's first ambiguous one, and whether any is set
   int64_t scratch[40];
 };
 static_assert(sizeof(TileShared) <= 2048);
@@ -67,15 +68,18 @@ __device__ __forceinline__ unsigned long long now_ns() {
   return t;
 }
 
-// Bounded wait: false once the block has given up, or after four seconds.
-__device__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const unsigned long long start = now_ns();
+// Bounded wait: false once the block has given up, or after four seconds.  The
+// clock is looked at after the first polls only: reading it takes longer than
+// most waits.
+__device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up) {
+  unsigned long long start = 0;
   for (;;) {
-    for (int i = 0; i < 64; ++i)
+    for (int i = 0; i < 256; ++i)
       if (mbar_try_wait(bar, parity)) return true;
     if (*(volatile int*)gave_up) return false;
-    if (now_ns() - start > 4000000000ull) {
+    const unsigned long long now = now_ns();
+    if (start == 0) start = now;
+    if (now - start > 4000000000ull) {
       *(volatile int*)gave_up = 1;
       atomicOr(&g_tile_flags, kErrTimeout);
       return false;
@@ -83,23 +87,39 @@ __device__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up)
   }
 }
 
-// Shared-memory operand of tcgen05.mma, 128-byte swizzle: `lead` and `stride`
-// are the byte distances of 64-element blocks along the contiguous axis (used
-// where that axis is not the summed one) and of groups of 8 rows.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32_t stride) {
-  return (uint64_t)(addr >> 4 & 0x3FFF) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// The same for a whole warp.
+__device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parity, int* gave_up) {
+  return __all_sync(~0u, wait_bar(bar, parity, gave_up));
 }
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+// The first lane's value in every lane, which the compiler then knows to be uniform.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(~0u, v, 0); }
+
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
+
+// Shared-memory operands of tcgen05.mma, 128-byte swizzle: the low word holds the
+// address and, for an operand whose contiguous axis is not the summed one (V),
+// the distance of its blocks of 64 along that axis; the high word the distance
+// of groups of 8 rows (1,024 bytes) and the form.
+constexpr uint32_t kOperandHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t operand_low(uint32_t addr, uint32_t blocks) { return addr >> 4 | blocks >> 4 << 16; }
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, uint32_t add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((int)add)
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(add), "r"(kOperandHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, uint32_t add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((int)add)
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(add), "r"(kOperandHigh)
       : "memory");
 }
 __device__ __forceinline__ void commit(unsigned long long* bar) {
@@ -128,6 +148,21 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
       "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld16(float* r, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+        "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 
@@ -166,7 +201,7 @@ __device__ __forceinline__ bool not_finite2(uint32_t x) {
 // sum over k < n of floor((a + b k) / 128), a, b >= 0: after the whole parts are
 // taken out, the points under the line are counted by the other axis, as in
 // Euclid's algorithm.
-__device__ int64_t floor_sum(uint32_t n, uint32_t b, uint32_t a) {
+__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t b, uint32_t a) {
   int64_t sum = 0;
   uint32_t m = 128;
   while (n > 0) {
@@ -223,12 +258,12 @@ struct TileWalk {
   int req, head, pair, t0, cost, seg;
   int64_t left;
   TileReq x;
-  int tok0, n[2], tiles;  // first token; key tiles of each row tile from t0; their maximum
+  int tok0, n0, n1, tiles;  // first token; key tiles of each row tile from t0; their maximum
   int lim_first;          // what the item's first row sees
   bool starts, ends;
 
   // By whole warps.
-  __device__ void begin(const AttnParams& p, const AttnRange& range) {
+  __device__ __forceinline__ void begin(const AttnParams& p, const AttnRange& range) {
     req = range.req;
     left = range.end - range.begin;
     x = tile_req(p, req);
@@ -254,22 +289,21 @@ struct TileWalk {
     ends = t0 + seg == cost;
     tok0 = pair * 2 * x.toks;
     lim_first = attn_limit(p, x.r, tok0);
-    tiles = 0;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int64_t first = (int64_t)tok0 + s * x.toks;
-      n[s] = 0;
-      if (first < x.r.ql) {
-        const int end = (int)(first + x.toks < x.r.ql ? first + x.toks : x.r.ql);
-        const int lim = attn_limit(p, x.r, end - 1), need = lim == 0 ? 0 : (lim - 1) / kKeys + 1;
-        const int stop = t0 + seg < need ? t0 + seg : need;
-        n[s] = stop > t0 ? stop - t0 : 0;
-      }
-      tiles = n[s] > tiles ? n[s] : tiles;
-    }
+    n0 = key_count(p, tok0);
+    n1 = key_count(p, (int64_t)tok0 + x.toks);
+    tiles = n0 > n1 ? n0 : n1;
   }
+  // Key tiles from t0 on that some row of the tile beginning at token `first` sees.
+  __device__ __forceinline__ int key_count(const AttnParams& p, int64_t first) const {
+    if (first >= x.r.ql) return 0;
+    const int end = (int)(first + x.toks < x.r.ql ? first + x.toks : x.r.ql);
+    const int lim = attn_limit(p, x.r, end - 1), need = lim == 0 ? 0 : (lim - 1) / kKeys + 1;
+    const int stop = t0 + seg < need ? t0 + seg : need;
+    return stop > t0 ? stop - t0 : 0;
+  }
+  __device__ __forceinline__ int count(int s) const { return s ? n1 : n0; }
   // False after the last item.
-  __device__ bool next(const AttnParams& p) {
+  __device__ __forceinline__ bool next(const AttnParams& p) {
     left -= seg;
     if (left <= 0) return false;
     t0 = 0;
@@ -307,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       mbar_init(&sh.full[s], 1);
       mbar_init(&sh.empty[s], 1);
       mbar_init(&sh.asked[s], 1);
-      mbar_init(&sh.checked[s], 2);
+      mbar_init(&sh.checked[s], 1);
     }
     mbar_init(&sh.q_full, 1);
     mbar_init(&sh.q_empty, 1);
@@ -341,140 +375,175 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   const uint32_t tmem = sh.tmem;  // S0/P0 at 0, S1/P1 at 128, O0 at 256, O1 at 384
   int* const gave_up = &sh.gave_up;
 
-  TileWalk w;
-  w.begin(p, range);
-
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");  // 2 x 224 + 56 = 3 x 168
-    if (warp == 9) {
-      // ---- copies ----
-      const int box = p.box, per = kKeys / box, mine = lane % per, blk = lane / per;
-      uint32_t idx = 0, item = 0, gt = 0;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // 2 x 216 + 72 = 3 x 168
+    if (warp == 9 || warp == 10) {
+      // ---- copies: warp 9 queries and keys, warp 10 values ----
+      // Tile g of the block (over all its items) has its keys in use 2 g of the
+      // ring and its values in use 2 g + 1.  A warp waits for every second use's
+      // slot only; the products release the uses in order, so a use that has
+      // been released implies all before it, and no wait is a phase early.
+      TileWalk w;
+      w.begin(p, range);
+      const int v = warp - 9, box = p.box, per = kKeys / box;
+      const CUtensorMap* const map = v ? &p.map_v : &p.map_k;
+      uint32_t item = 0, gt = 0;
       bool ok = true;
-      auto load = [&](char* dst, const CUtensorMap* map, int t, int id, unsigned long long* bar) {
-        const int slot = (t * kKeys) & ((1 << p.page_log2) - 1);
-        if (lane < per * C::kBlk)
-          tma_load_4d(dst + blk * kKeys * 128 + mine * box * 128, map, blk * 64, slot, w.head, id, bar);
-      };
       do {
         if (w.tiles == 0) continue;
-        // queries
-        if (item > 0) ok = ok && __all_sync(~0u, wait_bar(&sh.q_empty, (item - 1) & 1, gave_up));
-        if (!ok) break;
-        if (lane == 0) {
-          const int tiles = w.n[1] > 0 ? 2 : 1;  // the second row tile sees at least what the first does
-          mbar_arrive_expect_tx(&sh.q_full, tiles * w.x.toks * p.group * 128 * C::kBlk);
-          for (int s = 0; s < tiles; ++s)
-            for (int b = 0; b < C::kBlk; ++b)
-              tma_load_3d(qbuf + (s * C::kBlk + b) * 128 * 128, &p.map_q, b * 64, w.head * p.group,
-                          w.x.r.q0 + w.tok0 + s * w.x.toks, &sh.q_full);
+        const int head = (int)uniform((uint32_t)w.head), t0 = (int)uniform((uint32_t)w.t0), tiles = (int)uniform((uint32_t)w.tiles);
+        if (v == 0) {
+          if (item > 0) ok = ok && wait_all(&sh.q_empty, (item - 1) & 1, gave_up);
+          if (!ok) break;
+          const int rows = w.n1 > 0 ? 2 : 1;  // the second row tile sees at least what the first does
+          const int tok = (int)uniform((uint32_t)(w.x.r.q0 + w.tok0)), toks = w.x.toks;
+          if (lane == 0) mbar_arrive_expect_tx(&sh.q_full, rows * toks * p.group * 128 * C::kBlk);
+          __syncwarp();
+          if (elect_one())
+            for (int s = 0; s < rows; ++s)
+#pragma unroll
+              for (int b = 0; b < C::kBlk; ++b)
+                tma_load_3d(qbuf + (s * C::kBlk + b) * 128 * 128, &p.map_q, b * 64, head * p.group, tok + s * toks, &sh.q_full);
+          __syncwarp();
+          ++item;
         }
-        ++item;
         const int32_t* row = p.table + (int64_t)w.req * p.table_stride;
-        auto page_of = [&](int j) -> int {
-          const int64_t key = (int64_t)(w.t0 + j) * kKeys + mine * box;
-          if (j >= w.tiles || key >= w.x.r.kvl) return -1;
+        const int kvl = w.x.r.kvl;
+        auto page_of = [&](int j) -> int {  // lane b: page of the tile's b-th box
+          const int64_t key = (int64_t)(t0 + j) * kKeys + lane * box;
+          if (j >= tiles || lane >= per || key >= kvl) return -1;
           const int id = row[key >> p.page_log2];
           return id < 0 || id >= p.n_pages ? -1 : id;
         };
         int next = page_of(0);
-        for (int j = 0; j < w.tiles; ++j, ++gt) {
+        for (int j = 0; j < tiles; ++j, ++gt) {
           const int id = next;
           next = page_of(j + 1);
+          const uint32_t idx = 2 * gt + v;
+          const int s = idx % C::kSlots;
+          if (idx >= C::kSlots) ok = ok && wait_all(&sh.empty[s], (idx / C::kSlots - 1) & 1, gave_up);
+          if (!ok) break;
           const unsigned held = __ballot_sync(~0u, id >= 0);
-#pragma unroll
-          for (int v = 0; v < 2; ++v, ++idx) {
-            const int s = idx % C::kSlots;
-            if (idx >= C::kSlots) ok = ok && __all_sync(~0u, wait_bar(&sh.empty[s], (idx / C::kSlots - 1) & 1, gave_up));
-            if (!ok) break;
-            if (lane == 0) {
-              if (v == 0) {
-                uint32_t m = 0;
-                for (int g = 0; g < kKeys / 8; ++g) m |= (held >> (g * 8 / box) & 1u) << g;
-                sh.held[gt % kHeldSets] = m;
-              }
-              mbar_arrive_expect_tx(&sh.full[s], C::kSlot);
+          if (lane == 0) {
+            if (v == 0) {
+              uint32_t m = 0;
+              for (int g = 0; g < kKeys / 8; ++g) m |= (held >> (g * 8 / box) & 1u) << g;
+              sh.held[gt % kHeldSets] = m;
             }
-            __syncwarp();
-            load(ring + s * C::kSlot, v ? &p.map_v : &p.map_k, w.t0 + j, id, &sh.full[s]);
-            if (v == 1 && w.partly(j)) {
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&sh.asked[s]);
+            mbar_arrive_expect_tx(&sh.full[s], C::kSlot);
+          }
+          __syncwarp();
+          const int slot = ((t0 + j) * kKeys) & ((1 << p.page_log2) - 1);
+          char* const dst = ring + s * C::kSlot;
+          for (int i = 0; i < per; ++i) {
+            const int page = __shfl_sync(~0u, id, i);
+            if (elect_one()) {
+#pragma unroll
+              for (int b = 0; b < C::kBlk; ++b)
+                tma_load_4d(dst + b * kKeys * 128 + i * box * 128, map, b * 64, slot, head, page, &sh.full[s]);
             }
           }
-          if (!ok) break;
+          __syncwarp();
+          if (v == 1 && w.partly(j) && lane == 0) mbar_arrive(&sh.asked[s]);
         }
       } while (ok && w.next(p));
       if (!ok) {  // copies in flight land before the block ends
-        for (uint32_t k = idx > C::kSlots ? idx - C::kSlots : 0; k < idx; ++k)
-          for (int i = 0; i < 1 << 16 && !mbar_try_wait(&sh.full[k % C::kSlots], (k / C::kSlots) & 1); ++i) {
+        for (uint32_t k = gt > C::kSlots ? gt - C::kSlots : 0; k < gt; ++k) {
+          const uint32_t idx = 2 * k + v;
+          for (int i = 0; i < 1 << 16 && !mbar_try_wait(&sh.full[idx % C::kSlots], (idx / C::kSlots) & 1); ++i) {
           }
+        }
       }
     } else if (warp == 8) {
       // ---- products ----
-      if (lane == 0) {
-        const int steps = (p.dim + 15) / 16;  // of 16 elements of a head; columns of O likewise
-        const uint32_t kind = 1u << 4 | (F16 ? 0u : 1u << 7 | 1u << 10) | 8u << 24;  // 32-bit sums, 128 rows
-        const uint32_t desc_s = kind | (kKeys >> 3) << 17, desc_o = kind | 1u << 16 | (uint32_t)(steps * 16 >> 3) << 17;
-        const uint32_t q_at = smem_u32(qbuf), ring_at = smem_u32(ring);
-        uint32_t idx = 0, item = 0, checks = 0, ready[2] = {0, 0};
-        bool ok = true;
-        auto scores = [&](int s, uint32_t k_at) {
-          for (int k = 0; k < steps; ++k) {
-            const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
-            mma_ss(tmem + s * 128, operand(q_at + s * C::kBlk * 128 * 128 + off, 16, 1024), operand(k_at + off, 16, 1024), desc_s, k > 0);
+      // The whole warp takes every step and one lane issues, with operands that
+      // the compiler knows to be the same in all lanes (the broadcasts): issued
+      // from a branch of one lane, each product cost about 100 cycles.
+      TileWalk w;
+      w.begin(p, range);
+      const uint32_t acc = uniform(tmem);
+      const int steps = (p.dim + 15) / 16;  // of 16 elements of a head; columns of O likewise
+      const uint32_t kind = 1u << 4 | (F16 ? 0u : 1u << 7 | 1u << 10) | 8u << 24;  // 32-bit sums, 128 rows
+      const uint32_t desc_s = kind | (kKeys >> 3) << 17, desc_o = kind | 1u << 16 | (uint32_t)(steps * 16 >> 3) << 17;
+      const uint32_t q_at = operand_low(smem_u32(qbuf), 0), ring_at = operand_low(smem_u32(ring), 0);
+      constexpr uint32_t kSlotStep = C::kSlot >> 4, kBlocks = (uint32_t)(kKeys * 128) >> 4 << 16;
+      uint32_t idx = 0, item = 0, checks = 0, ready = 0;
+      bool ok = true;
+      auto scores = [&](int s, uint32_t k_at) {
+        const uint32_t a = q_at + s * (C::kBlk * 128 * 128 >> 4);
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < HDP / 16; ++k) {
+            const uint32_t off = (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2;
+            if (k < steps) mma_ss(acc + s * 128, a + off, k_at + off, desc_s, k > 0);
           }
           commit(&sh.s_full[s]);
-        };
-        do {
-          if (w.tiles == 0) continue;
-          ok = wait_bar(&sh.q_full, item & 1, gave_up);
-          ++item;
-          if (!ok) break;
-          // idx: slot number of tile j's keys; its values are idx + 1
-          int s0 = idx % C::kSlots;
-          ok = wait_bar(&sh.full[s0], (idx / C::kSlots) & 1, gave_up);
-          if (!ok) break;
-          fence_after();
-          for (int s = 0; s < 2; ++s)
-            if (w.n[s] > 0) scores(s, ring_at + s0 * C::kSlot);
-          commit(&sh.empty[s0]);
-          for (int j = 0; j < w.tiles && ok; ++j, idx += 2) {
-            const bool more = j + 1 < w.tiles;
-            if (!more) commit(&sh.q_empty);
-            const uint32_t vi = idx + 1, ki = idx + 2;
-            const int sv = vi % C::kSlots, sk = ki % C::kSlots;
-            ok = wait_bar(&sh.full[sv], (vi / C::kSlots) & 1, gave_up);
-            if (ok && w.partly(j)) {
-              ok = wait_bar(&sh.checked[sv], checks >> sv & 1, gave_up);
-              checks ^= 1u << sv;
-            }
-            if (ok && more) ok = wait_bar(&sh.full[sk], (ki / C::kSlots) & 1, gave_up);
-            for (int s = 0; s < 2 && ok; ++s) {
-              if (j >= w.n[s]) continue;
-              ok = wait_bar(&sh.p_ready[s], ready[s] & 1, gave_up);
-              ++ready[s];
-              if (!ok) break;
-              fence_after();
-              for (int k = 0; k < kKeys / 16; ++k)
-                mma_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, operand(ring_at + sv * C::kSlot + k * 2048, kKeys * 128, 1024),
-                       desc_o, j > 0 || k > 0);
-              if (s == 1 || j >= w.n[1]) commit(&sh.empty[sv]);
-              if (j + 1 == w.n[s]) commit(&sh.o_full[s]);
-              else scores(s, ring_at + sk * C::kSlot);
-            }
-            if (!ok) break;
-            if (more) commit(&sh.empty[sk]);
-          }
-        } while (ok && w.next(p));
-        // nothing in flight when the tensor memory goes
-        commit(&sh.drain);
-        for (int i = 0; i < 1 << 20 && !mbar_try_wait(&sh.drain, 0); ++i) {
         }
+        __syncwarp();
+      };
+      auto committed = [&](unsigned long long* bar) {
+        if (elect_one()) commit(bar);
+        __syncwarp();
+      };
+      do {
+        const int tiles = (int)uniform((uint32_t)w.tiles), n0 = (int)uniform((uint32_t)w.n0), n1 = (int)uniform((uint32_t)w.n1);
+        const int sure = (int)uniform((uint32_t)(w.lim_first / kKeys - w.t0));  // tiles before it are seen whole by all rows
+        if (tiles == 0) continue;
+        ok = wait_all(&sh.q_full, item & 1, gave_up);
+        ++item;
+        if (!ok) break;
+        // idx: slot number of tile j's keys; its values are idx + 1
+        const int s0 = idx % C::kSlots;
+        ok = wait_all(&sh.full[s0], (idx / C::kSlots) & 1, gave_up);
+        if (!ok) break;
+        fence_after();
+        if (n0 > 0) scores(0, ring_at + s0 * kSlotStep);
+        if (n1 > 0) scores(1, ring_at + s0 * kSlotStep);
+        committed(&sh.empty[s0]);
+        for (int j = 0; j < tiles; ++j, idx += 2) {
+          const bool more = j + 1 < tiles;
+          if (!more) committed(&sh.q_empty);
+          const uint32_t vi = idx + 1, ki = idx + 2;
+          const int sv = vi % C::kSlots, sk = ki % C::kSlots;
+          ok = wait_all(&sh.full[sv], (vi / C::kSlots) & 1, gave_up);
+          if (ok && j >= sure) {
+            ok = wait_all(&sh.checked[sv], checks >> sv & 1, gave_up);
+            checks ^= 1u << sv;
+          }
+          if (ok && more) ok = wait_all(&sh.full[sk], (ki / C::kSlots) & 1, gave_up);
+          if (!ok) break;
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const int n = s ? n1 : n0;
+            if (j >= n) continue;
+            ok = ok && wait_all(&sh.p_ready[s], ready >> s & 1, gave_up);
+            ready ^= 1u << s;
+            if (!ok) break;
+            fence_after();
+            const uint32_t v_at = (ring_at + sv * kSlotStep) | kBlocks;
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < kKeys / 16; ++k)
+                mma_ts(acc + 256 + s * 128, acc + s * 128 + k * 8, v_at + k * (2048 >> 4), desc_o, j > 0 || k > 0);
+              if (s == 1 || j >= n1) commit(&sh.empty[sv]);
+              if (j + 1 == n) commit(&sh.o_full[s]);
+            }
+            __syncwarp();
+            if (j + 1 < n) scores(s, ring_at + sk * kSlotStep);
+          }
+          if (!ok) break;
+          if (more) committed(&sh.empty[sk]);
+        }
+      } while (ok && w.next(p));
+      // nothing in flight when the tensor memory goes
+      committed(&sh.drain);
+      for (int i = 0; i < 1 << 20 && !mbar_try_wait(&sh.drain, 0); ++i) {
       }
       __syncwarp();
     } else {
       // ---- values that some row must not see ----
+      TileWalk w;
+      w.begin(p, range);
       uint32_t idx = 0, item = 0, asks = 0;
       bool ok = true;
       do {
@@ -483,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           idx += 2 * w.tiles;
           continue;
         }
-        uint32_t* odd = sh.odd[item % kOddSets][warp - 10];
+        uint32_t* odd = sh.odd[item % kOddSets];
         ++item;
         if (lane < 9) odd[lane] = 0;
         __syncwarp();
@@ -492,32 +561,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           const uint32_t vi = idx + 1;
           const int s = vi % C::kSlots;
           // the copy of this use of the slot is under way once it is asked for, so the wait for it is for this use
-          ok = __all_sync(~0u, wait_bar(&sh.asked[s], asks >> s & 1, gave_up));
+          ok = wait_all(&sh.asked[s], asks >> s & 1, gave_up);
           asks ^= 1u << s;
-          ok = ok && __all_sync(~0u, wait_bar(&sh.full[s], (vi / C::kSlots) & 1, gave_up));
+          ok = ok && wait_all(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
           if (!ok) break;
           const uint32_t at = smem_u32(ring + s * C::kSlot);
           const int key0 = (w.t0 + j) * kKeys;
           const int from = w.lim_first > key0 ? w.lim_first - key0 : 0;
           bool wrote = false;
-          for (int row = from + (warp - 10); row < kKeys; row += 2) {
-            bool bad = false;
-            for (int ch = lane; ch < HDP / 8; ch += 32) {
-              uint4 v;
-              asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                           : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                           : "r"(at + (ch >> 3) * (kKeys * 128) + row * 128 + ((ch & 7) << 4)));
-              bad |= not_finite2<F16>(v.x) || not_finite2<F16>(v.y) || not_finite2<F16>(v.z) || not_finite2<F16>(v.w);
+          // lane i looks at the i-th 16 bytes of two rows (four where a head has 64 elements)
+          constexpr int kChunks = HDP / 8, kAtOnce = 32 / kChunks;
+          for (int row0 = from; row0 < kKeys; row0 += 4 * kAtOnce) {
+            uint4 x[4];
+            uint32_t place[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int row = row0 + u * kAtOnce + lane / kChunks, ch = lane % kChunks;
+              place[u] = at + (ch >> 3) * (kKeys * 128) + row * 128 + ((ch & 7) << 4);  // any order within the row's 128 bytes
+              x[u] = make_uint4(0, 0, 0, 0);
+              if (row < kKeys)
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[u].x), "=r"(x[u].y), "=r"(x[u].z), "=r"(x[u].w) : "r"(place[u]));
             }
-            if (!__any_sync(~0u, bad)) continue;
-            wrote = true;
-            for (int ch = lane; ch < HDP / 8; ch += 32)
-              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at + (ch >> 3) * (kKeys * 128) + row * 128 + ((ch & 7) << 4)), "r"(0)
-                           : "memory");
-            const int a = key0 + row - w.lim_first;  // at most one per token of the item
-            if (lane == 0 && key0 + row < w.x.r.kvl && a < 256) {
-              odd[a >> 5] |= 1u << (a & 31);
-              odd[8] = 1;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const bool bad = not_finite2<F16>(x[u].x) || not_finite2<F16>(x[u].y) || not_finite2<F16>(x[u].z) || not_finite2<F16>(x[u].w);
+              const unsigned hit = __ballot_sync(~0u, bad);
+              if (hit == 0) continue;
+              wrote = true;
+#pragma unroll
+              for (int h = 0; h < kAtOnce; ++h) {
+                const unsigned lanes = kAtOnce == 1 ? ~0u : 0xFFFFu >> (16 - kChunks) << (h * kChunks);
+                if (!(hit & lanes)) continue;
+                if (lanes >> lane & 1u) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(place[u]), "r"(0) : "memory");
+                const int key = key0 + row0 + u * kAtOnce + h, a = key - w.lim_first;  // a < 256 for every token of the item
+                if (lane == 0 && key < w.x.r.kvl && a < 256) {
+                  odd[a >> 5] |= 1u << (a & 31);
+                  odd[8] = 1;
+                }
+              }
             }
           }
           if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -527,8 +608,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       } while (ok && w.next(p));
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---- one row per thread ----
+    TileWalk w;
+    w.begin(p, range);
     const int s = warp >> 2, r = tid & 127, r_tok = r / p.group, sub = r % p.group;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + s * 128 + lanes, t_o = tmem + 256 + s * 128 + lanes;
     uint32_t scored = 0, done = 0, item = 0, gt = 0;
@@ -540,8 +623,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       const int lim = valid ? attn_limit(p, w.x.r, tok) : INT32_MAX;
       const int lim_tile = first_tok < w.x.r.ql ? attn_limit(p, w.x.r, (int)first_tok) : 0;  // what every row of the tile sees
       float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < w.n[s]; ++j) {
-        ok = __all_sync(~0u, wait_bar(&sh.s_full[s], scored & 1, gave_up));
+      for (int j = 0; j < w.count(s); ++j) {
+        ok = wait_all(&sh.s_full[s], scored & 1, gave_up);
         ++scored;
         if (!ok) break;
         fence_after();
@@ -571,31 +654,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           const float a = grows ? ex2(m - safe) : 1.f;
           m = grows ? top : m;
           l *= a;
-          for (int c = 0; c < HDP / 32; ++c) {
-            float o[32];
-            uint32_t u[32];
-            tmem_ld32(o, t_o + 32 * c);
+#pragma unroll 1
+          for (int c = 0; c < HDP; c += 16) {
+            float o[16];
+            uint32_t u[16];
+            tmem_ld16(o, t_o + c);
             wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(o[e] * a);
-            tmem_st32(t_o + 32 * c, u);
+            for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(o[e] * a);
+            tmem_st16(t_o + c, u);
           }
           wait_st();
         }
         const float ref = m == -INFINITY ? 0.f : m;
+        // P, rounded to the cache's type (the operand's), over S
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < 128; ++c) {
-          f[c] = ex2(fmaf(f[c], p.scale_log2, -ref));
-          sum[c & 3] += f[c];
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t x[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float a = ex2(fmaf(f[c + e], p.scale_log2, -ref)), b = ex2(fmaf(f[c + e + 1], p.scale_log2, -ref));
+            sum[e & 2] += a;
+            sum[(e & 2) + 1] += b;
+            x[e / 2] = pack2<F16>(a, b);
+          }
+          tmem_st16(t_s + c / 2, x);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        // P, rounded to the cache's type (the operand's), over S
-        uint32_t x[64];
-#pragma unroll
-        for (int c = 0; c < 64; ++c) x[c] = pack2<F16>(f[2 * c], f[2 * c + 1]);
-        tmem_st32(t_s, x);
-        tmem_st32(t_s + 32, x + 32);
         wait_st();
         fence_before();
         __syncwarp();
@@ -603,10 +689,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       }
       if (!ok) break;
       gt += w.tiles;
-      const uint32_t(*odd)[9] = nullptr;
+      const uint32_t* odd = nullptr;
       if (w.any_partly()) odd = sh.odd[item++ % kOddSets];
-      if (w.n[s] > 0) {
-        ok = __all_sync(~0u, wait_bar(&sh.o_full[s], done & 1, gave_up));
+      if (w.count(s) > 0) {
+        ok = wait_all(&sh.o_full[s], done & 1, gave_up);
         ++done;
         if (!ok) break;
         fence_after();
@@ -614,14 +700,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       // ---- out ----
       const bool whole = w.starts && w.ends;
       if (first_tok < w.x.r.ql) {
-        const bool extra = odd && w.n[s] > 0 && (odd[0][8] || odd[1][8]);
+        const bool extra = odd && w.count(s) > 0 && odd[8];
         const float inv = l == 0.f ? 0.f : 1.f / l, scale = whole ? inv : 1.f;
         const int64_t tok_at = (int64_t)w.x.r.q0 + tok, head = (int64_t)w.head * p.group + sub;
         char* out = p.out + 2 * (tok_at * p.out_tok + head * p.out_head);
         float* part = p.part + ((int64_t)blockIdx.x * 2 + (w.starts ? 1 : 0)) * (kRows * HDP + 2 * kRows);
         for (int c = 0; c < HDP / 32; ++c) {
           float o[32];
-          if (w.n[s] > 0) {
+          if (w.count(s) > 0) {
             tmem_ld32(o, t_o + 32 * c);
             wait_ld();
           } else {
@@ -633,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             const char* q = p.q + 2 * (tok_at * p.q_tok + head * p.q_head);
             for (int a = 0; a < 256; ++a) {
               const int key = w.lim_first + a;
-              if (!((odd[0][a >> 5] | odd[1][a >> 5]) >> (a & 31) & 1u) || key >= lim) continue;
+              if (!(odd[a >> 5] >> (a & 31) & 1u) || key >= lim) continue;
               const int64_t id = p.table[(int64_t)w.req * p.table_stride + (key >> p.page_log2)];
               if (id < 0 || id >= p.n_pages) continue;
               const int64_t slot = key & ((1 << p.page_log2) - 1);
@@ -748,11 +834,11 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
 template <int HDP, bool F16>
 cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream) {
   using C = TileCfg<HDP>;
-  // the warpgroups' shares (2 x 224 + 56) have to fit the registers of the launch, or they would wait for ever
+  // the warpgroups' shares (2 x 216 + 72) have to fit the registers of the launch, or they would wait for ever
   static const cudaError_t fits = [] {
     cudaFuncAttributes a;
     const cudaError_t e = cudaFuncGetAttributes(&a, k_attend_tile<HDP, F16>);
-    return e != cudaSuccess ? e : a.numRegs * 3 >= 2 * 224 + 56 ? cudaSuccess : cudaErrorInvalidConfiguration;
+    return e != cudaSuccess ? e : a.numRegs * 3 >= 2 * 216 + 72 ? cudaSuccess : cudaErrorInvalidConfiguration;
   }();
   if (fits != cudaSuccess) return fits;
   static std::atomic<uint64_t> allowed;
