@@ -68,28 +68,27 @@ __device__ __forceinline__ unsigned long long now_ns() {
   return t;
 }
 
-// Bounded wait: false once the block has given up, or after four seconds.  The
-// clock is looked at after the first polls only: reading it takes longer than
-// most waits.
-__device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up) {
+// Bounded wait of a whole warp: false once the block has given up, or after four
+// seconds.  The clock is looked at after the first polls only: reading it takes
+// longer than most waits.
+__device__ __forceinline__ bool wait_on(unsigned long long* bar, uint32_t parity, int* gave_up) {
   unsigned long long start = 0;
   for (;;) {
     for (int i = 0; i < 256; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
-    if (*(volatile int*)gave_up) return false;
+      if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
     const unsigned long long now = now_ns();
     if (start == 0) start = now;
+    bool over = *(volatile int*)gave_up != 0;
     if (now - start > 4000000000ull) {
+      over = true;
       *(volatile int*)gave_up = 1;
       atomicOr(&g_tile_flags, kErrTimeout);
-      return false;
     }
+    if (__any_sync(~0u, over)) return false;
   }
 }
-
-// The same for a whole warp.
 __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parity, int* gave_up) {
-  return __all_sync(~0u, wait_bar(bar, parity, gave_up));
+  return __all_sync(~0u, mbar_try_wait(bar, parity)) || wait_on(bar, parity, gave_up);
 }
 
 // The first lane's value in every lane, which the compiler then knows to be uniform.
@@ -140,17 +139,6 @@ __device__ __forceinline__ void tmem_ld32(float* r, uint32_t addr) {
         "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
       : "r"(addr));
 }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-
 __device__ __forceinline__ void tmem_ld16(float* r, uint32_t addr) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -172,6 +160,29 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
           smem_u32(dst)),
       "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
       : "memory");
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Pairs of 32-bit values in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
 template <bool F16>
@@ -446,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           __syncwarp();
           if (v == 1 && w.partly(j) && lane == 0) mbar_arrive(&sh.asked[s]);
         }
-      } while (ok && w.next(p));
+      } while (ok && uniform(w.next(p)));
       if (!ok) {  // copies in flight land before the block ends
         for (uint32_t k = gt > C::kSlots ? gt - C::kSlots : 0; k < gt; ++k) {
           const uint32_t idx = 2 * k + v;
@@ -461,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       // from a branch of one lane, each product cost about 100 cycles.
       TileWalk w;
       w.begin(p, range);
-      const uint32_t acc = uniform(tmem);
+      constexpr uint32_t acc = 0;  // all 512 columns are this block's: they begin at 0
       const int steps = (p.dim + 15) / 16;  // of 16 elements of a head; columns of O likewise
       const uint32_t kind = 1u << 4 | (F16 ? 0u : 1u << 7 | 1u << 10) | 8u << 24;  // 32-bit sums, 128 rows
       const uint32_t desc_s = kind | (kKeys >> 3) << 17, desc_o = kind | 1u << 16 | (uint32_t)(steps * 16 >> 3) << 17;
@@ -534,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           if (!ok) break;
           if (more) committed(&sh.empty[sk]);
         }
-      } while (ok && w.next(p));
+      } while (ok && uniform(w.next(p)));
       // nothing in flight when the tensor memory goes
       committed(&sh.drain);
       for (int i = 0; i < 1 << 20 && !mbar_try_wait(&sh.drain, 0); ++i) {
@@ -640,11 +651,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           for (int c = 0; c < 128; ++c)
             if (c >= sees || !(held >> (c >> 3) & 1u)) f[c] = -INFINITY;
         }
-        float mx[4] = {f[0], f[1], f[2], f[3]};
+        float mx[4];
 #pragma unroll
-        for (int c = 4; c < 128; c += 8)
+        for (int q = 0; q < 4; ++q) mx[q] = max3(f[q], f[4 + q], f[8 + q]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) mx[q] = c + 4 + q < 128 ? fmaxf(fmaxf(mx[q], f[c + q]), f[c + 4 + q]) : fmaxf(mx[q], f[c + q]);
+        for (int c = 12; c + 8 <= 128; c += 8)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], f[c + q], f[c + 4 + q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mx[q] = fmaxf(mx[q], f[124 + q]);
         const float top = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2);
         if (j == 0) {
           m = top;
@@ -668,20 +683,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         }
         const float ref = m == -INFINITY ? 0.f : m;
         // P, rounded to the cache's type (the operand's), over S
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint64_t sum[2] = {0, 0};  // pairs of 32-bit sums
+        const uint64_t mul = pair(p.scale_log2, p.scale_log2), off = pair(-ref, -ref);
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
           uint32_t x[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const float a = ex2(fmaf(f[c + e], p.scale_log2, -ref)), b = ex2(fmaf(f[c + e + 1], p.scale_log2, -ref));
-            sum[e & 2] += a;
-            sum[(e & 2) + 1] += b;
+            float a, b;
+            unpair(fma2(pair(f[c + e], f[c + e + 1]), mul, off), a, b);
+            a = ex2(a);
+            b = ex2(b);
+            sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair(a, b));
             x[e / 2] = pack2<F16>(a, b);
           }
           tmem_st16(t_s + c / 2, x);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float s0, s1;
+        unpair(add2(sum[0], sum[1]), s0, s1);
+        l += s0 + s1;
         wait_st();
         fence_before();
         __syncwarp();
