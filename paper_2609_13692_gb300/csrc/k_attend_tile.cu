@@ -19,7 +19,8 @@
 //   warps 9, 10     copies: queries once an item and keys, and values, of each
 //                   tile page by page into a ring of slots (with pages of 16 one
 //                   warp's 32 copies a tile take longer than its products)
-//   warp 11         looks at the values of tiles with masked keys (below)
+//   warp 11         waits for the copies on the products' behalf, and looks at
+//                   the values of tiles with masked keys (below)
 //
 // Rescaling O costs a pass over its 128 columns, so it waits until the maximum
 // has grown by 2^8: any reference below the maximum gives the same quotient,
@@ -40,7 +41,7 @@ __device__ int g_tile_flags;
 constexpr int kKeys = 128;     // keys of a tile
 constexpr int kRows = 256;     // rows of a slot of partial results
 constexpr int kThreads = 384;
-constexpr int kOddSets = 8;    // items whose notes are kept apart (ring depth in items + 2)
+constexpr int kOddSets = 4;    // items whose notes are kept apart (warp 11 is at most two ahead of the rows)
 constexpr int kHeldSets = 16;  // key tiles whose page marks are kept apart
 
 template <int HDP>
@@ -53,7 +54,7 @@ struct TileCfg {
 };
 
 struct TileShared {
-  unsigned long long full[8], empty[8], asked[8], checked[8], q_full, q_empty, s_full[2], p_ready[2], o_full[2], drain;
+  unsigned long long full[8], empty[8], q_full, q_empty, s_full[2], p_ready[2], o_full[2], drain;
   uint32_t tmem;
   int gave_up;
   uint32_t held[kHeldSets];
@@ -203,10 +204,12 @@ __device__ __forceinline__ float2 unpack2(uint32_t x) {
   }
   return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
 }
+// Nonzero if one of the eight elements is an infinity or a NaN: an exponent of
+// ones carries into the sign's place when one is added to it.
 template <bool F16>
-__device__ __forceinline__ bool not_finite2(uint32_t x) {
-  constexpr uint32_t e = F16 ? 0x7C00u : 0x7F80u;
-  return (x & e) == e || (x >> 16 & e) == e;
+__device__ __forceinline__ uint32_t not_finite8(const uint4& x) {
+  constexpr uint32_t e = F16 ? 0x7C007C00u : 0x7F807F80u, one = F16 ? 0x04000400u : 0x00800080u;
+  return (((x.x & e) + one) | ((x.y & e) + one) | ((x.z & e) + one) | ((x.w & e) + one)) & 0x80008000u;
 }
 
 // sum over k < n of floor((a + b k) / 128), a, b >= 0: after the whole parts are
@@ -228,6 +231,28 @@ __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t b, uint32_t a)
     b = t;
   }
   return sum;
+}
+
+// Transposes the 4 x 4 pieces of every four lanes.
+__device__ __forceinline__ void swap_with(uint4& x, int lane_mask) {
+  x.x = __shfl_xor_sync(~0u, x.x, lane_mask);
+  x.y = __shfl_xor_sync(~0u, x.y, lane_mask);
+  x.z = __shfl_xor_sync(~0u, x.z, lane_mask);
+  x.w = __shfl_xor_sync(~0u, x.w, lane_mask);
+}
+__device__ __forceinline__ void turn4(uint4* v, int lane) {
+#pragma unroll
+  for (int d = 1; d <= 2; d <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e & d) continue;
+      // the lane without bit d gives v[e | d] for the other's v[e]
+      const bool up = lane & d;
+      uint4 give = up ? v[e] : v[e | d];
+      swap_with(give, d);
+      if (up) v[e] = give;
+      else v[e | d] = give;
+    }
 }
 
 // One request's items: its pairs of row tiles and their key tiles.
@@ -333,8 +358,6 @@ struct TileWalk {
   }
   // Whether some row of the item does not see every key of tile t0 + j.
   __device__ __forceinline__ bool partly(int j) const { return (int64_t)(t0 + j + 1) * kKeys > lim_first; }
-  // Whether the item has such a tile (its last is one if any is).
-  __device__ __forceinline__ bool any_partly() const { return tiles > 0 && partly(tiles - 1); }
 };
 
 template <int HDP, bool F16>
@@ -351,14 +374,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     for (int s = 0; s < C::kSlots; ++s) {
       mbar_init(&sh.full[s], 1);
       mbar_init(&sh.empty[s], 1);
-      mbar_init(&sh.asked[s], 1);
-      mbar_init(&sh.checked[s], 1);
     }
     mbar_init(&sh.q_full, 1);
     mbar_init(&sh.q_empty, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sh.s_full[s], 1);
-      mbar_init(&sh.p_ready[s], 4);
+      mbar_init(&sh.p_ready[s], 5);  // four warps of rows, and warp 11
       mbar_init(&sh.o_full[s], 1);
     }
     mbar_init(&sh.drain, 1);
@@ -455,7 +476,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             }
           }
           __syncwarp();
-          if (v == 1 && w.partly(j) && lane == 0) mbar_arrive(&sh.asked[s]);
         }
       } while (ok && uniform(w.next(p)));
       if (!ok) {  // copies in flight land before the block ends
@@ -478,145 +498,161 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       const uint32_t desc_s = kind | (kKeys >> 3) << 17, desc_o = kind | 1u << 16 | (uint32_t)(steps * 16 >> 3) << 17;
       const uint32_t q_at = operand_low(smem_u32(qbuf), 0), ring_at = operand_low(smem_u32(ring), 0);
       constexpr uint32_t kSlotStep = C::kSlot >> 4, kBlocks = (uint32_t)(kKeys * 128) >> 4 << 16;
-      uint32_t idx = 0, item = 0, checks = 0, ready = 0;
+      uint32_t item = 0, ready = 0;
       bool ok = true;
-      auto scores = [&](int s, uint32_t k_at) {
-        const uint32_t a = q_at + s * (C::kBlk * 128 * 128 >> 4);
-        if (elect_one()) {
+      auto outputs = [&](int s, int slot, bool add) {  // by one lane
+        const uint32_t v_at = (ring_at + slot * kSlotStep) | kBlocks;
 #pragma unroll
-          for (int k = 0; k < HDP / 16; ++k) {
-            const uint32_t off = (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2;
-            if (k < steps) mma_ss(acc + s * 128, a + off, k_at + off, desc_s, k > 0);
-          }
-          commit(&sh.s_full[s]);
+        for (int k = 0; k < kKeys / 16; ++k)
+          mma_ts(acc + 256 + s * 128, acc + s * 128 + k * 8, v_at + k * (2048 >> 4), desc_o, add || k > 0);
+      };
+      auto scores = [&](int s, int slot) {  // by one lane
+        const uint32_t a = q_at + s * (C::kBlk * 128 * 128 >> 4), b = ring_at + slot * kSlotStep;
+#pragma unroll
+        for (int k = 0; k < HDP / 16; ++k) {
+          const uint32_t off = (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2;
+          if (k < steps) mma_ss(acc + s * 128, a + off, b + off, desc_s, k > 0);
         }
-        __syncwarp();
+        commit(&sh.s_full[s]);
       };
-      auto committed = [&](unsigned long long* bar) {
-        if (elect_one()) commit(bar);
-        __syncwarp();
-      };
+      auto after = [](int slot, int n) { return slot + n < C::kSlots ? slot + n : slot + n - C::kSlots; };
+      int sk = 0;          // slot of the next key tile; its values follow
+      uint32_t phase = 0;  // of the ring at that slot
       do {
         const int tiles = (int)uniform((uint32_t)w.tiles), n0 = (int)uniform((uint32_t)w.n0), n1 = (int)uniform((uint32_t)w.n1);
-        const int sure = (int)uniform((uint32_t)(w.lim_first / kKeys - w.t0));  // tiles before it are seen whole by all rows
         if (tiles == 0) continue;
-        ok = wait_all(&sh.q_full, item & 1, gave_up);
+        ok = wait_all(&sh.q_full, item & 1, gave_up) && wait_all(&sh.full[sk], phase, gave_up);
         ++item;
         if (!ok) break;
-        // idx: slot number of tile j's keys; its values are idx + 1
-        const int s0 = idx % C::kSlots;
-        ok = wait_all(&sh.full[s0], (idx / C::kSlots) & 1, gave_up);
-        if (!ok) break;
         fence_after();
-        if (n0 > 0) scores(0, ring_at + s0 * kSlotStep);
-        if (n1 > 0) scores(1, ring_at + s0 * kSlotStep);
-        committed(&sh.empty[s0]);
-        for (int j = 0; j < tiles; ++j, idx += 2) {
+        if (elect_one()) {
+          if (n0 > 0) scores(0, sk);
+          if (n1 > 0) scores(1, sk);
+          commit(&sh.empty[sk]);
+          if (tiles == 1) commit(&sh.q_empty);
+        }
+        __syncwarp();
+        for (int j = 0; j < tiles; ++j) {
+          const int sv = after(sk, 1);
+          if (sk + 2 >= C::kSlots) phase ^= 1;
+          sk = after(sk, 2);
           const bool more = j + 1 < tiles;
-          if (!more) committed(&sh.q_empty);
-          const uint32_t vi = idx + 1, ki = idx + 2;
-          const int sv = vi % C::kSlots, sk = ki % C::kSlots;
-          ok = wait_all(&sh.full[sv], (vi / C::kSlots) & 1, gave_up);
-          if (ok && j >= sure) {
-            ok = wait_all(&sh.checked[sv], checks >> sv & 1, gave_up);
-            checks ^= 1u << sv;
-          }
-          if (ok && more) ok = wait_all(&sh.full[sk], (ki / C::kSlots) & 1, gave_up);
-          if (!ok) break;
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const int n = s ? n1 : n0;
-            if (j >= n) continue;
-            ok = ok && wait_all(&sh.p_ready[s], ready >> s & 1, gave_up);
-            ready ^= 1u << s;
+          // p_ready is complete once P stands, and this tile's values and the
+          // next one's keys are there (warp 11 waits for those): one wait here
+          if (j < n0) {
+            ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
+            ready ^= 1;
             if (!ok) break;
             fence_after();
-            const uint32_t v_at = (ring_at + sv * kSlotStep) | kBlocks;
             if (elect_one()) {
-#pragma unroll
-              for (int k = 0; k < kKeys / 16; ++k)
-                mma_ts(acc + 256 + s * 128, acc + s * 128 + k * 8, v_at + k * (2048 >> 4), desc_o, j > 0 || k > 0);
-              if (s == 1 || j >= n1) commit(&sh.empty[sv]);
-              if (j + 1 == n) commit(&sh.o_full[s]);
+              outputs(0, sv, j > 0);
+              if (j >= n1) commit(&sh.empty[sv]);
+              if (j + 1 < n0) scores(0, sk);
+              else commit(&sh.o_full[0]);
+              if (more && j + 1 >= n1) {
+                commit(&sh.empty[sk]);
+                if (j + 2 == tiles) commit(&sh.q_empty);  // no more scores
+              }
             }
             __syncwarp();
-            if (j + 1 < n) scores(s, ring_at + sk * kSlotStep);
           }
-          if (!ok) break;
-          if (more) committed(&sh.empty[sk]);
+          if (j < n1) {
+            ok = wait_all(&sh.p_ready[1], ready >> 1, gave_up);
+            ready ^= 2;
+            if (!ok) break;
+            fence_after();
+            if (elect_one()) {
+              outputs(1, sv, j > 0);
+              commit(&sh.empty[sv]);
+              if (j + 1 < n1) {
+                scores(1, sk);
+                commit(&sh.empty[sk]);
+                if (j + 2 == tiles) commit(&sh.q_empty);
+              } else {
+                commit(&sh.o_full[1]);
+              }
+            }
+            __syncwarp();
+          }
         }
       } while (ok && uniform(w.next(p)));
       // nothing in flight when the tensor memory goes
-      committed(&sh.drain);
+      if (elect_one()) commit(&sh.drain);
+      __syncwarp();
       for (int i = 0; i < 1 << 20 && !mbar_try_wait(&sh.drain, 0); ++i) {
       }
       __syncwarp();
     } else {
-      // ---- values that some row must not see ----
+      // ---- copies that have landed, and values that some row must not see ----
       TileWalk w;
       w.begin(p, range);
-      uint32_t idx = 0, item = 0, asks = 0;
+      uint32_t idx = 0, item = 0, ready = 0, due = 0;  // idx: ring use of tile j's keys; due: row tiles with a phase to end
       bool ok = true;
       do {
         if (w.tiles == 0) continue;
-        if (!w.any_partly()) {
-          idx += 2 * w.tiles;
-          continue;
-        }
         uint32_t* odd = sh.odd[item % kOddSets];
         ++item;
         if (lane < 9) odd[lane] = 0;
         __syncwarp();
         for (int j = 0; j < w.tiles && ok; ++j, idx += 2) {
-          if (!w.partly(j)) continue;
-          const uint32_t vi = idx + 1;
+          const uint32_t vi = idx + 1, ki = idx + 2;
           const int s = vi % C::kSlots;
-          // the copy of this use of the slot is under way once it is asked for, so the wait for it is for this use
-          ok = wait_all(&sh.asked[s], asks >> s & 1, gave_up);
-          asks ^= 1u << s;
-          ok = ok && wait_all(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
+          ok = wait_all(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
           if (!ok) break;
-          const uint32_t at = smem_u32(ring + s * C::kSlot);
-          const int key0 = (w.t0 + j) * kKeys;
-          const int from = w.lim_first > key0 ? w.lim_first - key0 : 0;
-          bool wrote = false;
-          // lane i looks at the i-th 16 bytes of two rows (four where a head has 64 elements)
-          constexpr int kChunks = HDP / 8, kAtOnce = 32 / kChunks;
-          for (int row0 = from; row0 < kKeys; row0 += 4 * kAtOnce) {
-            uint4 x[4];
-            uint32_t place[4];
+          if (w.partly(j)) {
+            const uint32_t at = smem_u32(ring + s * C::kSlot);
+            const int key0 = (w.t0 + j) * kKeys;
+            const int from = w.lim_first > key0 ? w.lim_first - key0 : 0;
+            bool wrote = false;
+            // lane i looks at the i-th 16 bytes of two rows (four where a head has 64 elements)
+            constexpr int kChunks = HDP / 8, kAtOnce = 32 / kChunks, kLoads = 8;
+            const int ch = lane % kChunks;
+            const uint32_t mine = at + (ch >> 3) * (kKeys * 128) + ((ch & 7) << 4);  // any order within a row's 128 bytes
+#pragma unroll 1
+            for (int row0 = from / (kLoads * kAtOnce) * (kLoads * kAtOnce); row0 < kKeys; row0 += kLoads * kAtOnce) {
+              uint4 x[kLoads];
+              uint32_t any = 0;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const int row = row0 + u * kAtOnce + lane / kChunks, ch = lane % kChunks;
-              place[u] = at + (ch >> 3) * (kKeys * 128) + row * 128 + ((ch & 7) << 4);  // any order within the row's 128 bytes
-              x[u] = make_uint4(0, 0, 0, 0);
-              if (row < kKeys)
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[u].x), "=r"(x[u].y), "=r"(x[u].z), "=r"(x[u].w) : "r"(place[u]));
-            }
+              for (int u = 0; u < kLoads; ++u)
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(x[u].x), "=r"(x[u].y), "=r"(x[u].z), "=r"(x[u].w)
+                             : "r"(mine + (row0 + u * kAtOnce + lane / kChunks) * 128));
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const bool bad = not_finite2<F16>(x[u].x) || not_finite2<F16>(x[u].y) || not_finite2<F16>(x[u].z) || not_finite2<F16>(x[u].w);
-              const unsigned hit = __ballot_sync(~0u, bad);
-              if (hit == 0) continue;
-              wrote = true;
-#pragma unroll
-              for (int h = 0; h < kAtOnce; ++h) {
-                const unsigned lanes = kAtOnce == 1 ? ~0u : 0xFFFFu >> (16 - kChunks) << (h * kChunks);
-                if (!(hit & lanes)) continue;
-                if (lanes >> lane & 1u) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(place[u]), "r"(0) : "memory");
-                const int key = key0 + row0 + u * kAtOnce + h, a = key - w.lim_first;  // a < 256 for every token of the item
+              for (int u = 0; u < kLoads; ++u) any |= not_finite8<F16>(x[u]);
+              if (!__any_sync(~0u, any != 0)) continue;
+#pragma unroll 1
+              for (int row = row0 > from ? row0 : from; row < row0 + kLoads * kAtOnce; ++row) {  // row by row; seldom
+                uint4 y = make_uint4(0, 0, 0, 0);
+                if (lane < kChunks)
+                  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w) : "r"(mine + row * 128));
+                if (!__any_sync(~0u, not_finite8<F16>(y) != 0)) continue;
+                wrote = true;
+                if (lane < kChunks) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(mine + row * 128), "r"(0) : "memory");
+                const int key = key0 + row, a = key - w.lim_first;  // a < 256 for every token of the item
                 if (lane == 0 && key < w.x.r.kvl && a < 256) {
                   odd[a >> 5] |= 1u << (a & 31);
                   odd[8] = 1;
                 }
               }
             }
+            if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
           }
-          if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          if (j + 1 < w.tiles) ok = wait_all(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
+          if (!ok) break;
+          // not a tile ahead of the rows, or two arrivals would count in one phase
+          if (due & 1) ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
+          if (ok && (due & 2)) ok = wait_all(&sh.p_ready[1], ready >> 1, gave_up);
+          if (!ok) break;
+          ready ^= due;
+          due = (j < w.n0 ? 1 : 0) | (j < w.n1 ? 2 : 0);
+          if (lane == 0) {
+            if (due & 1) mbar_arrive(&sh.p_ready[0]);
+            if (due & 2) mbar_arrive(&sh.p_ready[1]);
+          }
           __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.checked[s]);
         }
-      } while (ok && w.next(p));
+      } while (ok && uniform(w.next(p)));
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -710,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       if (!ok) break;
       gt += w.tiles;
       const uint32_t* odd = nullptr;
-      if (w.any_partly()) odd = sh.odd[item++ % kOddSets];
+      if (w.tiles > 0) odd = sh.odd[item++ % kOddSets];
       if (w.count(s) > 0) {
         ok = wait_all(&sh.o_full[s], done & 1, gave_up);
         ++done;
@@ -723,7 +759,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         const bool extra = odd && w.count(s) > 0 && odd[8];
         const float inv = l == 0.f ? 0.f : 1.f / l, scale = whole ? inv : 1.f;
         const int64_t tok_at = (int64_t)w.x.r.q0 + tok, head = (int64_t)w.head * p.group + sub;
-        char* out = p.out + 2 * (tok_at * p.out_tok + head * p.out_head);
+        char* const out = valid ? p.out + 2 * (tok_at * p.out_tok + head * p.out_head) : nullptr;
+        char* rows4[4];  // of the four lanes of a group
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rows4[e] = (char*)__shfl_sync(~0u, (uint64_t)out, lane & ~3 | e);
         float* part = p.part + ((int64_t)blockIdx.x * 2 + (w.starts ? 1 : 0)) * (kRows * HDP + 2 * kRows);
         for (int c = 0; c < HDP / 32; ++c) {
           float o[32];
@@ -761,18 +800,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             }
           }
           if (whole) {
-            if (valid) {
+            // Four lanes hand 16-byte pieces round so that each store of a warp
+            // writes 64 contiguous bytes of eight rows instead of 16 of 32.
+            uint4 v[4];
 #pragma unroll
-              for (int e = 0; e < 32; e += 8)
-                if (32 * c + e < p.dim) {
-                  uint4 v;
-                  v.x = pack2<F16>(o[e] * scale, o[e + 1] * scale);
-                  v.y = pack2<F16>(o[e + 2] * scale, o[e + 3] * scale);
-                  v.z = pack2<F16>(o[e + 4] * scale, o[e + 5] * scale);
-                  v.w = pack2<F16>(o[e + 6] * scale, o[e + 7] * scale);
-                  *(uint4*)(out + 2 * (32 * c + e)) = v;
-                }
+            for (int e = 0; e < 4; ++e) {
+              v[e].x = pack2<F16>(o[8 * e] * scale, o[8 * e + 1] * scale);
+              v[e].y = pack2<F16>(o[8 * e + 2] * scale, o[8 * e + 3] * scale);
+              v[e].z = pack2<F16>(o[8 * e + 4] * scale, o[8 * e + 5] * scale);
+              v[e].w = pack2<F16>(o[8 * e + 6] * scale, o[8 * e + 7] * scale);
             }
+            turn4(v, lane);
+            const int col = 32 * c + 8 * (lane & 3);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (col < p.dim && rows4[e]) *(uint4*)(rows4[e] + 2 * col) = v[e];
           } else {
             // [column / 4][row][4]: a warp's 32 rows are 512 contiguous bytes
 #pragma unroll
