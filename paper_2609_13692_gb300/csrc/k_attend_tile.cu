@@ -42,6 +42,7 @@ constexpr int kKeys = 128;     // keys of a tile
 constexpr int kRows = 256;     // rows of a slot of partial results
 constexpr int kThreads = 384;
 constexpr int kOddSets = 4;    // items whose notes are kept apart (warp 11 is at most two ahead of the rows)
+constexpr int kList = 32;      // items listed at a time
 constexpr int kHeldSets = 16;  // key tiles whose page marks are kept apart
 
 template <int HDP>
@@ -53,6 +54,12 @@ struct TileCfg {
   static constexpr int kSmem = 1024 + kQ + kSlots * kSlot + 2048;
 };
 
+// One entry of a block's list of items: the item, and the part of its key tiles
+// that is the block's.
+struct alignas(16) TileEntry {
+  int req, head, pair, q0, ql, kvl, t0, seg;
+};
+
 struct TileShared {
   unsigned long long full[8], empty[8], q_full, q_empty, s_full[2], p_ready[2], o_full[2], drain;
   uint32_t tmem;
@@ -60,6 +67,10 @@ struct TileShared {
   uint32_t held[kHeldSets];
   uint32_t odd[kOddSets][9];  // 8 words of keys from the item's first ambiguous one, and whether any is set
   int64_t scratch[40];
+  int64_t left;  // key tiles that the list has yet to take
+  int items, stride, item, column, t0;  // all items; of the line: its step, and where the list goes on
+  int count, more;
+  alignas(16) TileEntry list[kList];
 };
 static_assert(sizeof(TileShared) <= 2048);
 
@@ -91,6 +102,8 @@ __device__ __forceinline__ bool wait_on(unsigned long long* bar, uint32_t parity
 __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parity, int* gave_up) {
   return __all_sync(~0u, mbar_try_wait(bar, parity)) || wait_on(bar, parity, gave_up);
 }
+
+__device__ __forceinline__ void bar_all() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
 
 // The first lane's value in every lane, which the compiler then knows to be uniform.
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(~0u, v, 0); }
@@ -212,27 +225,6 @@ __device__ __forceinline__ uint32_t not_finite8(const uint4& x) {
   return (((x.x & e) + one) | ((x.y & e) + one) | ((x.z & e) + one) | ((x.w & e) + one)) & 0x80008000u;
 }
 
-// sum over k < n of floor((a + b k) / 128), a, b >= 0: after the whole parts are
-// taken out, the points under the line are counted by the other axis, as in
-// Euclid's algorithm.
-__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t b, uint32_t a) {
-  int64_t sum = 0;
-  uint32_t m = 128;
-  while (n > 0) {
-    sum += (int64_t)n * (n - 1) / 2 * (b / m) + (int64_t)n * (a / m);
-    b %= m;
-    a %= m;
-    const uint32_t y = b * n + a;  // b < 256, n < 2^24
-    if (y < m) break;
-    n = y / m;
-    a = y % m;
-    const uint32_t t = m;
-    m = b;
-    b = t;
-  }
-  return sum;
-}
-
 // Transposes the 4 x 4 pieces of every four lanes.
 __device__ __forceinline__ void swap_with(uint4& x, int lane_mask) {
   x.x = __shfl_xor_sync(~0u, x.x, lane_mask);
@@ -255,110 +247,134 @@ __device__ __forceinline__ void turn4(uint4* v, int lane) {
     }
 }
 
-// One request's items: its pairs of row tiles and their key tiles.
-struct TileReq {
-  AttnReq r;
-  int toks, pairs;  // tokens of a row tile; pairs of row tiles
-  __device__ __forceinline__ int cost(const AttnParams& p, int pair) const {
-    int lim = r.kvl;
-    if (p.causal) {
-      const int64_t tok = (int64_t)2 * toks * (pair + 1);
-      lim = r.kvl - r.ql + (tok < r.ql ? (int)tok : r.ql);  // > -2^31 + 1
-    }
-    return lim <= kKeys ? 1 : (lim - 1) / kKeys + 1;
+// Items in their natural order: the requests, the KV heads of each, the pairs of
+// row tiles of each.  Where the call's keys and values fit in L2 the blocks share
+// the line as it is.  Where they do not, every block would at any time be at
+// heads of its own, each read from memory for every pair: then the line takes
+// the items in columns, c, c + n, c + 2 n, .. of an n-block grid for c = 0, 1, ..,
+// and the blocks work on neighbouring items, mostly pairs of the same head.
+// (Natural order and columns: 28 requests of up to 700 tokens over 6,000 keys of
+// 24 heads, 380 MB: 541 and 488 us; 4,096 tokens over 20,480 keys of 8 heads,
+// 84 MB: 785 and 840 us, the blocks reading the same keys at the same time.)
+constexpr int64_t kNaturalBytes = 100ll << 20;  // of 126 MB of L2
+__device__ __forceinline__ int pairs_of(const AttnParams& p, int ql) {
+  return (int)(((int64_t)ql + 2 * p.toks - 1) / (2 * p.toks));
+}
+// Key tiles that the pair has to take, one at least (a row without keys is written too).
+__device__ __forceinline__ int pair_cost(const AttnParams& p, int ql, int kvl, int pair) {
+  int lim = kvl;
+  if (p.causal) {
+    const int64_t tok = (int64_t)2 * p.toks * (pair + 1);
+    lim = kvl - ql + (tok < ql ? (int)tok : ql);  // > -2^31 + 1
   }
-  // key tiles of the pairs before `pair` (pair <= pairs)
-  __device__ int64_t before(const AttnParams& p, int pair) const {
-    if (!p.causal || pair == 0) return (int64_t)pair * cost(p, 0);
-    const int last = pair == pairs ? cost(p, pairs - 1) : 0;
-    const int n = pair == pairs ? pair - 1 : pair;
-    // cost(q) = max(1, floor((a + b q) / 128))
-    const int b = 2 * toks;
-    const int64_t a = (int64_t)r.kvl - r.ql + b + 127;
-    int64_t one = a >= 128 ? 0 : (128 - a + b - 1) / b;
-    if (one > n) one = n;
-    return one + floor_sum((uint32_t)(n - one), (uint32_t)b, n > one ? (uint32_t)(a + b * one) : 0u) + last;
-  }
-};
-
-__device__ __forceinline__ TileReq tile_req(const AttnParams& p, int i) {
-  TileReq t;
-  t.r = attn_req(p, i);
-  t.toks = 128 / p.group;
-  t.pairs = (int)(((int64_t)t.r.ql + 2 * t.toks - 1) / (2 * t.toks));
-  return t;
+  return lim <= kKeys ? 1 : (lim - 1) / kKeys + 1;
 }
 
-// A walk over the block's items; every role makes it on its own.
-struct TileWalk {
-  int req, head, pair, t0, cost, seg;
-  int64_t left;
-  TileReq x;
+// What a role needs of an entry.
+struct TileItem {
+  TileEntry e;
   int tok0, n0, n1, tiles;  // first token; key tiles of each row tile from t0; their maximum
-  int lim_first;          // what the item's first row sees
-  bool starts, ends;
-
-  // By whole warps.
-  __device__ __forceinline__ void begin(const AttnParams& p, const AttnRange& range) {
-    req = range.req;
-    left = range.end - range.begin;
-    x = tile_req(p, req);
-    const int64_t per_head = x.before(p, x.pairs);
-    head = (int)(range.off / per_head);
-    const int64_t rest = range.off % per_head;
-    int lo = 0, hi = x.pairs - 1;  // the last pair that begins at or before rest
-    const int lane = threadIdx.x & 31;
-    while (lo < hi) {
-      const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
-      const int k = __popc(__ballot_sync(~0u, at <= hi && x.before(p, at) <= rest));
-      lo += k * step;
-      hi = min(hi, lo + step - 1);
-    }
-    pair = lo;
-    t0 = (int)(rest - x.before(p, pair));
-    enter(p);
-  }
-  __device__ __forceinline__ void enter(const AttnParams& p) {
-    cost = x.cost(p, pair);
-    seg = (int)(left < cost - t0 ? left : cost - t0);
-    starts = t0 == 0;
-    ends = t0 + seg == cost;
-    tok0 = pair * 2 * x.toks;
-    lim_first = attn_limit(p, x.r, tok0);
+  int lim_first;            // what the item's first row sees
+  __device__ __forceinline__ void load(const AttnParams& p, const TileEntry* at) {
+    const int4 a = ((const int4*)at)[0], b = ((const int4*)at)[1];
+    e = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    tok0 = e.pair * 2 * p.toks;
+    lim_first = limit(p, tok0);
     n0 = key_count(p, tok0);
-    n1 = key_count(p, (int64_t)tok0 + x.toks);
+    n1 = key_count(p, (int64_t)tok0 + p.toks);
     tiles = n0 > n1 ? n0 : n1;
   }
+  __device__ __forceinline__ int limit(const AttnParams& p, int t) const { return attn_limit(p, {e.q0, e.ql, e.kvl}, t); }
   // Key tiles from t0 on that some row of the tile beginning at token `first` sees.
   __device__ __forceinline__ int key_count(const AttnParams& p, int64_t first) const {
-    if (first >= x.r.ql) return 0;
-    const int end = (int)(first + x.toks < x.r.ql ? first + x.toks : x.r.ql);
-    const int lim = attn_limit(p, x.r, end - 1), need = lim == 0 ? 0 : (lim - 1) / kKeys + 1;
-    const int stop = t0 + seg < need ? t0 + seg : need;
-    return stop > t0 ? stop - t0 : 0;
+    if (first >= e.ql) return 0;
+    const int end = (int)(first + p.toks < e.ql ? first + p.toks : e.ql);
+    const int lim = limit(p, end - 1), need = lim == 0 ? 0 : (lim - 1) / kKeys + 1;
+    const int stop = e.t0 + e.seg < need ? e.t0 + e.seg : need;
+    return stop > e.t0 ? stop - e.t0 : 0;
   }
   __device__ __forceinline__ int count(int s) const { return s ? n1 : n0; }
-  // False after the last item.
-  __device__ __forceinline__ bool next(const AttnParams& p) {
-    left -= seg;
-    if (left <= 0) return false;
-    t0 = 0;
-    if (++pair == x.pairs) {
-      pair = 0;
-      if (++head == p.kv_heads) {
-        head = 0;
-        do {
-          if (++req >= p.batch) return false;
-          x = tile_req(p, req);
-        } while (x.pairs == 0);
-      }
-    }
-    enter(p);
-    return true;
-  }
   // Whether some row of the item does not see every key of tile t0 + j.
-  __device__ __forceinline__ bool partly(int j) const { return (int64_t)(t0 + j + 1) * kKeys > lim_first; }
+  __device__ __forceinline__ bool partly(int j) const { return (int64_t)(e.t0 + j + 1) * kKeys > lim_first; }
 };
+
+// By one warp: the next entries of the block's list, from `item` on (its first
+// t0 key tiles are another block's), `left` key tiles in all.  Lane k finds the
+// k-th item; the requests are gone through 32 at a time.
+__device__ void fill_list(const AttnParams& p, TileShared& sh) {
+  const int lane = threadIdx.x & 31, n = sh.stride;
+  const int items = sh.items;
+  int item = sh.item, column = sh.column;
+  for (int j = lane; item < items;) {  // j items on, through the ends of columns
+    const int rest = (items - item - 1) / n + 1;
+    if (j < rest) {
+      item += j * n;
+      break;
+    }
+    j -= rest;
+    item = ++column < n ? column : items;
+  }
+  TileEntry e{};
+  int cost = 0;
+  int start = 0;
+  bool found = false;
+  for (int base = 0; base < p.batch && __any_sync(~0u, !found && item < items); base += 32) {
+    AttnReq r{0, 0, 0};
+    if (base + lane < p.batch) r = attn_req(p, base + lane);
+    const int pairs = pairs_of(p, r.ql);
+    int inc = pairs * p.kv_heads;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(~0u, inc, d);
+      if (lane >= d) inc += v;
+    }
+    const int end = start + inc, total = __shfl_sync(~0u, end, 31);
+    const bool here = !found && item < items && item < total;
+    // the request: how many of these 32 end at or before the item
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) at += __shfl_sync(~0u, end, i) <= item;
+    const int from = at < 32 ? at : 31;
+    const int before = __shfl_sync(~0u, end - pairs * p.kv_heads, from);
+    const int q0 = __shfl_sync(~0u, r.q0, from), ql = __shfl_sync(~0u, r.ql, from), kvl = __shfl_sync(~0u, r.kvl, from);
+    const int np = __shfl_sync(~0u, pairs, from);
+    if (here) {
+      const int local = item - before;
+      e.req = base + from;
+      e.head = local / np;
+      e.pair = local % np;
+      e.q0 = q0, e.ql = ql, e.kvl = kvl;
+      cost = pair_cost(p, ql, kvl, e.pair);
+      found = true;
+    }
+    start = total;
+  }
+  if (lane == 0) e.t0 = sh.t0;
+  const int mine = found ? cost - e.t0 : 0;
+  int64_t inc = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t v = __shfl_up_sync(~0u, inc, d);
+    if (lane >= d) inc += v;
+  }
+  const int64_t left = sh.left, open = left - (inc - mine);
+  e.seg = (int)(open < 0 ? 0 : open < mine ? open : mine);
+  const int n_used = __popc(__ballot_sync(~0u, e.seg > 0));  // a run from lane 0
+  __syncwarp();
+  if (e.seg > 0) sh.list[lane] = e;
+  const int last = n_used > 0 ? n_used - 1 : 0;
+  if (lane == last) {
+    const int64_t taken = inc - mine + e.seg;
+    sh.count = n_used;
+    sh.left = left - taken;
+    sh.more = n_used == kList && left > taken;
+    // after a full list whose last item is whole: the one that follows it in its column
+    sh.t0 = 0;
+    sh.item = item + n < items ? item + n : column + 1;
+    sh.column = item + n < items ? column : column + 1;
+  }
+  __syncwarp();
+}
 
 template <int HDP, bool F16>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_constant__ AttnParams p) {
@@ -387,12 +403,98 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     mbar_init_fence();
   }
   launch_dependents();
-  const AttnRange range = attn_range<kThreads>(p.batch, blockIdx.x, gridDim.x, sh.scratch, [&](int i) -> int64_t {
-    const TileReq t = tile_req(p, i);
-    return t.pairs == 0 ? 0 : p.kv_heads * t.before(p, t.pairs);
+  // The requests, in the room of the ring: first item, new tokens, keys, pairs.
+  int4* const reqs = (int4*)ring;
+  {
+    const int per = (p.batch + kThreads - 1) / kThreads, lo = min(tid * per, p.batch), hi = min(lo + per, p.batch);
+    int64_t sum = 0, keys = 0;  // items (fewer than 2^31: q would not fit in memory) and keys
+    for (int i = lo; i < hi; ++i) {
+      const AttnReq r = attn_req(p, i);
+      const int pairs = pairs_of(p, r.ql);
+      reqs[i] = make_int4((int)sum, r.ql, r.kvl, pairs);
+      sum += (int64_t)pairs * p.kv_heads;
+      keys += pairs > 0 ? r.kvl : 0;
+    }
+    int64_t inc = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t v = __shfl_up_sync(~0u, inc, d);
+      if (lane >= d) inc += v;
+      keys += __shfl_xor_sync(~0u, keys, d);
+    }
+    if (lane == 31) {
+      sh.scratch[warp] = inc;
+      sh.scratch[16 + warp] = keys;
+    }
+    __syncthreads();
+    int64_t before = inc - sum, all = 0;
+    keys = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += sh.scratch[w];
+      all += sh.scratch[w];
+      keys += sh.scratch[16 + w];
+    }
+    for (int i = lo; i < hi; ++i) reqs[i].x += (int)before;
+    if (tid == 0) {
+      sh.items = (int)all;
+      sh.stride = keys * p.kv_heads * p.dim * 4 > kNaturalBytes ? (int)gridDim.x : 1;
+    }
+    __syncthreads();
+  }
+  const int items = sh.items, stride = sh.stride;
+  // column c begins at item c, or in natural order at the c-th of equal runs
+  const int run = (items + (int)gridDim.x - 1) / (int)gridDim.x;
+  int at_req = 0;  // request of the thread's last item (they mostly come in rising order)
+  auto cost_of = [&](int item) -> int {
+    int hi = p.batch - 1;
+    if (reqs[at_req].x > item) at_req = 0;
+    while (at_req < hi) {
+      const int mid = (at_req + hi + 1) / 2;
+      if (reqs[mid].x <= item) at_req = mid;
+      else hi = mid - 1;
+    }
+    const int4 r = reqs[at_req];
+    return pair_cost(p, r.y, r.z, (item - r.x) % r.w);
+  };
+  const AttnRange range = attn_range<kThreads>((int)gridDim.x, blockIdx.x, gridDim.x, sh.scratch, [&](int c) -> int64_t {
+    int64_t sum = 0;
+    const int64_t end = stride > 1 ? items : min((int64_t)items, (int64_t)(c + 1) * run);
+    for (int64_t i = stride > 1 ? c : (int64_t)c * run; i < end; i += stride) sum += cost_of((int)i);
+    return sum;
   });
   if (tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (range.begin >= range.end) return;
+  if (warp == 11) {  // the block's first item, in column range.req
+    int64_t item = stride > 1 ? range.req : (int64_t)range.req * run, rest = range.off;
+    for (;;) {
+      const int64_t mine = item + (int64_t)lane * stride;
+      const int cost = mine < items ? cost_of((int)mine) : 0;
+      int64_t inc = cost;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t v = __shfl_up_sync(~0u, inc, d);
+        if (lane >= d) inc += v;
+      }
+      const unsigned past = __ballot_sync(~0u, inc > rest);
+      if (past) {
+        const int k = __ffs(past) - 1;
+        rest -= __shfl_sync(~0u, inc - cost, k);
+        item += (int64_t)k * stride;
+        break;
+      }
+      rest -= __shfl_sync(~0u, inc, 31);
+      item += (int64_t)32 * stride;
+    }
+    if (lane == 0) {
+      sh.item = (int)item;
+      sh.column = stride > 1 ? range.req : 0;
+      sh.t0 = (int)rest;
+      sh.left = range.end - range.begin;
+    }
+    __syncwarp();
+    fill_list(p, sh);
+  }
+  __syncthreads();  // the requests are done with: the ring is free
 
   // rows that no copy fills (whole tokens only in a tile) stay 0
   for (int e = tid; e < C::kQ / 16; e += kThreads) ((uint4*)qbuf)[e] = make_uint4(0, 0, 0, 0);
@@ -406,6 +508,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   fence_after();
   const uint32_t tmem = sh.tmem;  // S0/P0 at 0, S1/P1 at 128, O0 at 256, O1 at 384
   int* const gave_up = &sh.gave_up;
+  // The next entry of the list; at its end, where the block has more items, all
+  // roles meet and warp 11 writes the next ones.
+  auto next_item = [&](int& k) -> bool {
+    if (++k < sh.count) return true;
+    if (!sh.more) return false;
+    bar_all();
+    if (warp == 11) fill_list(p, sh);
+    bar_all();
+    k = 0;
+    return true;
+  };
+  // A role that has given up still meets the others.
+  auto leave = [&] {
+    while (sh.more) {
+      bar_all();
+      if (warp == 11) fill_list(p, sh);
+      bar_all();
+    }
+  };
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // 2 x 216 + 72 = 3 x 168
@@ -415,20 +536,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       // ring and its values in use 2 g + 1.  A warp waits for every second use's
       // slot only; the products release the uses in order, so a use that has
       // been released implies all before it, and no wait is a phase early.
-      TileWalk w;
-      w.begin(p, range);
+      TileItem w;
+      int k = 0;
       const int v = warp - 9, box = p.box, per = kKeys / box;
       const CUtensorMap* const map = v ? &p.map_v : &p.map_k;
       uint32_t item = 0, gt = 0;
       bool ok = true;
       do {
+        w.load(p, &sh.list[k]);
         if (w.tiles == 0) continue;
-        const int head = (int)uniform((uint32_t)w.head), t0 = (int)uniform((uint32_t)w.t0), tiles = (int)uniform((uint32_t)w.tiles);
+        const int head = (int)uniform((uint32_t)w.e.head), t0 = (int)uniform((uint32_t)w.e.t0), tiles = (int)uniform((uint32_t)w.tiles);
         if (v == 0) {
           if (item > 0) ok = ok && wait_all(&sh.q_empty, (item - 1) & 1, gave_up);
           if (!ok) break;
           const int rows = w.n1 > 0 ? 2 : 1;  // the second row tile sees at least what the first does
-          const int tok = (int)uniform((uint32_t)(w.x.r.q0 + w.tok0)), toks = w.x.toks;
+          const int tok = (int)uniform((uint32_t)(w.e.q0 + w.tok0)), toks = p.toks;
           if (lane == 0) mbar_arrive_expect_tx(&sh.q_full, rows * toks * p.group * 128 * C::kBlk);
           __syncwarp();
           if (elect_one())
@@ -439,8 +561,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           __syncwarp();
           ++item;
         }
-        const int32_t* row = p.table + (int64_t)w.req * p.table_stride;
-        const int kvl = w.x.r.kvl;
+        const int32_t* row = p.table + (int64_t)w.e.req * p.table_stride;
+        const int kvl = w.e.kvl;
         auto page_of = [&](int j) -> int {  // lane b: page of the tile's b-th box
           const int64_t key = (int64_t)(t0 + j) * kKeys + lane * box;
           if (j >= tiles || lane >= per || key >= kvl) return -1;
@@ -477,21 +599,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           }
           __syncwarp();
         }
-      } while (ok && uniform(w.next(p)));
+      } while (ok && uniform(next_item(k)));
       if (!ok) {  // copies in flight land before the block ends
         for (uint32_t k = gt > C::kSlots ? gt - C::kSlots : 0; k < gt; ++k) {
           const uint32_t idx = 2 * k + v;
           for (int i = 0; i < 1 << 16 && !mbar_try_wait(&sh.full[idx % C::kSlots], (idx / C::kSlots) & 1); ++i) {
           }
         }
+        leave();
       }
     } else if (warp == 8) {
       // ---- products ----
       // The whole warp takes every step and one lane issues, with operands that
       // the compiler knows to be the same in all lanes (the broadcasts): issued
       // from a branch of one lane, each product cost about 100 cycles.
-      TileWalk w;
-      w.begin(p, range);
+      TileItem w;
+      int k = 0;
       constexpr uint32_t acc = 0;  // all 512 columns are this block's: they begin at 0
       const int steps = (p.dim + 15) / 16;  // of 16 elements of a head; columns of O likewise
       const uint32_t kind = 1u << 4 | (F16 ? 0u : 1u << 7 | 1u << 10) | 8u << 24;  // 32-bit sums, 128 rows
@@ -519,6 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       int sk = 0;          // slot of the next key tile; its values follow
       uint32_t phase = 0;  // of the ring at that slot
       do {
+        w.load(p, &sh.list[k]);
         const int tiles = (int)uniform((uint32_t)w.tiles), n0 = (int)uniform((uint32_t)w.n0), n1 = (int)uniform((uint32_t)w.n1);
         if (tiles == 0) continue;
         ok = wait_all(&sh.q_full, item & 1, gave_up) && wait_all(&sh.full[sk], phase, gave_up);
@@ -575,20 +699,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             __syncwarp();
           }
         }
-      } while (ok && uniform(w.next(p)));
+      } while (ok && uniform(next_item(k)));
       // nothing in flight when the tensor memory goes
       if (elect_one()) commit(&sh.drain);
       __syncwarp();
       for (int i = 0; i < 1 << 20 && !mbar_try_wait(&sh.drain, 0); ++i) {
       }
       __syncwarp();
+      if (!ok) leave();
     } else {
       // ---- copies that have landed, and values that some row must not see ----
-      TileWalk w;
-      w.begin(p, range);
+      TileItem w;
+      int k = 0;
       uint32_t idx = 0, item = 0, ready = 0, due = 0;  // idx: ring use of tile j's keys; due: row tiles with a phase to end
       bool ok = true;
       do {
+        w.load(p, &sh.list[k]);
         if (w.tiles == 0) continue;
         uint32_t* odd = sh.odd[item % kOddSets];
         ++item;
@@ -601,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           if (!ok) break;
           if (w.partly(j)) {
             const uint32_t at = smem_u32(ring + s * C::kSlot);
-            const int key0 = (w.t0 + j) * kKeys;
+            const int key0 = (w.e.t0 + j) * kKeys;
             const int from = w.lim_first > key0 ? w.lim_first - key0 : 0;
             bool wrote = false;
             // lane i looks at the i-th 16 bytes of two rows (four where a head has 64 elements)
@@ -629,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
                 wrote = true;
                 if (lane < kChunks) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(mine + row * 128), "r"(0) : "memory");
                 const int key = key0 + row, a = key - w.lim_first;  // a < 256 for every token of the item
-                if (lane == 0 && key < w.x.r.kvl && a < 256) {
+                if (lane == 0 && key < w.e.kvl && a < 256) {
                   odd[a >> 5] |= 1u << (a & 31);
                   odd[8] = 1;
                 }
@@ -652,23 +778,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           }
           __syncwarp();
         }
-      } while (ok && uniform(w.next(p)));
+      } while (ok && uniform(next_item(k)));
+      if (!ok) leave();
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---- one row per thread ----
-    TileWalk w;
-    w.begin(p, range);
+    TileItem w;
+    int k = 0;
     const int s = warp >> 2, r = tid & 127, r_tok = r / p.group, sub = r % p.group;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + s * 128 + lanes, t_o = tmem + 256 + s * 128 + lanes;
     uint32_t scored = 0, done = 0, item = 0, gt = 0;
     bool ok = true;
     do {
-      const int64_t first_tok = (int64_t)w.tok0 + s * w.x.toks;
-      const bool valid = r_tok < w.x.toks && first_tok + r_tok < w.x.r.ql;
+      w.load(p, &sh.list[k]);
+      const int64_t first_tok = (int64_t)w.tok0 + s * p.toks;
+      const bool valid = r_tok < p.toks && first_tok + r_tok < w.e.ql;
       const int tok = valid ? (int)first_tok + r_tok : 0;
-      const int lim = valid ? attn_limit(p, w.x.r, tok) : INT32_MAX;
-      const int lim_tile = first_tok < w.x.r.ql ? attn_limit(p, w.x.r, (int)first_tok) : 0;  // what every row of the tile sees
+      const int lim = valid ? w.limit(p, tok) : INT32_MAX;
+      const int lim_tile = first_tok < w.e.ql ? w.limit(p, (int)first_tok) : 0;  // what every row of the tile sees
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < w.count(s); ++j) {
         ok = wait_all(&sh.s_full[s], scored & 1, gave_up);
@@ -680,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         for (int c = 0; c < 4; ++c) tmem_ld32(f + 32 * c, t_s + 32 * c);
         wait_ld();
         const uint32_t held = sh.held[(gt + j) % kHeldSets];
-        const int key0 = (w.t0 + j) * kKeys;
+        const int key0 = (w.e.t0 + j) * kKeys;
         if (key0 + kKeys > lim_tile || held != 0xFFFFu) {
           const int sees = lim - key0;
 #pragma unroll
@@ -754,16 +882,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         fence_after();
       }
       // ---- out ----
-      const bool whole = w.starts && w.ends;
-      if (first_tok < w.x.r.ql) {
+      const int cost = pair_cost(p, w.e.ql, w.e.kvl, w.e.pair);
+      const bool starts = w.e.t0 == 0, ends = w.e.t0 + w.e.seg == cost, whole = starts && ends;
+      if (first_tok < w.e.ql) {
         const bool extra = odd && w.count(s) > 0 && odd[8];
         const float inv = l == 0.f ? 0.f : 1.f / l, scale = whole ? inv : 1.f;
-        const int64_t tok_at = (int64_t)w.x.r.q0 + tok, head = (int64_t)w.head * p.group + sub;
+        const int64_t tok_at = (int64_t)w.e.q0 + tok, head = (int64_t)w.e.head * p.group + sub;
         char* const out = valid ? p.out + 2 * (tok_at * p.out_tok + head * p.out_head) : nullptr;
         char* rows4[4];  // of the four lanes of a group
 #pragma unroll
         for (int e = 0; e < 4; ++e) rows4[e] = (char*)__shfl_sync(~0u, (uint64_t)out, lane & ~3 | e);
-        float* part = p.part + ((int64_t)blockIdx.x * 2 + (w.starts ? 1 : 0)) * (kRows * HDP + 2 * kRows);
+        float* part = p.part + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * (kRows * HDP + 2 * kRows);
         for (int c = 0; c < HDP / 32; ++c) {
           float o[32];
           if (w.count(s) > 0) {
@@ -779,11 +908,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             for (int a = 0; a < 256; ++a) {
               const int key = w.lim_first + a;
               if (!(odd[a >> 5] >> (a & 31) & 1u) || key >= lim) continue;
-              const int64_t id = p.table[(int64_t)w.req * p.table_stride + (key >> p.page_log2)];
+              const int64_t id = p.table[(int64_t)w.e.req * p.table_stride + (key >> p.page_log2)];
               if (id < 0 || id >= p.n_pages) continue;
               const int64_t slot = key & ((1 << p.page_log2) - 1);
-              const char* kp = p.k + 2 * (id * p.k_page + slot * p.k_slot + w.head * p.k_head);
-              const char* vp = p.v + 2 * (id * p.v_page + slot * p.v_slot + w.head * p.v_head);
+              const char* kp = p.k + 2 * (id * p.k_page + slot * p.k_slot + w.e.head * p.k_head);
+              const char* vp = p.v + 2 * (id * p.v_page + slot * p.v_slot + w.e.head * p.v_head);
               float dot = 0.f;
               for (int d = 0; d < p.dim; d += 2) {
                 const float2 a2 = unpack2<F16>(*(const uint32_t*)(q + 2 * d)), b2 = unpack2<F16>(*(const uint32_t*)(kp + 2 * d));
@@ -829,12 +958,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           part[kRows * HDP + kRows + s * 128 + r] = l;
         }
       }
-      if (w.starts && !w.ends && tid == 0) {
-        const int64_t first = range.end - w.seg;  // the item's first unit
-        p.desc[blockIdx.x] = make_int4(w.req, w.head, w.pair, attn_block_of(range, first + w.cost - 1) - (int)blockIdx.x + 1);
+      if (starts && !ends && tid == 0) {
+        const int64_t first = range.end - w.e.seg;  // the item's first unit
+        p.desc[blockIdx.x] = make_int4(w.e.req, w.e.head, w.e.pair, attn_block_of(range, first + cost - 1) - (int)blockIdx.x + 1);
       }
       fence_before();  // O is read before the next item's first product may write it
-    } while (w.next(p));
+    } while (next_item(k));
+    if (!ok) leave();
   }
 
   __syncthreads();
@@ -849,10 +979,10 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
   const int4 d = p.desc[blockIdx.x];
   if (d.w == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const TileReq x = tile_req(p, d.x);
-  const int slot_row = blockIdx.y * 32 + lane, s = slot_row >> 7, r = slot_row & 127;
-  const int64_t row_tok = ((int64_t)d.z * 2 + s) * x.toks + r / p.group;
-  if (r >= x.toks * p.group || row_tok >= x.r.ql) return;
+  const AttnReq r = attn_req(p, d.x);
+  const int slot_row = blockIdx.y * 32 + lane, s = slot_row >> 7, row = slot_row & 127;
+  const int64_t row_tok = ((int64_t)d.z * 2 + s) * p.toks + row / p.group;
+  if (row >= p.toks * p.group || row_tok >= r.ql) return;
   constexpr int64_t kSlot = kRows * HDP + 2 * kRows;
   constexpr int kCols = HDP / 8;
   const float* first = p.part + ((int64_t)blockIdx.x * 2 + 1) * kSlot;
@@ -878,7 +1008,7 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int64_t tok = x.r.q0 + row_tok, head = (int64_t)d.y * p.group + r % p.group;
+  const int64_t tok = r.q0 + row_tok, head = (int64_t)d.y * p.group + row % p.group;
 #pragma unroll
   for (int c = 0; c < kCols; c += 8) {
     const int col = warp * kCols + c;

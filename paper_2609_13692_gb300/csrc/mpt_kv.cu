@@ -141,6 +141,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   p.kv_heads = c->kv_heads;
   p.group = heads / c->kv_heads;
   p.dim = c->head_dim;
+  p.toks = 128 / p.group;
   p.causal = causal != 0;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t stream = (cudaStream_t)stream_ptr;
@@ -151,7 +152,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   // Few rows per KV head: 16 of them fill the smaller kernel's products.  Where
   // the caller does not say, as many tokens as requests are taken for one each.
   const int64_t most = max_q_len > 0 ? max_q_len : tokens <= c->batch ? 1 : 129;
-  const bool tile = c->head_dim <= 128 && most * p.group > 16;
+  const bool tile = c->head_dim <= 128 && most * p.group > 16 && c->batch <= mpt::kTileBatch;
   const int keys = tile ? 128 : 64;
   p.box = c->page_size < keys ? c->page_size : keys;
   if (!mpt::make_map(&p.map_k, *c, c->k, c->k_stride, p.box) || !mpt::make_map(&p.map_v, *c, c->v, c->v_stride, p.box) ||

@@ -198,6 +198,17 @@ def test_many_requests(kv):
     check(kv, make(14, q_lens, [n + 5 for n in q_lens], 4, 2, 128, 8, F16, poison=True))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_more_items_than_a_block_lists(kv, dim):
+    """Thousands of small items, whole and cut, in both kernels."""
+    rng = random.Random(6)
+    q_lens = [rng.choice([0, 1, 2, 5, 70]) for _ in range(900)]
+    kv_lens = [n + rng.choice([0, 1, 30, 200]) for n in q_lens]
+    c = make(22, q_lens, kv_lens, 8, 8, dim, 8, BF16, poison=True)
+    check(kv, c, hint=70)
+    check(kv, c, hint=1)
+
+
 @pytest.mark.parametrize("q_len,heads", [(1, 8), (1, 64), (33, 8), (300, 2)])
 def test_long_keys(kv, q_len, heads):
     """Few rows over many keys: the keys are cut across all blocks and joined."""
