@@ -809,11 +809,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         wait_ld();
         const uint32_t held = sh.held[(gt + j) % kHeldSets];
         const int key0 = (w.e.t0 + j) * kKeys;
-        if (key0 + kKeys > lim_tile || held != 0xFFFFu) {
+        if (held != 0xFFFFu) {  // pages that the cache does not hold, 8 keys at a time
+#pragma unroll
+          for (int g = 0; g < 16; ++g)
+            if (!(held >> g & 1u)) {
+#pragma unroll
+              for (int c = 8 * g; c < 8 * g + 8; ++c) f[c] = -INFINITY;
+            }
+        }
+        if (key0 + kKeys > lim_tile) {
           const int sees = lim - key0;
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (c >= sees || !(held >> (c >> 3) & 1u)) f[c] = -INFINITY;
+          for (int c = 0; c < 128; ++c) f[c] = c < sees ? f[c] : -INFINITY;
         }
         float mx[4];
 #pragma unroll
