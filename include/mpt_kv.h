@@ -80,7 +80,8 @@ mpt_status mpt_kv_attend_workspace_bytes(int32_t head_dim, size_t* bytes);
  *   q, out: device, `type`, [tokens][heads][head_dim] with element strides
  *     q_stride[2] / out_stride[2] between tokens and heads (multiples of 8);
  *     16-byte aligned; out must not overlap q or the cache;
- *   heads: a multiple of kv_heads, heads / kv_heads <= 128;
+ *   heads: a multiple of kv_heads, heads / kv_heads <= 128, tokens times that
+ *     < 2^31;
  *   lse: device float[tokens][heads], or NULL;
  *   max_q_len: the most new tokens of one request if the caller knows it, else
  *     0.  It only chooses the kernel; any value gives the same function.

@@ -11,8 +11,8 @@
 // Bound: the cache is read once, 2 L Hkv d elements, for 4 d operations per
 // element and query head of the group: with up to 16 rows that is below what
 // the memory allows a tensor core to do, so the kernel is built around the
-// copy.  One warp issues tensor-map copies of pages into a ring of stages (64
-// keys of K and V each); the others take 16 keys of a stage apiece through
+// copy.  Four warps issue tensor-map copies of pages into a ring of stages (64
+// keys of K and V each); eight others take 16 keys of a stage apiece through
 // ldmatrix and m16n8k16 products with 32-bit accumulators, without a barrier
 // among them until the item's end.
 #include <cuda_bf16.h>
@@ -32,13 +32,16 @@ template <int HDP>
 struct FewCfg {
   static constexpr int kWarps = HDP == 256 ? 4 : 8;  // 256: 128 accumulators a thread
   static constexpr int kGroups = kWarps / 4;         // groups of four warps take stages in turn
-  static constexpr int kThreads = 32 * (kWarps + 1);
+  // One warp issues a copy every 95 cycles or so: with pages of 16 (2 KB each)
+  // that is 21 bytes a cycle, less than an SM's share of the memory.
+  static constexpr int kCopyWarps = HDP == 256 ? 2 : 4;
+  static constexpr int kThreads = 32 * (kWarps + kCopyWarps);
   static constexpr int kStage = 2 * kKeys * HDP * 2;
   // A stage always belongs to one group: a group that waits for a stage's next
   // phase has then itself seen the phase before complete.  Copies may land out
   // of order, and a wait one phase ahead would pass at once.
-  static constexpr int kStages = HDP == 64 ? 10 : HDP == 128 ? 4 : 2;
-  static_assert(kStages % kGroups == 0);
+  static constexpr int kStages = HDP == 64 ? 12 : HDP == 128 ? 4 : 2;
+  static_assert(kStages % kGroups == 0 && kStages % kCopyWarps == 0);
   static constexpr int kBufs = kWarps / 2;
   static constexpr int kPad = HDP + 8;               // row of a joining buffer, in floats
   static constexpr int kBuf = kBufs * kRows * kPad * 4;
@@ -136,7 +139,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
   unsigned long long* empty = full + C::kStages;
   uint32_t* there = (uint32_t*)(empty + C::kStages);  // per stage: which groups of 8 keys the cache holds
   int64_t* scratch = (int64_t*)((char*)ml + 1024 + 512);
-  __shared__ volatile int gave_up;
+  __shared__ int gave_up;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
@@ -146,6 +149,10 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
     }
     gave_up = 0;
     mbar_init_fence();
+  }
+  if (tid == 32) {  // the maps are read a good while before the first copy
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_k));
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_v));
   }
   launch_dependents();
   const AttnRange range = attn_range<C::kThreads>(p.batch, blockIdx.x, gridDim.x, scratch, [&](int i) -> int64_t {
@@ -162,14 +169,16 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
   int64_t item = range.off / cost;
   int t0 = (int)(range.off % cost);
   int64_t left = range.end - range.begin;
-  uint32_t it = 0;  // stages used so far
+  uint32_t it = 0;  // stages used so far (the products' count)
 
-  if (warp == C::kWarps) {
-    // ---- copies ----
+  if (warp >= C::kWarps) {
+    // ---- copies: the warps take stages in turn ----
+    const uint32_t me = warp - C::kWarps;
     const int per = kKeys >> p.page_log2 > 0 ? kKeys >> p.page_log2 : 1;  // boxes of a stage along the keys
     const int box = p.box;                                                // keys of one
     constexpr int kBlk = HDP / 64;
     bool ok = true;
+    uint32_t it0 = 0, done = 0;  // stages before the item; this warp's last use and one
     while (left > 0 && ok) {
       const FewItem x = few_item(p, r, req, item, rt);
       const int seg = (int)(left < cost - t0 ? left : cost - t0);
@@ -182,12 +191,15 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
         return id < 0 || id >= p.n_pages ? -1 : id;
       };
       const int mine = lane % per;  // per is a power of two of at most 8
-      int next = page_of(t0, mine);
-      for (int t = t0; t < last; ++t, ++it) {
+      // this warp's next tile, and its pages ahead of need
+      int t = t0 + (int)((me - it0) % C::kCopyWarps);
+      int next = page_of(t, mine);
+      for (; t < last; t += C::kCopyWarps) {
+        const uint32_t it = it0 + (uint32_t)(t - t0);
         const int s = it % C::kStages;
         const int id = next;
-        next = page_of(t + 1, mine);
-        if (it >= C::kStages && !mbar_wait(&empty[s], (it / C::kStages - 1) & 1)) {
+        next = page_of(t + C::kCopyWarps, mine);
+        if (it >= C::kStages && !wait_bar(&empty[s], (it / C::kStages - 1) & 1, &gave_up, &g_few_flags)) {
           ok = false;
           break;
         }
@@ -206,7 +218,10 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
           tma_load_4d(dst + v * (C::kStage / 2) + b * kKeys * 128 + mine * box * 128, v ? &p.map_v : &p.map_k, b * 64,
                       slot, x.head, id, &full[s]);
         }
+        done = it + 1;
       }
+      if (!ok) break;
+      if (last > t0) it0 += last - t0;
       left -= seg;
       t0 = 0;
       if (++item == (int64_t)p.kv_heads * rt) {
@@ -220,12 +235,11 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
         if (req >= p.batch) break;
       }
     }
-    if (!ok || gave_up) {
+    if (!ok) {
       // let the copies in flight land before the block ends
-      for (uint32_t k = it > C::kStages ? it - C::kStages : 0; k < it; ++k)
-        mbar_wait(&full[k % C::kStages], (k / C::kStages) & 1);
-      if (lane == 0) atomicOr(&g_few_flags, kErrTimeout);
-      gave_up = 1;
+      for (uint32_t k = done > C::kStages ? done - C::kStages : 0; k < done; ++k)
+        for (int i = 0; k % C::kCopyWarps == me && i < 1 << 16 && !mbar_try_wait(&full[k % C::kStages], (k / C::kStages) & 1); ++i) {
+        }
     }
     return;
   }
@@ -285,10 +299,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
     for (int t = t0; t < last; ++t, ++it) {
       if ((int)(it % C::kGroups) != group) continue;
       const int s = it % C::kStages;
-      if (!gave_up && !mbar_wait(&full[s], (it / C::kStages) & 1)) {
-        gave_up = 1;
-        atomicOr(&g_few_flags, kErrTimeout);
-      }
+      wait_bar(&full[s], (it / C::kStages) & 1, &gave_up, &g_few_flags);  // having given up, the block still ends in order
       const uint32_t kbase = smem_u32(ring + s * C::kStage), vbase = kbase + C::kStage / 2;
 
       // S = Q K^T for 16 keys
@@ -499,8 +510,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
     }
     if (starts && !ends && tid == 0) {
       const int64_t first = range.end - seg;  // the item's first unit
-      p.desc[blockIdx.x] = make_int4(req, (int)(item % 0x40000000), (int)(item / 0x40000000),
-                                     attn_block_of(range, first + cost - 1) - (int)blockIdx.x + 1);
+      p.desc[blockIdx.x] = make_int4(r.q0, x.row0, x.head | x.rows << 16, attn_block_of(range, first + cost - 1) - (int)blockIdx.x + 1);
     }
     bar_consumers(C::kWarps * 32);
 
@@ -519,64 +529,54 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
   }
 }
 
-// Joins the parts of the item that block c began and did not end: one block
-// per (c, row), the parts spread over its threads.
+// Joins the parts of the item that block c began and did not end: one block per
+// (c, row), its four warps a quarter of the parts each.
 template <int HDP, bool F16>
-__global__ void __launch_bounds__(512) k_attend_few_join(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(128) k_attend_few_join(const __grid_constant__ AttnParams p) {
+  constexpr int kCols = HDP / 32, kSlot = kRows * HDP + 2 * kRows;
+  __shared__ float acc[4][HDP], sums[4];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_for_primary();
   const int4 d = p.desc[blockIdx.x];
-  if (d.w == 0) return;
-  constexpr int kSubs = 512 / HDP;
-  __shared__ float acc[kSubs][HDP + 1], tops[512 / 32], sums[512 / 32];
-  __shared__ float all_top;
-  const int tid = threadIdx.x, sub = tid / HDP, col = tid % HDP, lane = tid & 31, warp = tid >> 5;
-  const AttnReq r = attn_req(p, d.x);
-  const int64_t item = (int64_t)d.z * 0x40000000 + d.y;
-  const FewItem x = few_item(p, r, d.x, item, row_tiles(p, r));
-  constexpr int kSlot = kRows * HDP + 2 * kRows;
+  const int rows = d.z >> 16, head0 = d.z & 0xFFFF, parts = d.w;
   // part k: block c's last segment, then the first segments of the following blocks
-  auto slot = [&](int k) { return p.part + (int64_t)((blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * kSlot; };
-  for (int row = blockIdx.y; row < x.rows; row += gridDim.y) {
+  const float* const base = p.part + (int64_t)blockIdx.x * 2 * kSlot;
+  auto slot = [&](int k) { return base + (int64_t)(k == 0 ? 1 : 2 * k) * kSlot; };
+  for (int row = blockIdx.y; parts != 0 && row < rows; row += gridDim.y) {
     float top = -INFINITY;
-    for (int k = tid; k < d.w; k += 512) top = fmaxf(top, slot(k)[kRows * HDP + row]);
+    for (int k = lane; k < parts; k += 32) top = fmaxf(top, slot(k)[kRows * HDP + row]);
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    if (lane == 0) tops[warp] = top;
-    __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
-      all_top = top;
-    }
-    __syncthreads();
-    top = all_top;
     const float safe = top == -INFINITY ? 0.f : top;
-    float v = 0.f, s = 0.f;
+    float v[kCols], s = 0.f;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) v[c] = 0.f;
 #pragma unroll 4
-    for (int k = sub; k < d.w; k += kSubs) {
+    for (int k = warp; k < parts; k += 4) {
       const float* at = slot(k);
       const float f = ex2(at[kRows * HDP + row] - safe);
-      v = fmaf(f, at[row * HDP + col], v);
       s = fmaf(f, at[kRows * HDP + kRows + row], s);
-    }
-    acc[sub][col] = v;
-    if (col == 0) sums[sub] = s;
-    __syncthreads();
-    if (tid < HDP) {
-      v = s = 0.f;
 #pragma unroll
-      for (int k = 0; k < kSubs; ++k) {
-        v += acc[k][tid];
-        s += sums[k];
+      for (int c = 0; c < kCols; c += 2) {
+        const float2 x = *(const float2*)(at + row * HDP + c * 32 + lane * 2);
+        v[c] = fmaf(f, x.x, v[c]);
+        v[c + 1] = fmaf(f, x.y, v[c + 1]);
       }
-      const int abs = x.row0 + row;
-      const int64_t tok = r.q0 + abs / p.group, head = (int64_t)x.head * p.group + abs % p.group;
-      v = s == 0.f ? 0.f : v / s;
-      if (tid < p.dim) {
-        uint16_t* to = (uint16_t*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + tid));
-        *to = F16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
-      }
-      if (p.lse && tid == 0) p.lse[tok * p.heads + head] = (top + log2f(s)) * 0.6931471805599453f;
     }
+#pragma unroll
+    for (int c = 0; c < kCols; c += 2) *(float2*)&acc[warp][c * 32 + lane * 2] = make_float2(v[c], v[c + 1]);
+    if (lane == 0) sums[warp] = s;
+    __syncthreads();
+    s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    const int abs = d.y + row;
+    const int64_t tok = d.x + abs / p.group, head = (int64_t)head0 * p.group + abs % p.group;
+    for (int col = threadIdx.x * 2; col < p.dim; col += 256) {
+      const float inv = s == 0.f ? 0.f : 1.f / s;
+      const float a = (acc[0][col] + acc[1][col]) + (acc[2][col] + acc[3][col]);
+      const float b = (acc[0][col + 1] + acc[1][col + 1]) + (acc[2][col + 1] + acc[3][col + 1]);
+      *(uint32_t*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) = pack2<F16>(a * inv, b * inv);
+    }
+    if (p.lse && threadIdx.x == 0) p.lse[tok * p.heads + head] = (top + log2f(s)) * 0.6931471805599453f;
     __syncthreads();
   }
 }
@@ -591,7 +591,7 @@ cudaError_t launch(const AttnParams& p, int rows_hint, int sms, int device, cuda
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(sms, rows_hint < 1 || rows_hint > kRows ? kRows : rows_hint);
-  cfg.blockDim = dim3(512);
+  cfg.blockDim = dim3(128);
   cfg.stream = stream;
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -96,6 +96,31 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+
+// Bounded wait of one thread: false once the block has given up, or after four
+// seconds (which it then flags).  The clock is looked at after the first polls
+// only: reading it takes longer than most waits.
+__device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up, int* flags) {
+  unsigned long long start = 0;
+  for (;;) {
+    for (int i = 0; i < 256; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long now = now_ns();
+    if (start == 0) start = now;
+    if (*(volatile int*)gave_up) return false;
+    if (now - start > 4000000000ull) {
+      *(volatile int*)gave_up = 1;
+      atomicOr(flags, kErrTimeout);
+      return false;
+    }
+  }
+}
+
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

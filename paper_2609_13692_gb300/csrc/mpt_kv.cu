@@ -109,7 +109,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   if (st != MPT_OK) return st;
   if (heads < 1 || heads % c->kv_heads != 0 || max_q_len < 0 || !std::isfinite(scale) || !(scale > 0.f) || !q_stride || !out_stride)
     return MPT_ERR_INVALID_ARG;
-  if (heads / c->kv_heads > 128) return MPT_ERR_TOO_LARGE;
+  if (heads / c->kv_heads > 128 || tokens * (heads / c->kv_heads) > INT32_MAX) return MPT_ERR_TOO_LARGE;
   const int64_t entries[2] = {tokens, heads};
   for (int i = 0; i < 2; ++i)
     if (!mpt::stride_ok(q_stride[i], entries[i]) || !mpt::stride_ok(out_stride[i], entries[i])) return MPT_ERR_INVALID_ARG;
