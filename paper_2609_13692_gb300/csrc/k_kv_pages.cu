@@ -311,7 +311,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   // Free pages of this warp's run.
   int free_here = 0;
   if (OP != kBookFree) {
-#pragma unroll 4
+#pragma unroll 8
     for (int at = run.lo; at < run.hi; at += 32) free_here += __popc(__ballot_sync(~0u, at + lane < run.hi && b.refs[at + lane] <= 0));
   }
 
@@ -367,11 +367,16 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   if (OP == kBookFree) flags &= ~MPT_KV_NO_PAGES;
   if (flags == 0 && OP != kBookFree) {
     int at = before;
-    for (int id = run.lo; id < run.hi && at < need; id += 32) {
-      const unsigned f = __ballot_sync(~0u, id + lane < run.hi && b.refs[id + lane] <= 0);
-      const int r = at + __popc(f & ((1u << lane) - 1u));
-      if ((f >> lane & 1u) && r < need) fresh[r] = id + lane;
-      at += __popc(f);
+    for (int id0 = run.lo; id0 < run.hi && at < need; id0 += 256) {
+      unsigned f[8];  // eight loads at a time
+#pragma unroll
+      for (int u = 0; u < 8; ++u) f[u] = __ballot_sync(~0u, id0 + 32 * u + lane < run.hi && b.refs[id0 + 32 * u + lane] <= 0);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int r = at + __popc(f[u] & ((1u << lane) - 1u));
+        if ((f[u] >> lane & 1u) && r < need) fresh[r] = id0 + 32 * u + lane;
+        at += __popc(f[u]);
+      }
     }
   }
   cl.sync();  // the fresh pages are known; nobody reads the first block's shared memory any more
@@ -432,7 +437,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   if (OP == kBookFree) {  // the pages that this call freed are counted too
     cl.sync();
     int n = 0, all;
-#pragma unroll 4
+#pragma unroll 8
     for (int at = run.lo; at < run.hi; at += 32) n += __popc(__ballot_sync(~0u, at + lane < run.hi && b.refs[at + lane] <= 0));
     cluster_prefix(cl, n, sh.mine, sh.all, &all);
     if (gw == 0 && lane == 0) {
@@ -456,7 +461,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   int per;
   const Scan run = my_run(b.n_pages, gw, &per);
   int live = 0, n_live;
-#pragma unroll 4
+#pragma unroll 8
   for (int at = run.lo; at < run.hi; at += 32) live += __popc(__ballot_sync(~0u, at + lane < run.hi && b.refs[at + lane] > 0));
   int before = cluster_prefix(cl, live, sh.mine, sh.all, &n_live);
   // live pages of id < n_live: those of the warps before the one whose run holds n_live, and a part of its own
@@ -464,6 +469,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   if (warp == 0) {
     int sum = 0;
     for (int i = lane; i < border && i < kScanWarps; i += 32) sum += sh.all[i];
+#pragma unroll 8
     for (int at = border * per; at < n_live; at += 32) {
       const int c = __popc(__ballot_sync(~0u, at + lane < n_live && b.refs[at + lane] > 0));
       if (lane == 0) sum += c;
@@ -474,15 +480,20 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   }
   __syncthreads();
   const int stay = sh.partial, moves = n_live - stay, half = b.n_pages / 2;
-  for (int id0 = run.lo; id0 < run.hi; id0 += 32) {
-    const int id = id0 + lane;
-    const bool in = id < run.hi, on = in && b.refs[id] > 0;
-    const unsigned f = __ballot_sync(~0u, on);
-    const int ahead = before + __popc(f & ((1u << lane) - 1u));  // live pages of a lower id
-    if (in && !on && id < n_live) p.copy_dst[id - ahead] = id;
-    if (on && id >= n_live) p.copy_src[ahead - stay] = id;
-    if (in && !on && id >= n_live) to[id] = id;
-    before += __popc(f);
+  for (int id0 = run.lo; id0 < run.hi; id0 += 256) {
+    unsigned f[8];  // eight loads at a time
+#pragma unroll
+    for (int u = 0; u < 8; ++u) f[u] = __ballot_sync(~0u, id0 + 32 * u + lane < run.hi && b.refs[id0 + 32 * u + lane] > 0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int id = id0 + 32 * u + lane;
+      const bool in = id < run.hi, on = f[u] >> lane & 1u;
+      const int ahead = before + __popc(f[u] & ((1u << lane) - 1u));  // live pages of a lower id
+      if (in && !on && id < n_live) p.copy_dst[id - ahead] = id;
+      if (on && id >= n_live) p.copy_src[ahead - stay] = id;
+      if (in && !on && id >= n_live) to[id] = id;
+      before += __popc(f[u]);
+    }
   }
   for (int k = moves + rank * kBookThreads + tid; k < half; k += all_threads) p.copy_src[k] = p.copy_dst[k] = -1;
   cl.sync();

@@ -162,9 +162,9 @@ def mpt_kv_merge(outs, lses, *, out=None, lse=None, stream: Optional[int] = None
 
     outs: a sequence of [.., head_dim] tensors (or one tensor of them along its first axis), bf16,
     f16 or f32; lses: likewise, float32 [..].  Parts with lse = -inf have no part in a row."""
-    po, shape, dtype, o = _parts(outs, "outs")
-    pl, lshape, ldtype, z = _parts(lses, "lses")
-    if len(po) != len(pl) or lshape != shape[:-1] or ldtype is not torch.float32:
+    n, po, shape, dtype, o = _parts(outs, "outs")
+    nl, pl, lshape, ldtype, z = _parts(lses, "lses")
+    if n != nl or lshape != shape[:-1] or ldtype is not torch.float32:
         raise ValueError("lses must be as many float32 tensors as outs, of their shape without the last axis")
     if dtype not in _TYPES or not shape:
         raise ValueError("outs must be bfloat16, float16 or float32 with heads of a last axis")
@@ -177,36 +177,39 @@ def mpt_kv_merge(outs, lses, *, out=None, lse=None, stream: Optional[int] = None
         _device(o, lse)
         if lse.shape != lshape or lse.dtype is not torch.float32 or not lse.is_contiguous():
             raise ValueError("lse must be contiguous float32 of lses' shape")
-    return _run(index, stream, _merge, po, pl, shape, dtype, o.device, out, lse)
+    return _run(index, stream, _merge, n, po, pl, shape, dtype, o.device, out, lse)
+
+
+def _addresses(at: list) -> bytes:
+    return struct.pack("@%dP" % len(at), *at)
 
 
 def _parts(parts, name: str):
-    """(addresses, shape, type, a tensor) of equal contiguous parts."""
+    """(number, packed addresses, shape, type, a tensor) of equal contiguous parts."""
     if isinstance(parts, torch.Tensor):
-        if parts.dim() < 1 or parts.shape[0] < 1 or not parts.is_contiguous():
+        shape = parts.shape
+        n = shape[0] if len(shape) else 0
+        if n < 1 or not parts.is_contiguous():
             raise ValueError(f"{name} must be contiguous parts, one at least")
-        n, at = parts.shape[0], parts.data_ptr()
-        step = parts.stride(0) * parts.element_size()
-        return [at + i * step for i in range(n)], parts.shape[1:], parts.dtype, parts
+        at, step = parts.data_ptr(), parts.stride(0) * parts.element_size()
+        return n, _addresses([at + i * step for i in range(n)]), shape[1:], parts.dtype, parts
     parts = list(parts)
     if not parts:
         raise ValueError(f"{name} must not be empty")
-    first = parts[0]
+    first, n = parts[0], len(parts)
     _device(first, *parts)
     for t in parts:
         if t.shape != first.shape or t.dtype is not first.dtype or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous and of one shape and type")
-    return [t.data_ptr() for t in parts], first.shape, first.dtype, first
+    return n, _addresses([t.data_ptr() for t in parts]), first.shape, first.dtype, first
 
 
-def _merge(s, po, pl, shape, dtype, device, out, lse):
+def _merge(s, n, po, pl, shape, dtype, device, out, lse):
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=device)
     if lse is None:
         lse = torch.empty(shape[:-1], dtype=torch.float32, device=device)
-    n = len(po)
-    status = _mpt.load().mpt_kv_merge(struct.pack("%dP" % n, *po), struct.pack("%dP" % n, *pl), n, lse.numel(), shape[-1],
-                                      _TYPES[dtype], out.data_ptr(), lse.data_ptr(), s)
+    status = _mpt.load().mpt_kv_merge(po, pl, n, lse.numel(), shape[-1], _TYPES[dtype], out.data_ptr(), lse.data_ptr(), s)
     if status:
         _mpt._check(status, "mpt_kv_merge")
     return out, lse
@@ -278,7 +281,8 @@ def mpt_kv_fork(table, lens, refs, page_size: int, src, dst, keep, *, workspace=
 
 
 def _fork(s, book, index, rows, n_pages, n, device, src, dst, keep, workspace):
-    old, fresh, status = torch.empty(2 * n + 2, dtype=_INT, device=device).split((n, n, 2))
+    old, fresh = torch.empty(n, dtype=_INT, device=device), torch.empty(n, dtype=_INT, device=device)
+    status = torch.empty(2, dtype=_INT, device=device)
     ws = _pages_workspace(workspace, index, rows, n_pages, device)
     st = _mpt.load().mpt_kv_fork(book, src.data_ptr(), dst.data_ptr(), keep.data_ptr(), n, old.data_ptr(), fresh.data_ptr(),
                                  status.data_ptr(), ws.data_ptr(), ws.numel(), s)
@@ -326,7 +330,8 @@ def mpt_kv_compact(table, lens, refs, page_size: int, *, workspace=None, stream:
 
 def _compact(s, book, index, rows, n_pages, _, device, workspace):
     n = n_pages // 2
-    old, fresh, status = torch.empty(2 * n + 2, dtype=_INT, device=device).split((n, n, 2))
+    old, fresh = torch.empty(n, dtype=_INT, device=device), torch.empty(n, dtype=_INT, device=device)
+    status = torch.empty(2, dtype=_INT, device=device)
     ws = _pages_workspace(workspace, index, rows, n_pages, device)
     st = _mpt.load().mpt_kv_compact(book, old.data_ptr(), fresh.data_ptr(), status.data_ptr(), ws.data_ptr(), ws.numel(), s)
     if st:
