@@ -396,11 +396,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     sh.gave_up = 0;
     mbar_init_fence();
   }
-  if (tid == 32) {  // the maps are read a good while before the first copy
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_k));
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_v));
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_q));
-  }
   launch_dependents();
   // The requests, in the room of the ring: first item, new tokens, keys, pairs.
   int4* const reqs = (int4*)ring;
@@ -978,7 +973,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
 }
 
 // Joins the parts of the item that block c began and did not end: a block per
-// (c, 32 rows, 32 columns), a lane per row, a warp per four columns.
+// (c, 32 rows), a lane per row, a warp per eighth of the columns.  (Four times the
+// blocks for a quarter of the columns each: 1 us less where 20 parts of 8 items
+// are joined, 20 us more where 152 items of 2 parts are.)
 template <int HDP, bool F16>
 __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant__ AttnParams p) {
   wait_for_primary();
@@ -990,30 +987,43 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
   const int64_t row_tok = ((int64_t)d.z * 2 + s) * p.toks + row / p.group;
   if (row >= p.toks * p.group || row_tok >= r.ql) return;
   constexpr int64_t kSlot = kRows * HDP + 2 * kRows;
-  const int col = blockIdx.z * 32 + warp * 4;
+  constexpr int kCols = HDP / 8;
   const float* first = p.part + ((int64_t)blockIdx.x * 2 + 1) * kSlot;
   const float* rest = p.part + ((int64_t)blockIdx.x * 2 + 2) * kSlot;  // then every second slot
-  float top = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, sum = 0.f, acc[kCols];
+#pragma unroll
+  for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
 #pragma unroll 8
   for (int k = 0; k < d.w; ++k) top = fmaxf(top, (k ? rest + 2 * (k - 1) * kSlot : first)[kRows * HDP + slot_row]);
   const float safe = top == -INFINITY ? 0.f : top;
-#pragma unroll 8
+#pragma unroll 4
   for (int k = 0; k < d.w; ++k) {
     const float* at = k ? rest + 2 * (k - 1) * kSlot : first;
     const float f = ex2(at[kRows * HDP + slot_row] - safe);
-    const float4 v = *(const float4*)(at + ((int64_t)(col / 4) * kRows + slot_row) * 4);
     sum = fmaf(f, at[kRows * HDP + kRows + slot_row], sum);
-    acc[0] = fmaf(f, v.x, acc[0]);
-    acc[1] = fmaf(f, v.y, acc[1]);
-    acc[2] = fmaf(f, v.z, acc[2]);
-    acc[3] = fmaf(f, v.w, acc[3]);
+#pragma unroll
+    for (int c = 0; c < kCols; c += 4) {
+      const float4 v = *(const float4*)(at + ((int64_t)(warp * kCols + c) / 4 * kRows + slot_row) * 4);
+      acc[c] = fmaf(f, v.x, acc[c]);
+      acc[c + 1] = fmaf(f, v.y, acc[c + 1]);
+      acc[c + 2] = fmaf(f, v.z, acc[c + 2]);
+      acc[c + 3] = fmaf(f, v.w, acc[c + 3]);
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int64_t tok = r.q0 + row_tok, head = (int64_t)d.y * p.group + row % p.group;
-  if (col < p.dim)
-    *(uint2*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) =
-        make_uint2(pack2<F16>(acc[0] * inv, acc[1] * inv), pack2<F16>(acc[2] * inv, acc[3] * inv));
-  if (p.lse && col == 0) p.lse[tok * p.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
+#pragma unroll
+  for (int c = 0; c < kCols; c += 8) {
+    const int col = warp * kCols + c;
+    if (col >= p.dim) break;
+    uint4 v;
+    v.x = pack2<F16>(acc[c] * inv, acc[c + 1] * inv);
+    v.y = pack2<F16>(acc[c + 2] * inv, acc[c + 3] * inv);
+    v.z = pack2<F16>(acc[c + 4] * inv, acc[c + 5] * inv);
+    v.w = pack2<F16>(acc[c + 6] * inv, acc[c + 7] * inv);
+    *(uint4*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) = v;
+  }
+  if (p.lse && warp == 0) p.lse[tok * p.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <int HDP, bool F16>
@@ -1032,7 +1042,7 @@ cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream
   k_attend_tile<HDP, F16><<<sms, kThreads, C::kSmem, stream>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(sms, kRows / 32, HDP / 32);
+  cfg.gridDim = dim3(sms, kRows / 32);
   cfg.blockDim = dim3(256);
   cfg.stream = stream;
   cudaLaunchAttribute at{};
