@@ -66,7 +66,7 @@ typedef struct mpt_kv_cache {
 } mpt_kv_cache;
 
 /* Bytes of workspace mpt_kv_attend needs on the current device (it depends on
- * the device and head_dim only, not on the lengths).  Errors: INVALID_ARG, CUDA. */
+ * the device only, not on the lengths).  Errors: INVALID_ARG, CUDA. */
 mpt_status mpt_kv_attend_workspace_bytes(int32_t head_dim, size_t* bytes);
 
 /* Attention of new tokens over a paged cache (the new tokens' keys and values

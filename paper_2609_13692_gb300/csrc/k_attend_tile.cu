@@ -4,7 +4,7 @@
 //
 // The running form over key tiles is that of k_attend_few.cu.  An item is a KV
 // head and two tiles of up to 128 query rows (row = token t, query head g of
-// the group), so both products of a key tile, S = Q K^T and O += P V, are
+// the group; one tile with heads above 128 elements), so both products of a key tile, S = Q K^T and O += P V, are
 // 128 x 128 x 128 and every key tile read serves 256 rows.
 //
 // Bound: 4 d operations per visible pair, on the tensor cores; per key tile two
@@ -39,7 +39,6 @@ namespace {
 __device__ int g_tile_flags;
 
 constexpr int kKeys = 128;     // keys of a tile
-constexpr int kRows = 256;     // rows of a slot of partial results
 constexpr int kThreads = 384;
 constexpr int kOddSets = 4;    // items whose notes are kept apart (warp 11 is at most two ahead of the rows)
 constexpr int kList = 32;      // items listed at a time
@@ -48,9 +47,11 @@ constexpr int kHeldSets = 16;  // key tiles whose page marks are kept apart
 template <int HDP>
 struct TileCfg {
   static constexpr int kBlk = HDP / 64;
+  static constexpr int kTiles = HDP == 256 ? 1 : 2;  // row tiles of an item: O takes HDP columns each, S 128, of 512
+  static constexpr int kRows = 128 * kTiles;         // rows of a slot of partial results
   static constexpr int kSlot = kKeys * HDP * 2;
-  static constexpr int kQ = 2 * 128 * HDP * 2;
-  static constexpr int kSlots = HDP == 64 ? 8 : 5;
+  static constexpr int kQ = kRows * HDP * 2;
+  static constexpr int kSlots = HDP == 64 ? 8 : HDP == 128 ? 5 : 2;
   static constexpr int kSmem = 1024 + kQ + kSlots * kSlot + 2048;
 };
 
@@ -242,7 +243,7 @@ __device__ __forceinline__ void turn4(uint4* v, int lane) {
 }
 
 // Items in their natural order: the requests, the KV heads of each, the pairs of
-// row tiles of each.  Where the call's keys and values fit in L2 the blocks share
+// row tiles of each (single row tiles with heads above 128).  Where the call's keys and values fit in L2 the blocks share
 // the line as it is.  Where they do not, every block would at any time be at
 // heads of its own, each read from memory for every pair: then the line takes
 // the items in columns, c, c + n, c + 2 n, .. of an n-block grid for c = 0, 1, ..,
@@ -252,13 +253,13 @@ __device__ __forceinline__ void turn4(uint4* v, int lane) {
 // 84 MB: 785 and 840 us, the blocks reading the same keys at the same time.)
 constexpr int64_t kNaturalBytes = 100ll << 20;  // of 126 MB of L2
 __device__ __forceinline__ int pairs_of(const AttnParams& p, int ql) {
-  return (int)(((int64_t)ql + 2 * p.toks - 1) / (2 * p.toks));
+  return (int)(((int64_t)ql + p.item_toks - 1) / p.item_toks);
 }
 // Key tiles that the pair has to take, one at least (a row without keys is written too).
 __device__ __forceinline__ int pair_cost(const AttnParams& p, int ql, int kvl, int pair) {
   int lim = kvl;
   if (p.causal) {
-    const int64_t tok = (int64_t)2 * p.toks * (pair + 1);
+    const int64_t tok = (int64_t)p.item_toks * (pair + 1);
     lim = kvl - ql + (tok < ql ? (int)tok : ql);  // > -2^31 + 1
   }
   return lim <= kKeys ? 1 : (lim - 1) / kKeys + 1;
@@ -272,10 +273,10 @@ struct TileItem {
   __device__ __forceinline__ void load(const AttnParams& p, const TileEntry* at) {
     const int4 a = ((const int4*)at)[0], b = ((const int4*)at)[1];
     e = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    tok0 = e.pair * 2 * p.toks;
+    tok0 = e.pair * p.item_toks;
     lim_first = limit(p, tok0);
     n0 = key_count(p, tok0);
-    n1 = key_count(p, (int64_t)tok0 + p.toks);
+    n1 = p.item_toks > p.toks ? key_count(p, (int64_t)tok0 + p.toks) : 0;
     tiles = n0 > n1 ? n0 : n1;
   }
   __device__ __forceinline__ int limit(const AttnParams& p, int t) const { return attn_limit(p, {e.q0, e.ql, e.kvl}, t); }
@@ -885,7 +886,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       // ---- out ----
       const int cost = pair_cost(p, w.e.ql, w.e.kvl, w.e.pair);
       const bool starts = w.e.t0 == 0, ends = w.e.t0 + w.e.seg == cost, whole = starts && ends;
-      if (first_tok < w.e.ql) {
+      if (s < C::kTiles && first_tok < w.e.ql) {
         const bool extra = odd && w.count(s) > 0 && odd[8];
         const float inv = l == 0.f ? 0.f : 1.f / l, scale = whole ? inv : 1.f;
         const int64_t tok_at = (int64_t)w.e.q0 + tok, head = (int64_t)w.e.head * p.group + sub;
@@ -893,7 +894,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         char* rows4[4];  // of the four lanes of a group
 #pragma unroll
         for (int e = 0; e < 4; ++e) rows4[e] = (char*)__shfl_sync(~0u, (uint64_t)out, lane & ~3 | e);
-        float* part = p.part + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * (kRows * HDP + 2 * kRows);
+        float* part = p.part + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * (C::kRows * HDP + 2 * C::kRows);
         for (int c = 0; c < HDP / 32; ++c) {
           float o[32];
           if (w.count(s) > 0) {
@@ -949,14 +950,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             // [column / 4][row][4]: a warp's 32 rows are 512 contiguous bytes
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
-              *(float4*)(part + ((int64_t)(8 * c + e / 4) * kRows + s * 128 + r) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              *(float4*)(part + ((int64_t)(8 * c + e / 4) * C::kRows + s * 128 + r) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
         if (whole) {
           if (valid && p.lse) p.lse[tok_at * p.heads + head] = (m + log2f(l)) * 0.6931471805599453f;
         } else {
-          part[kRows * HDP + s * 128 + r] = m;
-          part[kRows * HDP + kRows + s * 128 + r] = l;
+          part[C::kRows * HDP + s * 128 + r] = m;
+          part[C::kRows * HDP + C::kRows + s * 128 + r] = l;
         }
       }
       if (starts && !ends && tid == 0) {
@@ -984,9 +985,10 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const AttnReq r = attn_req(p, d.x);
   const int slot_row = blockIdx.y * 32 + lane, s = slot_row >> 7, row = slot_row & 127;
-  const int64_t row_tok = ((int64_t)d.z * 2 + s) * p.toks + row / p.group;
+  const int64_t row_tok = (int64_t)d.z * p.item_toks + s * p.toks + row / p.group;
   if (row >= p.toks * p.group || row_tok >= r.ql) return;
-  constexpr int64_t kSlot = kRows * HDP + 2 * kRows;
+  using C = TileCfg<HDP>;
+  constexpr int64_t kSlot = C::kRows * HDP + 2 * C::kRows;
   constexpr int kCols = HDP / 8;
   const float* first = p.part + ((int64_t)blockIdx.x * 2 + 1) * kSlot;
   const float* rest = p.part + ((int64_t)blockIdx.x * 2 + 2) * kSlot;  // then every second slot
@@ -994,16 +996,16 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
 #pragma unroll
   for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
 #pragma unroll 8
-  for (int k = 0; k < d.w; ++k) top = fmaxf(top, (k ? rest + 2 * (k - 1) * kSlot : first)[kRows * HDP + slot_row]);
+  for (int k = 0; k < d.w; ++k) top = fmaxf(top, (k ? rest + 2 * (k - 1) * kSlot : first)[C::kRows * HDP + slot_row]);
   const float safe = top == -INFINITY ? 0.f : top;
 #pragma unroll 4
   for (int k = 0; k < d.w; ++k) {
     const float* at = k ? rest + 2 * (k - 1) * kSlot : first;
-    const float f = ex2(at[kRows * HDP + slot_row] - safe);
-    sum = fmaf(f, at[kRows * HDP + kRows + slot_row], sum);
+    const float f = ex2(at[C::kRows * HDP + slot_row] - safe);
+    sum = fmaf(f, at[C::kRows * HDP + C::kRows + slot_row], sum);
 #pragma unroll
     for (int c = 0; c < kCols; c += 4) {
-      const float4 v = *(const float4*)(at + ((int64_t)(warp * kCols + c) / 4 * kRows + slot_row) * 4);
+      const float4 v = *(const float4*)(at + ((int64_t)(warp * kCols + c) / 4 * C::kRows + slot_row) * 4);
       acc[c] = fmaf(f, v.x, acc[c]);
       acc[c + 1] = fmaf(f, v.y, acc[c + 1]);
       acc[c + 2] = fmaf(f, v.z, acc[c + 2]);
@@ -1042,7 +1044,7 @@ cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream
   k_attend_tile<HDP, F16><<<sms, kThreads, C::kSmem, stream>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(sms, kRows / 32);
+  cfg.gridDim = dim3(sms, C::kRows / 32);
   cfg.blockDim = dim3(256);
   cfg.stream = stream;
   cudaLaunchAttribute at{};
@@ -1055,13 +1057,14 @@ cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream
 
 }  // namespace
 
-size_t attend_tile_workspace(int sms) {
-  return (size_t)sms * sizeof(int4) + 256 + (size_t)sms * 2 * (kRows * 128 + 2 * kRows) * sizeof(float);
+size_t attend_tile_workspace(int sms) {  // a slot has as much room for 128 rows of 256 columns as for 256 of 128
+  return (size_t)sms * sizeof(int4) + 256 + (size_t)sms * 2 * (256 * 128 + 2 * 256) * sizeof(float);
 }
 
 cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int device, cudaStream_t stream) {
   if (p.dim <= 64) return f16 ? launch<64, true>(p, sms, device, stream) : launch<64, false>(p, sms, device, stream);
-  return f16 ? launch<128, true>(p, sms, device, stream) : launch<128, false>(p, sms, device, stream);
+  if (p.dim <= 128) return f16 ? launch<128, true>(p, sms, device, stream) : launch<128, false>(p, sms, device, stream);
+  return f16 ? launch<256, true>(p, sms, device, stream) : launch<256, false>(p, sms, device, stream);
 }
 
 cudaError_t attend_tile_flags(cudaStream_t stream, int* flags) {

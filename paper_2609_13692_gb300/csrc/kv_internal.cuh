@@ -27,7 +27,7 @@ struct alignas(128) AttnParams {
   int4* desc;   // one per block: what its last, unfinished item is
   int64_t tokens;
   int32_t width, n_pages, page_log2, batch, heads, kv_heads, group, dim, causal;
-  int32_t box, toks;  // page slots per copy; whole tokens of 128 rows
+  int32_t box, toks, item_toks;  // page slots per copy; whole tokens of 128 rows, and of an item
   float scale_log2;  // scale * log2(e)
 };
 
@@ -197,7 +197,7 @@ cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int 
 // Flags of the kernels since the last call (waits for the stream).
 cudaError_t attend_few_flags(cudaStream_t stream, int* flags);
 
-// Whole tiles of query rows on tcgen05 (k_attend_tile.cu); head_dim <= 128, at
+// Whole tiles of query rows on tcgen05 (k_attend_tile.cu); at
 // most kTileBatch requests (its list of them, 16 bytes each, is in the room of
 // the ring of slots).
 constexpr int kTileBatch = 8192;

@@ -84,9 +84,9 @@ bool make_query_map(CUtensorMap* map, const AttnParams& p, bool f16) {
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-size_t attend_workspace(int head_dim, int sms) {
+size_t attend_workspace(int sms) {
   const size_t few = attend_few_workspace(sms), tile = attend_tile_workspace(sms);
-  return head_dim > 128 || few > tile ? few : tile;
+  return few > tile ? few : tile;
 }
 
 }  // namespace
@@ -97,7 +97,7 @@ extern "C" {
 mpt_status mpt_kv_attend_workspace_bytes(int32_t head_dim, size_t* bytes) {
   if (!bytes || head_dim < 8 || head_dim > 256 || head_dim % 8 != 0) return MPT_ERR_INVALID_ARG;
   int device = 0;
-  *bytes = mpt::attend_workspace(head_dim, mpt::kv_sm_count(&device));
+  *bytes = mpt::attend_workspace(mpt::kv_sm_count(&device));
   return MPT_OK;
 }
 
@@ -118,7 +118,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   int device = 0;
   const int sms = mpt::kv_sm_count(&device);
   if (!workspace || !mpt::aligned(workspace, 256)) return MPT_ERR_INVALID_ARG;
-  if (workspace_bytes < mpt::attend_workspace(c->head_dim, sms)) return MPT_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < mpt::attend_workspace(sms)) return MPT_ERR_WORKSPACE_TOO_SMALL;
 
   mpt::AttnParams p;
   std::memset((void*)&p, 0, sizeof(p));
@@ -142,6 +142,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   p.group = heads / c->kv_heads;
   p.dim = c->head_dim;
   p.toks = 128 / p.group;
+  p.item_toks = p.toks * (p.dim > 128 ? 1 : 2);
   p.causal = causal != 0;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t stream = (cudaStream_t)stream_ptr;
@@ -152,7 +153,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   // Few rows per KV head: 16 of them fill the smaller kernel's products.  Where
   // the caller does not say, as many tokens as requests are taken for one each.
   const int64_t most = max_q_len > 0 ? max_q_len : tokens <= c->batch ? 1 : 129;
-  const bool tile = c->head_dim <= 128 && most * p.group > 16 && c->batch <= mpt::kTileBatch;
+  const bool tile = most * p.group > 16 && c->batch <= mpt::kTileBatch;
   const int keys = tile ? 128 : 64;
   p.box = c->page_size < keys ? c->page_size : keys;
   if (!mpt::make_map(&p.map_k, *c, c->k, c->k_stride, p.box) || !mpt::make_map(&p.map_v, *c, c->v, c->v_stride, p.box) ||
