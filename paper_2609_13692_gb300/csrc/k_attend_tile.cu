@@ -52,6 +52,11 @@ struct TileCfg {
   static constexpr int kSlot = kKeys * HDP * 2;
   static constexpr int kQ = kRows * HDP * 2;
   static constexpr int kSlots = HDP == 64 ? 8 : HDP == 128 ? 5 : 2;
+  // Who waits for keys.  Warp 11 may, as it may skip an item's first ones, where
+  // the slot's next use is far enough off to imply that they have landed; with
+  // two slots the next key tile is the slot's next phase, and a wait for it
+  // before the one at hand has landed would pass at once.
+  static constexpr bool kWatchKeys = kSlots > 2;
   static constexpr int kSmem = 1024 + kQ + kSlots * kSlot + 2048;
 };
 
@@ -661,6 +666,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           if (j < n0) {
             ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
             ready ^= 1;
+            if (!C::kWatchKeys && ok && more) ok = wait_all(&sh.full[sk], phase, gave_up);
             if (!ok) break;
             fence_after();
             if (elect_one()) {
@@ -759,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
           }
-          if (j + 1 < w.tiles) ok = wait_all(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
+          if (C::kWatchKeys && j + 1 < w.tiles) ok = wait_all(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
           if (!ok) break;
           // not a tile ahead of the rows, or two arrivals would count in one phase
           if (due & 1) ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
