@@ -47,7 +47,12 @@ constexpr int kHeldSets = 16;  // key tiles whose page marks are kept apart
 template <int HDP>
 struct TileCfg {
   static constexpr int kBlk = HDP / 64;
-  static constexpr int kTiles = HDP == 256 ? 1 : 2;  // row tiles of an item: O takes HDP columns each, S 128, of 512
+  // Row tiles of an item: O takes HDP columns each, S 128, of 512.  With one, S
+  // has two buffers, and the scores of the next key tile are made while P of this
+  // one is (2,048 tokens over 10,000 keys, 32 heads of 256: 719 -> 610 us).  For
+  // single row tiles of smaller heads the same was slower (28 rows over 20,001
+  // keys 43 -> 50 us): the ring then holds less ahead.
+  static constexpr int kTiles = HDP == 256 ? 1 : 2;
   static constexpr int kRows = 128 * kTiles;         // rows of a slot of partial results
   static constexpr int kSlot = kKeys * HDP * 2;
   static constexpr int kQ = kRows * HDP * 2;
@@ -67,7 +72,7 @@ struct alignas(16) TileEntry {
 };
 
 struct TileShared {
-  unsigned long long full[8], empty[8], q_full, q_empty, s_full[2], p_ready[2], o_full[2], drain;
+  unsigned long long full[8], empty[8], q_full, q_empty, s_full[3], p_ready[3], o_full[2], o_step, drain;
   uint32_t tmem;
   int gave_up;
   uint32_t held[kHeldSets];
@@ -393,11 +398,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     }
     mbar_init(&sh.q_full, 1);
     mbar_init(&sh.q_empty, 1);
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < 3; ++s) {  // 2: the second score buffer with one row tile
       mbar_init(&sh.s_full[s], 1);
       mbar_init(&sh.p_ready[s], 5);  // four warps of rows, and warp 11
-      mbar_init(&sh.o_full[s], 1);
     }
+    mbar_init(&sh.o_full[0], 1);
+    mbar_init(&sh.o_full[1], 1);
+    mbar_init(&sh.o_step, 1);
     mbar_init(&sh.drain, 1);
     sh.gave_up = 0;
     mbar_init_fence();
@@ -623,20 +630,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       constexpr uint32_t kSlotStep = C::kSlot >> 4, kBlocks = (uint32_t)(kKeys * 128) >> 4 << 16;
       uint32_t item = 0, ready = 0;
       bool ok = true;
-      auto outputs = [&](int s, int slot, bool add) {  // by one lane
+      // from P at column `at`, into row tile s's output
+      auto outputs = [&](int s, int at, int slot, bool add) {  // by one lane
         const uint32_t v_at = (ring_at + slot * kSlotStep) | kBlocks;
 #pragma unroll
         for (int k = 0; k < kKeys / 16; ++k)
-          mma_ts(acc + 256 + s * 128, acc + s * 128 + k * 8, v_at + k * (2048 >> 4), desc_o, add || k > 0);
+          mma_ts(acc + 256 + s * 128, acc + at + k * 8, v_at + k * (2048 >> 4), desc_o, add || k > 0);
       };
-      auto scores = [&](int s, int slot) {  // by one lane
+      // of row tile s, into column `at`
+      auto scores = [&](int s, int at, int bar, int slot) {  // by one lane
         const uint32_t a = q_at + s * (C::kBlk * 128 * 128 >> 4), b = ring_at + slot * kSlotStep;
 #pragma unroll
         for (int k = 0; k < HDP / 16; ++k) {
           const uint32_t off = (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2;
-          if (k < steps) mma_ss(acc + s * 128, a + off, b + off, desc_s, k > 0);
+          if (k < steps) mma_ss(acc + at, a + off, b + off, desc_s, k > 0);
         }
-        commit(&sh.s_full[s]);
+        commit(&sh.s_full[bar]);
       };
       auto after = [](int slot, int n) { return slot + n < C::kSlots ? slot + n : slot + n - C::kSlots; };
       int sk = 0;          // slot of the next key tile; its values follow
@@ -650,54 +659,101 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         if (!ok) break;
         fence_after();
         if (elect_one()) {
-          if (n0 > 0) scores(0, sk);
-          if (n1 > 0) scores(1, sk);
+          if (n0 > 0) scores(0, 0, 0, sk);
+          if (n1 > 0) scores(1, 128, 1, sk);
           commit(&sh.empty[sk]);
           if (tiles == 1) commit(&sh.q_empty);
         }
         __syncwarp();
-        for (int j = 0; j < tiles; ++j) {
-          const int sv = after(sk, 1);
-          if (sk + 2 >= C::kSlots) phase ^= 1;
-          sk = after(sk, 2);
-          const bool more = j + 1 < tiles;
-          // p_ready is complete once P stands, and this tile's values and the
-          // next one's keys are there (warp 11 waits for those): one wait here
-          if (j < n0) {
-            ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
-            ready ^= 1;
-            if (!C::kWatchKeys && ok && more) ok = wait_all(&sh.full[sk], phase, gave_up);
+        if constexpr (C::kTiles == 1) {
+          // The next scores are made while this tile's P is.
+          int sv = after(sk, 1);
+          auto step = [&] {
+            if (sk + 2 >= C::kSlots) phase ^= 1;
+            sk = after(sk, 2);
+          };
+          step();
+          if (tiles > 1) {
+            ok = wait_all(&sh.full[sk], phase, gave_up);
             if (!ok) break;
             fence_after();
             if (elect_one()) {
-              outputs(0, sv, j > 0);
-              if (j >= n1) commit(&sh.empty[sv]);
-              if (j + 1 < n0) scores(0, sk);
-              else commit(&sh.o_full[0]);
-              if (more && j + 1 >= n1) {
-                commit(&sh.empty[sk]);
-                if (j + 2 == tiles) commit(&sh.q_empty);  // no more scores
-              }
+              scores(0, 128, 2, sk);
+              commit(&sh.empty[sk]);
+              if (tiles == 2) commit(&sh.q_empty);
             }
             __syncwarp();
+            step();
           }
-          if (j < n1) {
-            ok = wait_all(&sh.p_ready[1], ready >> 1, gave_up);
-            ready ^= 2;
+          for (int j = 0; j < tiles; ++j) {
+            const int b = j & 1 ? 2 : 0;
+            ok = wait_all(&sh.p_ready[b], ready >> b & 1, gave_up);
+            ready ^= 1u << b;
             if (!ok) break;
             fence_after();
             if (elect_one()) {
-              outputs(1, sv, j > 0);
+              outputs(0, j & 1 ? 128 : 0, sv, j > 0);
               commit(&sh.empty[sv]);
-              if (j + 1 < n1) {
-                scores(1, sk);
-                commit(&sh.empty[sk]);
-                if (j + 2 == tiles) commit(&sh.q_empty);
-              } else {
-                commit(&sh.o_full[1]);
-              }
+              commit(&sh.o_step);
+              if (j + 1 == tiles) commit(&sh.o_full[0]);
             }
             __syncwarp();
+            sv = after(sv, 2);
+            if (j + 2 < tiles) {
+              if (!C::kWatchKeys) ok = wait_all(&sh.full[sk], phase, gave_up);
+              if (!ok) break;
+              if (elect_one()) {
+                scores(0, j & 1 ? 128 : 0, b, sk);
+                commit(&sh.empty[sk]);
+                if (j + 3 == tiles) commit(&sh.q_empty);
+              }
+              __syncwarp();
+              step();
+            }
+          }
+        } else {
+          for (int j = 0; j < tiles; ++j) {
+            const int sv = after(sk, 1);
+            if (sk + 2 >= C::kSlots) phase ^= 1;
+            sk = after(sk, 2);
+            const bool more = j + 1 < tiles;
+            // p_ready is complete once P stands, and this tile's values and the
+            // next one's keys are there (warp 11 waits for those): one wait here
+            if (j < n0) {
+              ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
+              ready ^= 1;
+              if (!ok) break;
+              fence_after();
+              if (elect_one()) {
+                outputs(0, 0, sv, j > 0);
+                if (j >= n1) commit(&sh.empty[sv]);
+                if (j + 1 < n0) scores(0, 0, 0, sk);
+                else commit(&sh.o_full[0]);
+                if (more && j + 1 >= n1) {
+                  commit(&sh.empty[sk]);
+                  if (j + 2 == tiles) commit(&sh.q_empty);  // no more scores
+                }
+              }
+              __syncwarp();
+            }
+            if (j < n1) {
+              ok = wait_all(&sh.p_ready[1], ready >> 1, gave_up);
+              ready ^= 2;
+              if (!ok) break;
+              fence_after();
+              if (elect_one()) {
+                outputs(1, 128, sv, j > 0);
+                commit(&sh.empty[sv]);
+                if (j + 1 < n1) {
+                  scores(1, 128, 1, sk);
+                  commit(&sh.empty[sk]);
+                  if (j + 2 == tiles) commit(&sh.q_empty);
+                } else {
+                  commit(&sh.o_full[1]);
+                }
+              }
+              __syncwarp();
+            }
           }
         }
       } while (ok && uniform(next_item(k)));
@@ -712,7 +768,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       // ---- copies that have landed, and values that some row must not see ----
       TileItem w;
       int k = 0;
-      uint32_t idx = 0, item = 0, ready = 0, due = 0;  // idx: ring use of tile j's keys; due: row tiles with a phase to end
+      uint32_t idx = 0, item = 0, ready = 0, due = 0;  // idx: ring use of tile j's keys; due: score buffers with a phase to end
       bool ok = true;
       do {
         w.load(p, &sh.list[k]);
@@ -768,14 +824,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           if (C::kWatchKeys && j + 1 < w.tiles) ok = wait_all(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
           if (!ok) break;
           // not a tile ahead of the rows, or two arrivals would count in one phase
+          constexpr int kSecond = C::kTiles == 1 ? 2 : 1;
           if (due & 1) ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
-          if (ok && (due & 2)) ok = wait_all(&sh.p_ready[1], ready >> 1, gave_up);
+          if (ok && (due & 2)) ok = wait_all(&sh.p_ready[kSecond], ready >> 1, gave_up);
           if (!ok) break;
           ready ^= due;
-          due = (j < w.n0 ? 1 : 0) | (j < w.n1 ? 2 : 0);
+          due = C::kTiles == 1 ? 1 + (j & 1) : (j < w.n0 ? 1 : 0) | (j < w.n1 ? 2 : 0);
           if (lane == 0) {
             if (due & 1) mbar_arrive(&sh.p_ready[0]);
-            if (due & 2) mbar_arrive(&sh.p_ready[1]);
+            if (due & 2) mbar_arrive(&sh.p_ready[kSecond]);
           }
           __syncwarp();
         }
@@ -789,7 +846,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     int k = 0;
     const int s = warp >> 2, r = tid & 127, r_tok = r / p.group, sub = r % p.group;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + s * 128 + lanes, t_o = tmem + 256 + s * 128 + lanes;
-    uint32_t scored = 0, done = 0, item = 0, gt = 0;
+    uint32_t scored = 0, done = 0, item = 0, gt = 0, steps = 0;  // scored: phases of this row tile's buffer and of buffer 2
     bool ok = true;
     do {
       w.load(p, &sh.list[k]);
@@ -800,13 +857,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       const int lim_tile = first_tok < w.e.ql ? w.limit(p, (int)first_tok) : 0;  // what every row of the tile sees
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < w.count(s); ++j) {
-        ok = wait_all(&sh.s_full[s], scored & 1, gave_up);
-        ++scored;
+        const bool second = C::kTiles == 1 && (j & 1);  // of the two score buffers
+        const int buf = second ? 2 : s;
+        const uint32_t t_p = second ? t_s + 128 : t_s;
+        ok = wait_all(&sh.s_full[buf], second ? scored >> 1 : scored & 1, gave_up);
+        scored ^= second ? 2 : 1;
         if (!ok) break;
         fence_after();
         float f[128];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(f + 32 * c, t_s + 32 * c);
+        for (int c = 0; c < 4; ++c) tmem_ld32(f + 32 * c, t_p + 32 * c);
         wait_ld();
         const uint32_t held = sh.held[(gt + j) % kHeldSets];
         const int key0 = (w.e.t0 + j) * kKeys;
@@ -836,9 +896,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         if (j == 0) {
           m = top;
         } else if (__any_sync(~0u, top - m > 8.f)) {
-          const float safe = top == -INFINITY ? 0.f : top;
+          if (C::kTiles == 1) {  // these scores did not wait for the outputs before them, which come in order
+            ok = wait_all(&sh.o_step, (steps + j - 1) & 1, gave_up);
+            if (!ok) break;
+            fence_after();
+          }
           const bool grows = top - m > 8.f;
-          const float a = grows ? ex2(m - safe) : 1.f;
+          const float a = grows ? ex2(m - top) : 1.f;
           m = grows ? top : m;
           l *= a;
 #pragma unroll 1
@@ -869,7 +933,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair(a, b));
             x[e / 2] = pack2<F16>(a, b);
           }
-          tmem_st16(t_s + c / 2, x);
+          tmem_st16(t_p + c / 2, x);
         }
         float s0, s1;
         unpair(add2(sum[0], sum[1]), s0, s1);
@@ -877,10 +941,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         wait_st();
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_ready[s]);
+        if (lane == 0) mbar_arrive(&sh.p_ready[buf]);
       }
       if (!ok) break;
       gt += w.tiles;
+      if (C::kTiles == 1) steps += w.n0;
       const uint32_t* odd = nullptr;
       if (w.tiles > 0) odd = sh.odd[item++ % kOddSets];
       if (w.count(s) > 0) {
