@@ -12,15 +12,17 @@
 // Bound: the cache is read once, 2 L Hkv d elements, for 4 d operations per
 // element and query head of the group: with up to 16 rows that is below what
 // the memory allows a tensor core to do, so the kernel is built around the
-// copy.  Four warps issue tensor-map copies of pages into a ring of stages (64
-// keys of K and V each); eight others take 16 keys of a stage apiece through
-// ldmatrix and m16n8k16 products with 32-bit accumulators, without a barrier
-// among them until the item's end.
+// copy.  A warp issues tensor-map copies of pages into a ring of stages (64 keys
+// of K and V each); four others take 16 keys of a stage apiece through ldmatrix
+// and m16n8k16 products with 32-bit accumulators, without a barrier among them
+// until the item's end.  Two or three such blocks share an SM, so that one's
+// reads of queries and joins do not hold up the other's products (200 requests
+// of 200 to 400 keys: 57 us, 78 with one block of eight such warps).
 //
 // Measured (one GB300, 8 KV heads of 128): 3 requests of 100,001 to 131,072 keys,
 // pages of 64: 204 us, 6.6 TB/s, 0.97 of the measured copy rate; 28 of 2,000 to
-// 6,000, pages of 16: 82 us, 5.6 TB/s (copies of 2 KB); one of 777: 9.9 us,
-// launches and a chain of dependent reads.
+// 6,000, pages of 16: 79 us, 5.8 TB/s, 12 us of it start, end and join; one of
+// 777: 9.9 us, launches and a chain of dependent reads.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -36,24 +38,24 @@ constexpr int kRows = 16;      // query rows of an item
 
 template <int HDP>
 struct FewCfg {
-  static constexpr int kWarps = HDP == 256 ? 4 : 8;  // 256: 128 accumulators a thread
-  static constexpr int kGroups = kWarps / 4;         // groups of four warps take stages in turn
+  static constexpr int kPerSm = HDP == 64 ? 3 : HDP == 128 ? 2 : 1;  // blocks: an item's end in one, products in another
+  static constexpr int kWarps = 4;                                   // each 16 keys of a stage
   // One warp issues a copy every 95 cycles or so: with pages of 16 (2 KB each)
-  // that is 21 bytes a cycle, less than an SM's share of the memory.
-  static constexpr int kCopyWarps = HDP == 256 ? 2 : 4;
+  // that is 21 bytes a cycle, where an SM's share of the memory is 23.
+  static constexpr int kCopyWarps = HDP == 256 ? 3 : 1;
   static constexpr int kThreads = 32 * (kWarps + kCopyWarps);
   static constexpr int kStage = 2 * kKeys * HDP * 2;
-  // A stage always belongs to one group: a group that waits for a stage's next
-  // phase has then itself seen the phase before complete.  Copies may land out
-  // of order, and a wait one phase ahead would pass at once.
-  static constexpr int kStages = HDP == 64 ? 12 : HDP == 128 ? 4 : 2;
-  static_assert(kStages % kGroups == 0 && kStages % kCopyWarps == 0);
-  static constexpr int kBufs = kWarps / 2;
-  static constexpr int kPad = HDP + 8;               // row of a joining buffer, in floats
-  static constexpr int kBuf = kBufs * kRows * kPad * 4;
+  // A stage always belongs to one copying warp, and every warp of products waits
+  // for every stage: each sees all of a barrier's phases in order.  (A wait for
+  // a phase before the one at hand is complete would pass at once.)
+  static constexpr int kStages = HDP == 64 ? 4 : 3;
+  static_assert(kStages % kCopyWarps == 0);
+  static constexpr int kPad = HDP + 8;               // row of the joining buffer, in floats
+  static constexpr int kBuf = kRows * kPad * 4;
   static constexpr int kQPad = HDP + 8;              // row of the staged queries (HDP 256)
   static constexpr int kQ = HDP == 256 ? kRows * kQPad * 2 : 0;
-  static constexpr int kSmem = 1024 + kStages * kStage + kBuf + kQ + 1024 + 2048;
+  static constexpr int kMl = kWarps * 2 * kRows * 4;
+  static constexpr int kSmem = 1024 + kStages * kStage + kBuf + kQ + kMl + 128 + 320;
 };
 
 template <bool F16>
@@ -133,7 +135,7 @@ __device__ __forceinline__ FewItem few_item(const AttnParams& p, const AttnReq& 
 }
 
 template <int HDP, bool F16>
-__global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_attend_few(const __grid_constant__ AttnParams p) {
   using C = FewCfg<HDP>;
   extern __shared__ char raw[];
   char* base = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
@@ -141,10 +143,10 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
   float* bufs = (float*)(base + C::kStages * C::kStage);
   uint16_t* qs = (uint16_t*)((char*)bufs + C::kBuf);
   float* ml = (float*)((char*)qs + C::kQ);  // [kWarps][2][kRows]
-  unsigned long long* full = (unsigned long long*)((char*)ml + 1024);
+  unsigned long long* full = (unsigned long long*)((char*)ml + C::kMl);
   unsigned long long* empty = full + C::kStages;
   uint32_t* there = (uint32_t*)(empty + C::kStages);  // per stage: which groups of 8 keys the cache holds
-  int64_t* scratch = (int64_t*)((char*)ml + 1024 + 512);
+  int64_t* scratch = (int64_t*)((char*)ml + C::kMl + 128);
   __shared__ int gave_up;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -198,7 +200,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
       };
       const int mine = lane % per;  // per is a power of two of at most 8
       // this warp's next tile, and its pages ahead of need
-      int t = t0 + (int)((me - it0) % C::kCopyWarps);
+      int t = t0 + (int)((me + C::kCopyWarps - it0 % C::kCopyWarps) % C::kCopyWarps);
       int next = page_of(t, mine);
       for (; t < last; t += C::kCopyWarps) {
         const uint32_t it = it0 + (uint32_t)(t - t0);
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
   }
 
   // ---- products ----
-  const int group = warp >> 2, key0 = (warp & 3) * 16;
+  const int key0 = warp * 16;
   const int g = lane >> 2, c2 = (lane & 3) * 2;
   constexpr int kK = HDP / 16;
   while (left > 0) {
@@ -303,7 +305,6 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
     for (int t = t0; t < last; ++t, ++it) {
-      if ((int)(it % C::kGroups) != group) continue;
       const int s = it % C::kStages;
       wait_bar(&full[s], (it / C::kStages) & 1, &gave_up, &g_few_flags);  // having given up, the block still ends in order
       const uint32_t kbase = smem_u32(ring + s * C::kStage), vbase = kbase + C::kStage / 2;
@@ -452,18 +453,21 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
       for (int w = 0; w < C::kWarps; ++w) top = fmaxf(top, ml[(w * 2) * kRows + g + 8 * h]);
       f[h] = ex2(m[h] - (top == -INFINITY ? 0.f : top));
     }
-    // A warp without a key in a row adds nothing (f = 0, its o is 0).
+    // A warp without a key in a row adds nothing (f = 0, its o is 0).  The warps
+    // add one after the other into one buffer, the first half of the columns in
+    // the order 3, 2, 1, 0 and the second in 2, 3, 0, 1, two warps at a time.
 #pragma unroll
-    for (int half = 1; half >= 0; --half) {
-      if ((warp >= C::kBufs) == (half == 1)) {
-        float* buf = bufs + (warp % C::kBufs) * kRows * C::kPad;
+    for (int round = 0; round < 4; ++round) {
 #pragma unroll
-        for (int n = 0; n < HDP / 8; ++n)
+      for (int half = 0; half < 2; ++half) {
+        if (warp != (half == 0 ? 3 - round : (round + 2) & 3)) continue;
+#pragma unroll
+        for (int n = half * (HDP / 16); n < (half + 1) * (HDP / 16); ++n)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            float2* at = (float2*)(buf + (g + 8 * h) * C::kPad + n * 8 + c2);
+            float2* at = (float2*)(bufs + (g + 8 * h) * C::kPad + n * 8 + c2);
             float2 v = make_float2(o[n][2 * h] * f[h], o[n][2 * h + 1] * f[h]);
-            if (half == 0) {
+            if (round > 0) {
               const float2 w = *at;
               v.x += w.x;
               v.y += w.y;
@@ -486,11 +490,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, 1) k_attend_few(const _
 #pragma unroll
       for (int w = 0; w < C::kWarps; ++w) sum += ml[(w * 2 + 1) * kRows + row] * ex2(ml[(w * 2) * kRows + row] - safe);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = 0.f;
-#pragma unroll
-      for (int b = 0; b < C::kBufs; ++b)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] += bufs[(b * kRows + row) * C::kPad + col + q];
+      for (int q = 0; q < 8; q += 4) *(float4*)(v + q) = *(const float4*)(bufs + row * C::kPad + col + q);
       if (whole) {
         const int abs = x.row0 + row;
         const int64_t tok = r.q0 + abs / p.group, head = (int64_t)x.head * p.group + abs % p.group;
@@ -593,10 +593,11 @@ cudaError_t launch(const AttnParams& p, int rows_hint, int sms, int device, cuda
   static std::atomic<uint64_t> allowed;
   cudaError_t e = kv_allow_smem(k_attend_few<HDP, F16>, C::kSmem, device, allowed);
   if (e != cudaSuccess) return e;
-  k_attend_few<HDP, F16><<<sms, C::kThreads, C::kSmem, stream>>>(p);
+  const int blocks = sms * C::kPerSm;
+  k_attend_few<HDP, F16><<<blocks, C::kThreads, C::kSmem, stream>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(sms, rows_hint < 1 || rows_hint > kRows ? kRows : rows_hint);
+  cfg.gridDim = dim3(blocks, rows_hint < 1 || rows_hint > kRows ? kRows : rows_hint);
   cfg.blockDim = dim3(128);
   cfg.stream = stream;
   cudaLaunchAttribute at{};
@@ -610,7 +611,8 @@ cudaError_t launch(const AttnParams& p, int rows_hint, int sms, int device, cuda
 }  // namespace
 
 size_t attend_few_workspace(int sms) {
-  return (size_t)sms * sizeof(int4) + 256 + (size_t)sms * 2 * (kRows * 256 + 2 * kRows) * sizeof(float);
+  // slots of 64 columns for three blocks an SM, 128 for two, 256 for one: 256 hold any
+  return (size_t)sms * kFewPerSm * sizeof(int4) + 256 + (size_t)sms * 2 * (kRows * 256 + 2 * kRows * kFewPerSm) * sizeof(float);
 }
 
 cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, int device, cudaStream_t stream) {

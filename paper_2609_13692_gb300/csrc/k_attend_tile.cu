@@ -1141,7 +1141,7 @@ cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream
 }  // namespace
 
 size_t attend_tile_workspace(int sms) {  // a slot has as much room for 128 rows of 256 columns as for 256 of 128
-  return (size_t)sms * sizeof(int4) + 256 + (size_t)sms * 2 * (256 * 128 + 2 * 256) * sizeof(float);
+  return (size_t)sms * kFewPerSm * sizeof(int4) + 256 + (size_t)sms * 2 * (256 * 128 + 2 * 256) * sizeof(float);
 }
 
 cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int device, cudaStream_t stream) {

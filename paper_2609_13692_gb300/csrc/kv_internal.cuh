@@ -192,6 +192,7 @@ __device__ __forceinline__ int attn_block_of(const AttnRange& r, int64_t u) {
 }
 
 // Few query rows per KV head (k_attend_few.cu): bytes of workspace and launch.
+constexpr int kFewPerSm = 3;  // blocks per SM, at most
 size_t attend_few_workspace(int sms);
 cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, int device, cudaStream_t stream);
 // Flags of the kernels since the last call (waits for the stream).
