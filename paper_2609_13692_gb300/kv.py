@@ -33,15 +33,21 @@ _INT = torch.int32
 _CACHE = struct.Struct("@2P6q6iPqi2P")  # mpt_kv_cache
 _BOOK = struct.Struct("@Pq2i2P2i")      # mpt_kv_book
 _PAIR = struct.Struct("@2q")            # two strides
+_TWO = struct.Struct("@2P")             # two addresses
 
+_load = _mpt.load
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+_current_device = torch.cuda.current_device
+_empty, _U8, _F32 = torch.empty, torch.uint8, torch.float32
 
 
 def _run(index: int, stream: Optional[int], call, *args):
     """call(stream address, *args) with device `index` current and `stream` as torch's current
     stream there, so that what the call allocates belongs to it."""
-    if stream is None and index == torch.cuda.current_device():
+    if stream is None and index == _current_device():
         return call(_raw_stream(index), *args)
     with torch.cuda.device(index):
         if stream is None:
@@ -60,9 +66,18 @@ def _device(first, *others) -> int:
     return index
 
 
-def _ints(t, name: str, dims: int = 1):
-    if t.dtype is not _INT or t.dim() != dims or (t.stride(-1) != 1 and t.numel() > 0):
-        raise ValueError(f"{name} must be a {dims}-d int32 tensor with contiguous rows")
+def _ints(t, name: str):
+    if t.dtype is not _INT or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous 1-d int32 tensor")
+
+
+def _table(t, name: str):
+    """(rows, width, row stride) of a table of ints."""
+    shape, strides = t.shape, t.stride()
+    if t.dtype is not _INT or len(shape) != 2 or (strides[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-d int32 tensor with contiguous rows")
+    rows, width = shape
+    return rows, width, strides[0] if rows > 1 else max(width, 1)
 
 
 def _cache(k_pages, v_pages, page_table, q_offsets, kv_lens):
@@ -76,25 +91,27 @@ def _cache(k_pages, v_pages, page_table, q_offsets, kv_lens):
     vp, vs, vh, ve = v_pages.stride()
     if ke != 1 or ve != 1:
         raise ValueError("the elements of a head must be contiguous")
-    _ints(page_table, "page_table", 2)
+    batch, width, stride = _table(page_table, "page_table")
     _ints(q_offsets, "q_offsets")
     _ints(kv_lens, "kv_lens")
-    batch, width = page_table.shape
-    if q_offsets.shape[0] != batch + 1 or kv_lens.shape[0] != batch:
+    if len(q_offsets) != batch + 1 or len(kv_lens) != batch:
         raise ValueError("q_offsets needs batch + 1 entries, kv_lens batch")
     n_pages, page_size, kv_heads, dim = shape
-    stride = page_table.stride(0) if batch > 1 else max(width, 1)
     return _CACHE.pack(k_pages.data_ptr(), v_pages.data_ptr(), kp, ks, kh, vp, vs, vh, _TYPES[dtype], n_pages, page_size,
                        kv_heads, dim, batch, page_table.data_ptr(), stride, width, q_offsets.data_ptr(),
                        kv_lens.data_ptr()), dtype, kv_heads, dim
 
 
-def _strides(t) -> bytes:
-    return _PAIR.pack(t.stride(0), t.stride(1))
+def _heads_strides(t, name: str) -> bytes:
+    """The strides of a [tokens, heads, head_dim] tensor, the heads contiguous."""
+    a, b, c = t.stride()
+    if c != 1 and t.numel() > 0:
+        raise ValueError(f"{name} must have contiguous heads")
+    return _PAIR.pack(a, b)
 
 
 def _check_workspace(workspace, index: int):
-    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != index:
+    if workspace.dtype is not _U8 or not workspace.is_contiguous() or workspace.get_device() != index:
         raise ValueError("workspace must be a contiguous CUDA uint8 tensor on the same device")
 
 
@@ -104,7 +121,7 @@ _workspace_bytes: dict = {}
 def mpt_kv_attend_workspace_bytes(head_dim: int) -> int:
     """Bytes of workspace of :func:`mpt_kv_attend` on the current device."""
     out = ctypes.c_size_t()
-    _mpt._check(_mpt.load().mpt_kv_attend_workspace_bytes(int(head_dim), ctypes.byref(out)), "mpt_kv_attend_workspace_bytes")
+    _mpt._check(_load().mpt_kv_attend_workspace_bytes(int(head_dim), ctypes.byref(out)), "mpt_kv_attend_workspace_bytes")
     return int(out.value)
 
 
@@ -122,36 +139,41 @@ def mpt_kv_attend(q, k_pages, v_pages, page_table, q_offsets, kv_lens, *, max_q_
     index = _device(q, k_pages, v_pages, page_table, q_offsets, kv_lens)
     cache, dtype, _, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
     shape = q.shape
-    if len(shape) != 3 or q.dtype is not dtype or shape[2] != dim or (q.stride(2) != 1 and q.numel() > 0):
-        raise ValueError("q must be [tokens, heads, head_dim] of the cache's type with contiguous heads")
+    if len(shape) != 3 or q.dtype is not dtype or shape[2] != dim:
+        raise ValueError("q must be [tokens, heads, head_dim] of the cache's type")
+    strides = _heads_strides(q, "q")
     if out is not None:
         _device(q, out)
-        if out.shape != shape or out.dtype is not dtype or (out.stride(2) != 1 and out.numel() > 0):
-            raise ValueError("out must have q's shape and type, with contiguous heads")
+        if out.shape != shape or out.dtype is not dtype:
+            raise ValueError("out must have q's shape and type")
+        out = (out, _heads_strides(out, "out"))
     if lse is not None:
         _device(q, lse)
-        if lse.shape != shape[:2] or lse.dtype is not torch.float32 or not lse.is_contiguous():
+        if lse.shape != shape[:2] or lse.dtype is not _F32 or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous float32[tokens, heads]")
     if workspace is not None:
         _check_workspace(workspace, index)
-    return _run(index, stream, _attend, index, cache, q, int(max_q_len), 1 if causal else 0,
-                1.0 / math.sqrt(dim) if scale is None else float(scale), out, lse, workspace)
+    return _run(index, stream, _attend, index, cache, q, strides, shape, dtype, max_q_len, 1 if causal else 0,
+                1.0 / math.sqrt(dim) if scale is None else scale, out, lse, workspace)
 
 
-def _attend(s, index, cache, q, max_q_len, causal, scale, out, lse, workspace):
-    (tokens, heads, dim), device = q.shape, q.device
+def _attend(s, index, cache, q, strides, shape, dtype, max_q_len, causal, scale, out, lse, workspace):
+    (tokens, heads, dim), device = shape, q.device
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=device)
+        out, out_strides = _empty(shape, dtype=dtype, device=device), _PAIR.pack(heads * dim, dim)
+    else:
+        out, out_strides = out
     if lse is None:
-        lse = torch.empty((tokens, heads), dtype=torch.float32, device=device)
+        lse = _empty((tokens, heads), dtype=_F32, device=device)
     if workspace is None:
-        size = _workspace_bytes.get((index, dim))
+        size = _workspace_bytes.get(index)
         if size is None:
-            size = _workspace_bytes[index, dim] = mpt_kv_attend_workspace_bytes(dim)
-        workspace = torch.empty(size, dtype=torch.uint8, device=device)
-    status = _mpt.load().mpt_kv_attend(cache, q.data_ptr(), _strides(q), tokens, heads, max_q_len, causal, scale,
-                                       out.data_ptr(), _strides(out), lse.data_ptr(), workspace.data_ptr(),
-                                       workspace.numel(), s)
+            size = _workspace_bytes[index] = mpt_kv_attend_workspace_bytes(dim)
+        workspace = _empty(size, dtype=_U8, device=device)
+    else:
+        size = workspace.numel()
+    status = _load().mpt_kv_attend(cache, q.data_ptr(), strides, tokens, heads, max_q_len, causal, scale, out.data_ptr(),
+                                   out_strides, lse.data_ptr(), workspace.data_ptr(), size, s)
     if status:
         _mpt._check(status, "mpt_kv_attend")
     return out, lse
@@ -163,11 +185,12 @@ def mpt_kv_merge(outs, lses, *, out=None, lse=None, stream: Optional[int] = None
     outs: a sequence of [.., head_dim] tensors (or one tensor of them along its first axis), bf16,
     f16 or f32; lses: likewise, float32 [..].  Parts with lse = -inf have no part in a row."""
     n, po, shape, dtype, o = _parts(outs, "outs")
-    nl, pl, lshape, ldtype, z = _parts(lses, "lses")
-    if n != nl or lshape != shape[:-1] or ldtype is not torch.float32:
-        raise ValueError("lses must be as many float32 tensors as outs, of their shape without the last axis")
-    if dtype not in _TYPES or not shape:
+    nl, pl, rows, ldtype, z = _parts(lses, "lses")
+    kind = _TYPES.get(dtype)
+    if kind is None or not shape:
         raise ValueError("outs must be bfloat16, float16 or float32 with heads of a last axis")
+    if n != nl or rows != shape[:-1] or ldtype is not _F32:
+        raise ValueError("lses must be as many float32 tensors as outs, of their shape without the last axis")
     index = _device(o, z)
     if out is not None:
         _device(o, out)
@@ -175,9 +198,9 @@ def mpt_kv_merge(outs, lses, *, out=None, lse=None, stream: Optional[int] = None
             raise ValueError("out must be contiguous, of outs' shape and type")
     if lse is not None:
         _device(o, lse)
-        if lse.shape != lshape or lse.dtype is not torch.float32 or not lse.is_contiguous():
+        if lse.shape != rows or lse.dtype is not _F32 or not lse.is_contiguous():
             raise ValueError("lse must be contiguous float32 of lses' shape")
-    return _run(index, stream, _merge, n, po, pl, shape, dtype, o.device, out, lse)
+    return _run(index, stream, _merge, n, po, pl, shape, rows, dtype, kind, o.device, out, lse)
 
 
 def _addresses(at: list) -> bytes:
@@ -188,11 +211,10 @@ def _parts(parts, name: str):
     """(number, packed addresses, shape, type, a tensor) of equal contiguous parts."""
     if isinstance(parts, torch.Tensor):
         shape = parts.shape
-        n = shape[0] if len(shape) else 0
-        if n < 1 or not parts.is_contiguous():
+        if not shape or shape[0] < 1 or not parts.is_contiguous():
             raise ValueError(f"{name} must be contiguous parts, one at least")
-        at, step = parts.data_ptr(), parts.stride(0) * parts.element_size()
-        return n, _addresses([at + i * step for i in range(n)]), shape[1:], parts.dtype, parts
+        n, at, step = shape[0], parts.data_ptr(), parts.stride(0) * parts.element_size()
+        return n, _TWO.pack(at, at + step) if n == 2 else _addresses([at + i * step for i in range(n)]), shape[1:], parts.dtype, parts
     parts = list(parts)
     if not parts:
         raise ValueError(f"{name} must not be empty")
@@ -204,12 +226,12 @@ def _parts(parts, name: str):
     return n, _addresses([t.data_ptr() for t in parts]), first.shape, first.dtype, first
 
 
-def _merge(s, n, po, pl, shape, dtype, device, out, lse):
+def _merge(s, n, po, pl, shape, rows, dtype, kind, device, out, lse):
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
+        out = _empty(shape, dtype=dtype, device=device)
     if lse is None:
-        lse = torch.empty(shape[:-1], dtype=torch.float32, device=device)
-    status = _mpt.load().mpt_kv_merge(po, pl, n, lse.numel(), shape[-1], _TYPES[dtype], out.data_ptr(), lse.data_ptr(), s)
+        lse = _empty(rows, dtype=_F32, device=device)
+    status = _load().mpt_kv_merge(po, pl, n, lse.numel(), shape[-1], kind, out.data_ptr(), lse.data_ptr(), s)
     if status:
         _mpt._check(status, "mpt_kv_merge")
     return out, lse
@@ -220,15 +242,15 @@ def mpt_kv_write(k_new, v_new, k_pages, v_pages, page_table, q_offsets, kv_lens,
     their pages: the last q_offsets[i+1] - q_offsets[i] of request i's kv_lens[i] positions."""
     index = _device(k_pages, v_pages, page_table, q_offsets, kv_lens, k_new, v_new)
     cache, dtype, kv_heads, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
-    tokens = k_new.shape[0] if k_new.dim() else 0
-    for t in (k_new, v_new):
-        if t.shape != (tokens, kv_heads, dim) or t.dtype is not dtype or (t.stride(2) != 1 and t.numel() > 0):
-            raise ValueError("k_new and v_new must be [tokens, kv_heads, head_dim] of the cache's type with contiguous heads")
-    _run(index, stream, _write, cache, k_new, v_new, tokens)
+    shape = k_new.shape
+    if len(shape) != 3 or shape[1] != kv_heads or shape[2] != dim or v_new.shape != shape or k_new.dtype is not dtype or v_new.dtype is not dtype:
+        raise ValueError("k_new and v_new must be [tokens, kv_heads, head_dim] of the cache's type")
+    _run(index, stream, _write, cache, k_new.data_ptr(), _heads_strides(k_new, "k_new"), v_new.data_ptr(),
+         _heads_strides(v_new, "v_new"), shape[0])
 
 
-def _write(s, cache, k_new, v_new, tokens):
-    status = _mpt.load().mpt_kv_write(cache, k_new.data_ptr(), _strides(k_new), v_new.data_ptr(), _strides(v_new), tokens, s)
+def _write(s, *args):
+    status = _load().mpt_kv_write(*args, s)
     if status:
         _mpt._check(status, "mpt_kv_write")
 
@@ -240,26 +262,26 @@ def _write(s, cache, k_new, v_new, tokens):
 def _book(table, lens, refs, page_size: int, *lists):
     """The packed mpt_kv_book, the device, (rows, n_pages) and the length of the lists."""
     index = _device(table, lens, refs, *lists)
-    _ints(table, "table", 2)
+    rows, width, stride = _table(table, "table")
     _ints(lens, "lens")
     _ints(refs, "refs")
-    rows, width = table.shape
-    if lens.shape[0] != rows:
+    if len(lens) != rows:
         raise ValueError("lens needs one entry per table row")
-    n = lists[0].shape[0] if lists and lists[0].dim() else 0
+    n = None
     for t in lists:
         _ints(t, "a list of rows or lengths")
-        if t.shape[0] != n:
+        if n is None:
+            n = len(t)
+        elif len(t) != n:
             raise ValueError("the lists must be of one length")
-    n_pages = refs.shape[0]
-    stride = table.stride(0) if rows > 1 else max(width, 1)
+    n_pages = len(refs)
     return _BOOK.pack(table.data_ptr(), stride, width, rows, lens.data_ptr(), refs.data_ptr(), n_pages,
                       int(page_size)), index, rows, n_pages, n
 
 
 def _pages_workspace(workspace, index, rows, n_pages, device):
     if workspace is None:  # what mpt_kv_pages_workspace_bytes says: a header, one int per page and per row
-        return torch.empty(4 * (16 + n_pages + rows), dtype=torch.uint8, device=device)
+        return _empty(4 * (16 + n_pages + rows), dtype=_U8, device=device)
     _check_workspace(workspace, index)
     return workspace
 
@@ -268,7 +290,7 @@ def mpt_kv_pages_workspace_bytes(table, lens, refs, page_size: int) -> int:
     """Bytes of workspace of the bookkeeping calls."""
     book = _book(table, lens, refs, page_size)[0]
     out = ctypes.c_size_t()
-    _mpt._check(_mpt.load().mpt_kv_pages_workspace_bytes(book, ctypes.byref(out)), "mpt_kv_pages_workspace_bytes")
+    _mpt._check(_load().mpt_kv_pages_workspace_bytes(book, ctypes.byref(out)), "mpt_kv_pages_workspace_bytes")
     return int(out.value)
 
 
@@ -281,10 +303,10 @@ def mpt_kv_fork(table, lens, refs, page_size: int, src, dst, keep, *, workspace=
 
 
 def _fork(s, book, index, rows, n_pages, n, device, src, dst, keep, workspace):
-    old, fresh = torch.empty(n, dtype=_INT, device=device), torch.empty(n, dtype=_INT, device=device)
-    status = torch.empty(2, dtype=_INT, device=device)
+    old, fresh = _empty(n, dtype=_INT, device=device), _empty(n, dtype=_INT, device=device)
+    status = _empty(2, dtype=_INT, device=device)
     ws = _pages_workspace(workspace, index, rows, n_pages, device)
-    st = _mpt.load().mpt_kv_fork(book, src.data_ptr(), dst.data_ptr(), keep.data_ptr(), n, old.data_ptr(), fresh.data_ptr(),
+    st = _load().mpt_kv_fork(book, src.data_ptr(), dst.data_ptr(), keep.data_ptr(), n, old.data_ptr(), fresh.data_ptr(),
                                  status.data_ptr(), ws.data_ptr(), ws.numel(), s)
     if st:
         _mpt._check(st, "mpt_kv_fork")
@@ -298,9 +320,9 @@ def mpt_kv_extend(table, lens, refs, page_size: int, rows, more, *, workspace=No
 
 
 def _extend(s, book, index, n_rows, n_pages, n, device, rows, more, workspace):
-    status = torch.empty(2, dtype=_INT, device=device)
+    status = _empty(2, dtype=_INT, device=device)
     ws = _pages_workspace(workspace, index, n_rows, n_pages, device)
-    st = _mpt.load().mpt_kv_extend(book, rows.data_ptr(), more.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    st = _load().mpt_kv_extend(book, rows.data_ptr(), more.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
     if st:
         _mpt._check(st, "mpt_kv_extend")
     return status
@@ -313,9 +335,9 @@ def mpt_kv_free(table, lens, refs, page_size: int, rows, *, workspace=None, stre
 
 
 def _free(s, book, index, n_rows, n_pages, n, device, rows, workspace):
-    status = torch.empty(2, dtype=_INT, device=device)
+    status = _empty(2, dtype=_INT, device=device)
     ws = _pages_workspace(workspace, index, n_rows, n_pages, device)
-    st = _mpt.load().mpt_kv_free(book, rows.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    st = _load().mpt_kv_free(book, rows.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
     if st:
         _mpt._check(st, "mpt_kv_free")
     return status
@@ -330,10 +352,10 @@ def mpt_kv_compact(table, lens, refs, page_size: int, *, workspace=None, stream:
 
 def _compact(s, book, index, rows, n_pages, _, device, workspace):
     n = n_pages // 2
-    old, fresh = torch.empty(n, dtype=_INT, device=device), torch.empty(n, dtype=_INT, device=device)
-    status = torch.empty(2, dtype=_INT, device=device)
+    old, fresh = _empty(n, dtype=_INT, device=device), _empty(n, dtype=_INT, device=device)
+    status = _empty(2, dtype=_INT, device=device)
     ws = _pages_workspace(workspace, index, rows, n_pages, device)
-    st = _mpt.load().mpt_kv_compact(book, old.data_ptr(), fresh.data_ptr(), status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    st = _load().mpt_kv_compact(book, old.data_ptr(), fresh.data_ptr(), status.data_ptr(), ws.data_ptr(), ws.numel(), s)
     if st:
         _mpt._check(st, "mpt_kv_compact")
     return old, fresh, status
@@ -361,7 +383,7 @@ def mpt_kv_copy_pages(pool, src, dst, *, stream: Optional[int] = None) -> None:
 
 
 def _copy_pages(s, pool, planes, plane_stride, n_pages, page_stride, page_bytes, src, dst):
-    st = _mpt.load().mpt_kv_copy_pages(pool.data_ptr(), planes, plane_stride, n_pages, page_stride, page_bytes, src.data_ptr(),
+    st = _load().mpt_kv_copy_pages(pool.data_ptr(), planes, plane_stride, n_pages, page_stride, page_bytes, src.data_ptr(),
                                        dst.data_ptr(), src.shape[0], s)
     if st:
         _mpt._check(st, "mpt_kv_copy_pages")
@@ -370,4 +392,4 @@ def _copy_pages(s, pool, planes, plane_stride, n_pages, page_stride, page_bytes,
 def mpt_kv_check(stream: Optional[int] = None) -> None:
     """Waits for the stream and raises if a kernel of this module gave up a bounded wait since the last check."""
     s = _mpt._default_stream_ptr() if stream is None else int(stream)
-    _mpt._check(_mpt.load().mpt_kv_check(s), "mpt_kv_check")
+    _mpt._check(_load().mpt_kv_check(s), "mpt_kv_check")
