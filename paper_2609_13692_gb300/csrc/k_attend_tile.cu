@@ -242,26 +242,10 @@ __device__ __forceinline__ uint32_t not_finite8(const uint4& x) {
   return (((x.x & e) + one) | ((x.y & e) + one) | ((x.z & e) + one) | ((x.w & e) + one)) & 0x80008000u;
 }
 
-// Transposes the 4 x 4 pieces of every four lanes.
-__device__ __forceinline__ void swap_with(uint4& x, int lane_mask) {
-  x.x = __shfl_xor_sync(~0u, x.x, lane_mask);
-  x.y = __shfl_xor_sync(~0u, x.y, lane_mask);
-  x.z = __shfl_xor_sync(~0u, x.z, lane_mask);
-  x.w = __shfl_xor_sync(~0u, x.w, lane_mask);
-}
-__device__ __forceinline__ void turn4(uint4* v, int lane) {
-#pragma unroll
-  for (int d = 1; d <= 2; d <<= 1)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (e & d) continue;
-      // the lane without bit d gives v[e | d] for the other's v[e]
-      const bool up = lane & d;
-      uint4 give = up ? v[e] : v[e | d];
-      swap_with(give, d);
-      if (up) v[e] = give;
-      else v[e | d] = give;
-    }
+__device__ __forceinline__ void store32(void* to, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+               "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
 
 // Items in their natural order: the requests, the KV heads of each, the pairs of
@@ -973,10 +957,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         const bool extra = odd && w.count(s) > 0 && odd[8];
         const float inv = l == 0.f ? 0.f : 1.f / l, scale = whole ? inv : 1.f;
         const int64_t tok_at = (int64_t)w.e.q0 + tok, head = (int64_t)w.e.head * p.group + sub;
-        char* const out = valid ? p.out + 2 * (tok_at * p.out_tok + head * p.out_head) : nullptr;
-        char* rows4[4];  // of the four lanes of a group
-#pragma unroll
-        for (int e = 0; e < 4; ++e) rows4[e] = (char*)__shfl_sync(~0u, (uint64_t)out, lane & ~3 | e);
+        char* const out = p.out + 2 * (tok_at * p.out_tok + head * p.out_head);
         float* part = p.part + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * (C::kRows * HDP + 2 * C::kRows);
         for (int c = 0; c < HDP / 32; ++c) {
           float o[32];
@@ -1014,21 +995,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             }
           }
           if (whole) {
-            // Four lanes hand 16-byte pieces round so that each store of a warp
-            // writes 64 contiguous bytes of eight rows instead of 16 of 32.
-            uint4 v[4];
+            uint32_t v[16];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              v[e].x = pack2<F16>(o[8 * e] * scale, o[8 * e + 1] * scale);
-              v[e].y = pack2<F16>(o[8 * e + 2] * scale, o[8 * e + 3] * scale);
-              v[e].z = pack2<F16>(o[8 * e + 4] * scale, o[8 * e + 5] * scale);
-              v[e].w = pack2<F16>(o[8 * e + 6] * scale, o[8 * e + 7] * scale);
+            for (int e = 0; e < 16; ++e) v[e] = pack2<F16>(o[2 * e] * scale, o[2 * e + 1] * scale);
+            if (valid && p.wide) {  // whole 32-byte sectors
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (32 * c + 16 * e < p.dim) store32(out + 2 * (32 * c + 16 * e), v + 8 * e);
+            } else if (valid) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (32 * c + 8 * e < p.dim)
+                  *(uint4*)(out + 2 * (32 * c + 8 * e)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
             }
-            turn4(v, lane);
-            const int col = 32 * c + 8 * (lane & 3);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (col < p.dim && rows4[e]) *(uint4*)(rows4[e] + 2 * col) = v[e];
           } else {
             // [column / 4][row][4]: a warp's 32 rows are 512 contiguous bytes
 #pragma unroll

@@ -28,6 +28,7 @@ struct alignas(128) AttnParams {
   int64_t tokens;
   int32_t width, n_pages, page_log2, batch, heads, kv_heads, group, dim, causal;
   int32_t box, toks, item_toks;  // page slots per copy; whole tokens of 128 rows, and of an item
+  int32_t wide;                  // out's heads are whole 32-byte pieces
   float scale_log2;  // scale * log2(e)
 };
 

@@ -151,6 +151,7 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* c, const void* q, const int64_t* q_
   p.dim = c->head_dim;
   p.toks = 128 / p.group;
   p.item_toks = p.toks * (p.dim > 128 ? 1 : 2);
+  p.wide = p.dim % 16 == 0 && mpt::aligned(out, 32) && (heads == 1 || p.out_head % 16 == 0) && (tokens == 1 || p.out_tok % 16 == 0);
   p.causal = causal != 0;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t stream = (cudaStream_t)stream_ptr;
