@@ -122,6 +122,28 @@ __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parit
 
 __device__ __forceinline__ void bar_all() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
 
+// The same for warp 11, which has time: its polls take issue slots that the rows'
+// arithmetic needs (4,096 tokens over 20,480 keys: 797 us with its polls back to
+// back, 770 with 20 to 400 ns between them; the copying warps' polls matter less,
+// the others' waits are on the chain and any longer sleep costs).
+__device__ __forceinline__ bool wait_seldom(unsigned long long* bar, uint32_t parity, int* gave_up) {
+  unsigned long long start = 0;
+  for (int n = 1;; ++n) {
+    if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
+    __nanosleep(100);
+    if (n % 256 != 0) continue;
+    const unsigned long long now = now_ns();
+    if (start == 0) start = now;
+    bool over = *(volatile int*)gave_up != 0;
+    if (now - start > 4000000000ull) {
+      over = true;
+      *(volatile int*)gave_up = 1;
+      atomicOr(&g_tile_flags, kErrTimeout);
+    }
+    if (__any_sync(~0u, over)) return false;
+  }
+}
+
 // The first lane's value in every lane, which the compiler then knows to be uniform.
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(~0u, v, 0); }
 
@@ -776,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         for (int j = 0; j < w.tiles && ok; ++j, idx += 2) {
           const uint32_t vi = idx + 1, ki = idx + 2;
           const int s = vi % C::kSlots;
-          ok = wait_all(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
+          ok = wait_seldom(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
           if (!ok) break;
           if (w.partly(j)) {
             const uint32_t at = smem_u32(ring + s * C::kSlot);
@@ -817,12 +839,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
           }
-          if (C::kWatchKeys && j + 1 < w.tiles) ok = wait_all(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
+          if (C::kWatchKeys && j + 1 < w.tiles) ok = wait_seldom(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
           if (!ok) break;
           // not a tile ahead of the rows, or two arrivals would count in one phase
           constexpr int kSecond = C::kTiles == 1 ? 2 : 1;
-          if (due & 1) ok = wait_all(&sh.p_ready[0], ready & 1, gave_up);
-          if (ok && (due & 2)) ok = wait_all(&sh.p_ready[kSecond], ready >> 1, gave_up);
+          if (due & 1) ok = wait_seldom(&sh.p_ready[0], ready & 1, gave_up);
+          if (ok && (due & 2)) ok = wait_seldom(&sh.p_ready[kSecond], ready >> 1, gave_up);
           if (!ok) break;
           ready ^= due;
           due = C::kTiles == 1 ? 1 + (j & 1) : (j < w.n0 ? 1 : 0) | (j < w.n1 ? 2 : 0);
