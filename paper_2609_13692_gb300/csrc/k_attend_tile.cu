@@ -122,15 +122,17 @@ __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parit
 
 __device__ __forceinline__ void bar_all() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
 
-// The same for warp 11, which has time: its polls take issue slots that the rows'
-// arithmetic needs (4,096 tokens over 20,480 keys: 797 us with its polls back to
-// back, 770 with 20 to 400 ns between them; the copying warps' polls matter less,
-// the others' waits are on the chain and any longer sleep costs).
-__device__ __forceinline__ bool wait_seldom(unsigned long long* bar, uint32_t parity, int* gave_up) {
+// The same for the warps that have time: polls take issue slots that the rows'
+// arithmetic needs.  (4,096 tokens over 20,480 keys: 797 us with warp 11's polls
+// back to back, 770 with 20 to 400 ns between them; 20 ns between the copying
+// warps' polls for free slots: heads of 64 149 -> 141 us, the rest 0 to 1 %.  The
+// others' waits are on the chain, and any longer sleep costs.)
+template <int kNs>
+__device__ __forceinline__ bool wait_spaced(unsigned long long* bar, uint32_t parity, int* gave_up) {
   unsigned long long start = 0;
   for (int n = 1;; ++n) {
     if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
-    __nanosleep(100);
+    __nanosleep(kNs);
     if (n % 256 != 0) continue;
     const unsigned long long now = now_ns();
     if (start == 0) start = now;
@@ -600,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           next = page_of(j + 1);
           const uint32_t idx = 2 * gt + v;
           const int s = idx % C::kSlots;
-          if (idx >= C::kSlots) ok = ok && wait_all(&sh.empty[s], (idx / C::kSlots - 1) & 1, gave_up);
+          if (idx >= C::kSlots) ok = ok && wait_spaced<20>(&sh.empty[s], (idx / C::kSlots - 1) & 1, gave_up);
           if (!ok) break;
           const unsigned held = __ballot_sync(~0u, id >= 0);
           if (lane == 0) {
@@ -798,7 +800,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         for (int j = 0; j < w.tiles && ok; ++j, idx += 2) {
           const uint32_t vi = idx + 1, ki = idx + 2;
           const int s = vi % C::kSlots;
-          ok = wait_seldom(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
+          ok = wait_spaced<100>(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
           if (!ok) break;
           if (w.partly(j)) {
             const uint32_t at = smem_u32(ring + s * C::kSlot);
@@ -839,12 +841,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
           }
-          if (C::kWatchKeys && j + 1 < w.tiles) ok = wait_seldom(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
+          if (C::kWatchKeys && j + 1 < w.tiles) ok = wait_spaced<100>(&sh.full[ki % C::kSlots], (ki / C::kSlots) & 1, gave_up);
           if (!ok) break;
           // not a tile ahead of the rows, or two arrivals would count in one phase
           constexpr int kSecond = C::kTiles == 1 ? 2 : 1;
-          if (due & 1) ok = wait_seldom(&sh.p_ready[0], ready & 1, gave_up);
-          if (ok && (due & 2)) ok = wait_seldom(&sh.p_ready[kSecond], ready >> 1, gave_up);
+          if (due & 1) ok = wait_spaced<100>(&sh.p_ready[0], ready & 1, gave_up);
+          if (ok && (due & 2)) ok = wait_spaced<100>(&sh.p_ready[kSecond], ready >> 1, gave_up);
           if (!ok) break;
           ready ^= due;
           due = C::kTiles == 1 ? 1 + (j & 1) : (j < w.n0 ? 1 : 0) | (j < w.n1 ? 2 : 0);
