@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             if (elect_one()) {
               outputs(0, j & 1 ? 128 : 0, sv, j > 0);
               commit(&sh.empty[sv]);
-              commit(&sh.o_step);
+              if (j + 2 == tiles) commit(&sh.o_step);
               if (j + 1 == tiles) commit(&sh.o_full[0]);
             }
             __syncwarp();
@@ -882,6 +882,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         const uint32_t t_p = second ? t_s + 128 : t_s;
         ok = wait_all(&sh.s_full[buf], second ? scored >> 1 : scored & 1, gave_up);
         scored ^= second ? 2 : 1;
+        if (C::kTiles == 1 && ok && j > 0 && j + 1 == w.n0) {  // no scores follow: the outputs before the last tile
+          ok = wait_all(&sh.o_step, steps & 1, gave_up);
+          ++steps;
+        }
         if (!ok) break;
         fence_after();
         float f[128];
@@ -916,8 +920,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         if (j == 0) {
           m = top;
         } else if (__any_sync(~0u, top - m > 8.f)) {
-          if (C::kTiles == 1) {  // these scores did not wait for the outputs before them, which come in order
-            ok = wait_all(&sh.o_step, (steps + j - 1) & 1, gave_up);
+          if (C::kTiles == 1 && j + 1 < w.n0) {
+            // These scores did not wait for the outputs of the tile before; the
+            // next ones, issued after those outputs, do.
+            ok = wait_all(&sh.s_full[second ? 0 : 2], (second ? scored : scored >> 1) & 1, gave_up);
             if (!ok) break;
             fence_after();
           }
@@ -965,7 +971,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       }
       if (!ok) break;
       gt += w.tiles;
-      if (C::kTiles == 1) steps += w.n0;
       const uint32_t* odd = nullptr;
       if (w.tiles > 0) odd = sh.odd[item++ % kOddSets];
       if (w.count(s) > 0) {

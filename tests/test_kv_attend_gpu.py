@@ -216,6 +216,28 @@ def test_long_keys(kv, q_len, heads):
     check(kv, make(16, [q_len, 0, q_len], [9_000, 12, 5_003], heads, 1, 64, 64, F16, poison=True), False)
 
 
+@pytest.mark.parametrize("q_len", [1, 33])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 256), (6, 2, 96), (3, 3, 200)])
+def test_long_keys_of_other_heads(kv, heads, kv_heads, dim, q_len):
+    """Many turns of the rings of copies, with requests of other lengths beside."""
+    c = make(23, [q_len, 1, q_len], [12_345, 700, 4_100], heads, kv_heads, dim, 16, BF16, poison=True)
+    check(kv, c, hint=q_len)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scores_that_grow_along_the_keys(kv, dim, causal):
+    """The running maximum is outgrown in tile after tile, the last among them."""
+    for q_lens, kv_lens in (([1, 3], [1_500, 640]), ([150, 40, 300], [1_500, 641, 300])):
+        c = make(24, q_lens, kv_lens, 4, 2, dim, 16, BF16)
+        lead = torch.randn(dim, device="cuda").to(BF16)
+        c["q"].copy_(lead.expand_as(c["q"]) * (1 + 0.1 * torch.rand(c["q"].shape[:2], device="cuda"))[..., None])
+        for i, n in enumerate(kv_lens):
+            j = torch.arange(n, device="cuda")
+            c["k"][c["table"][i].long()[j // 16], j % 16] += ((j // 100).float() * 0.2)[:, None, None].to(BF16) * lead
+        check(kv, c, causal, hint=max(q_lens))
+
+
 def test_offsets_beyond_32_bits(kv):
     """Pages whose elements lie past 2^31 and 2^32."""
     n_pages, page, kv_heads, dim = 70_000, 64, 8, 128
