@@ -131,10 +131,9 @@ mpt_status mpt_kv_write(const mpt_kv_cache* cache, const void* k_new, const int6
  *     listed twice, a fork onto a row that holds tokens, keep or a length out
  *     of range) + MPT_KV_NO_PAGES (too few free pages) + MPT_KV_ROW_FULL (a
  *     row would need more than `width` pages); [1] the free pages left.
- *   workspace: device, 16-byte aligned, at least mpt_kv_pages_workspace_bytes.
- * Limits: rows <= 2^20, list length n <= rows, n_pages < 2^30,
+ * Limits: rows <= 2^20, list length n <= min(rows, 16384), n_pages < 2^30,
  * width * page_size < 2^31.
- * Errors of each: INVALID_ARG, TOO_LARGE, WORKSPACE_TOO_SMALL, CUDA.
+ * Errors of each: INVALID_ARG, TOO_LARGE, CUDA.
  * ------------------------------------------------------------------------- */
 #define MPT_KV_BAD_ROW 1
 #define MPT_KV_NO_PAGES 2
@@ -151,33 +150,29 @@ typedef struct mpt_kv_book {
   int32_t page_size; /* power of two, 8 to 256 */
 } mpt_kv_book;
 
-mpt_status mpt_kv_pages_workspace_bytes(const mpt_kv_book* book, size_t* bytes);
-
 /* Fork: row dst[j] (empty) gets the first keep[j] tokens of row src[j].  Its
  * full pages are shared (one more reference each); a part page is copied to a
  * fresh page, which the caller's copy_src[j] -> copy_dst[j] names (-1, -1
  * where there is none) for mpt_kv_copy_pages.  src may repeat, dst may not.
  *   src, dst, keep, copy_src, copy_dst: device int32[n]. */
 mpt_status mpt_kv_fork(const mpt_kv_book* book, const int32_t* src, const int32_t* dst, const int32_t* keep,
-                       int32_t n, int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* workspace,
-                       size_t workspace_bytes, void* stream);
+                       int32_t n, int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* stream);
 
 /* Extend: row rows[j] grows by more[j] >= 0 tokens, onto fresh pages where its
  * last page is full.  No row twice.  device int32[n] each. */
 mpt_status mpt_kv_extend(const mpt_kv_book* book, const int32_t* rows, const int32_t* more, int32_t n,
-                         int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+                         int32_t* status, void* stream);
 
 /* Free: the pages of row rows[j] lose one reference each, the row is emptied
  * (length 0, entries -1).  No row twice. */
-mpt_status mpt_kv_free(const mpt_kv_book* book, const int32_t* rows, int32_t n, int32_t* status, void* workspace,
-                       size_t workspace_bytes, void* stream);
+mpt_status mpt_kv_free(const mpt_kv_book* book, const int32_t* rows, int32_t n, int32_t* status, void* stream);
 
 /* Compact: with n live pages (references > 0), the i-th live page of id >= n
  * moves to the i-th free page of id < n; reference counts and table entries
  * follow.  copy_src / copy_dst (device int32[n_pages / 2]) get the moves for
  * mpt_kv_copy_pages, then -1. */
 mpt_status mpt_kv_compact(const mpt_kv_book* book, int32_t* copy_src, int32_t* copy_dst, int32_t* status,
-                          void* workspace, size_t workspace_bytes, void* stream);
+                          void* stream);
 
 /* Copy whole pages within a pool, src[j] -> dst[j] (device int32[n]) in every
  * plane (a layer's pages; `planes` of them, plane_stride bytes apart; pages

@@ -223,9 +223,9 @@ __global__ void __launch_bounds__(kCopyThreads) k_kv_copy_pages(const __grid_con
 // before it (a prefix over the cluster's warps, read from the other blocks'
 // shared memory) plus its own ballots.  The counts are whole, so the ranks and
 // everything that follows do not depend on the order of anything.
-// Bound: launch, cluster barriers and dependent reads; 7 to 9 us with 4,096
-// pages, 12 to 21 us with 200,000.  One, two or four blocks are no faster with
-// 4,096 pages and take 35, 24 and 18 us for a fork with 65,536 (eight: 12).
+// Bound: launch, cluster barriers and dependent reads; 7 to 10 us with 4,096
+// pages, 13 to 23 us with 200,000.  One, two or four blocks are no faster with
+// 4,096 pages and take 35, 24 and 18 us for a fork with 65,536 (eight: 13).
 // ---------------------------------------------------------------------------
 
 constexpr int kCluster = 8, kBookThreads = 1024, kBookWarps = kBookThreads / 32;
@@ -303,15 +303,14 @@ __device__ __forceinline__ bool mark(uint32_t* marks, int r) { return atomicOr(&
 
 template <int OP>
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads) k_kv_book(const __grid_constant__ BookParams p) {
-  extern __shared__ uint32_t marks[];
+  extern __shared__ uint32_t marks[];  // a bit per row, then the first fresh page of each entry
   __shared__ BookShared sh;
   cg::cluster_group cl = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)cl.block_rank(), gw = rank * kBookWarps + warp;
   const mpt_kv_book& b = p.b;
   const int mask = (1 << p.page_log2) - 1;
-  int32_t* fresh = p.ws + kBookHeader;
-  int32_t* ranks = fresh + b.n_pages;
+  int* const ranks = (int*)(marks + (b.rows + 31) / 32);
   const Scan run = my_run(b.n_pages, gw);
   auto is_page = [&](int id) { return id >= 0 && id < b.n_pages; };
   const int64_t room = (int64_t)b.width << p.page_log2;  // tokens of a full row
@@ -373,77 +372,90 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   int flags = lead->flags;
   if (need > free_all) flags |= MPT_KV_NO_PAGES;
   if (OP == kBookFree) flags &= ~MPT_KV_NO_PAGES;
-  if (flags == 0 && OP != kBookFree) {
+  // A warp hands its free pages out: the r-th belongs to the last entry whose
+  // pages begin at or before r.  Eight pages a lane at a time: the warps of the
+  // lowest ids do it all, one after another's reads (a fork of 300 rows with
+  // 65,536 pages 19 us one by one).
+  if (flags == 0 && OP != kBookFree && __syncthreads_or(before < need)) {
+    if (rank != 0) {
+      const int* theirs = cl.map_shared_rank(ranks, 0);
+      for (int i = tid; i < p.n; i += kBookThreads) ranks[i] = theirs[i];
+      __syncthreads();
+    }
     int at = before;
     for (int id0 = run.lo; id0 < run.hi && at < need; id0 += 256) {
-      unsigned f[8];  // eight loads at a time
+      int r[8], j[8], x[8], y[8];  // rank (-1: not to give), entry
 #pragma unroll
-      for (int u = 0; u < 8; ++u) f[u] = __ballot_sync(~0u, id0 + 32 * u + lane < run.hi && b.refs[id0 + 32 * u + lane] <= 0);
+      for (int u = 0; u < 8; ++u) x[u] = id0 + 32 * u + lane < run.hi ? b.refs[id0 + 32 * u + lane] : 1;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int r = at + __popc(f[u] & ((1u << lane) - 1u));
-        if ((f[u] >> lane & 1u) && r < need) fresh[r] = id0 + 32 * u + lane;
-        at += __popc(f[u]);
+        const unsigned f = __ballot_sync(~0u, x[u] <= 0);
+        r[u] = at + __popc(f & ((1u << lane) - 1u));
+        if (x[u] > 0 || r[u] >= need) r[u] = -1;
+        at += __popc(f);
+        j[u] = 0;
+      }
+      for (int step = 1 << (31 - __clz(p.n)); step; step >>= 1) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (j[u] + step < p.n && ranks[j[u] + step] <= r[u]) j[u] += step;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        x[u] = OP == kBookFork ? p.l1[j[u]] : p.l0[j[u]];
+        if (OP == kBookFork) y[u] = p.l2[j[u]] >> p.page_log2;
+      }
+      if (OP == kBookExtend) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) y[u] = (int)(((int64_t)b.lens[x[u]] + mask) >> p.page_log2) + r[u] - ranks[j[u]];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (r[u] < 0) continue;
+        const int id = id0 + 32 * u + lane;
+        b.table[(int64_t)x[u] * b.table_stride + y[u]] = id;
+        b.refs[id] = 1;
+        if (OP == kBookFork) p.copy_dst[j[u]] = id;
       }
     }
   }
-  cl.sync();  // the fresh pages are known; nobody reads the first block's shared memory any more
-  if (flags == 0) {
-    for (int j = gw; j < p.n; j += kScanWarps) {
-      if (OP == kBookFork) {
-        const int src = p.l0[j], dst = p.l1[j], keep = p.l2[j];
-        const int32_t* from = b.table + (int64_t)src * b.table_stride;
-        int32_t* to = b.table + (int64_t)dst * b.table_stride;
-        const int full = keep >> p.page_log2;
-        for (int i = lane; i < b.width; i += 32) {
-          int id = -1, old = -1;
-          if (i < full) {
-            id = from[i];
-            if (is_page(id)) atomicAdd(&b.refs[id], 1);
-            else id = -1;
-          } else if (i == full && (keep & mask)) {
-            old = from[i];
-            if (is_page(old)) {
-              id = fresh[ranks[j]];
-              b.refs[id] = 1;
-            }
-          }
-          to[i] = id;
-          if (i == full || (full == b.width && i == b.width - 1)) {
-            const bool copy = i == full && id >= 0;
-            p.copy_src[j] = copy ? old : -1;
-            p.copy_dst[j] = copy ? id : -1;
-          }
+  if (OP == kBookFork) cl.sync();  // counts are read above: a row may name a page whose count is 0
+  if (flags == 0 && OP != kBookExtend) {
+    for (int j = kScanWarps - 1 - gw; j < p.n; j += kScanWarps) {  // the last warps have no pages to hand out
+      const int row = OP == kBookFork ? p.l1[j] : p.l0[j], keep = OP == kBookFork ? p.l2[j] : b.lens[row];
+      int32_t* to = b.table + (int64_t)row * b.table_stride;
+      const int32_t* from = OP == kBookFork ? b.table + (int64_t)p.l0[j] * b.table_stride : to;
+      // Fork: the full pages, beside which entry `have` is written above if the rest is on a page.
+      const int have = OP == kBookFork ? keep >> p.page_log2 : (int)(((int64_t)keep + mask) >> p.page_log2);
+      const int part = OP == kBookFork && (keep & mask) != 0 ? from[have] : -1;
+      for (int i0 = 0; i0 < b.width; i0 += 256) {
+        int id[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) id[u] = i0 + 32 * u + lane < have ? from[i0 + 32 * u + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int i = i0 + 32 * u + lane;
+          if (is_page(id[u])) atomicAdd(&b.refs[id[u]], OP == kBookFork ? 1 : -1);
+          else id[u] = -1;
+          if (i < b.width && !(i == have && is_page(part))) to[i] = OP == kBookFork ? id[u] : -1;
         }
-        if (lane == 0) b.lens[dst] = keep;
-      } else {
-        const int row = p.l0[j], len = b.lens[row];
-        int32_t* to = b.table + (int64_t)row * b.table_stride;
-        const int have = (int)(((int64_t)len + mask) >> p.page_log2);
-        if (OP == kBookExtend) {
-          const int more = p.l1[j], want = (int)(((int64_t)len + more + mask) >> p.page_log2), first = ranks[j];
-          for (int i = have + lane; i < want; i += 32) {
-            const int id = fresh[first + i - have];
-            to[i] = id;
-            b.refs[id] = 1;
-          }
-          __syncwarp();
-          if (lane == 0) b.lens[row] = len + more;
-        } else {
-          for (int i = lane; i < b.width; i += 32) {
-            if (i < have && is_page(to[i])) atomicSub(&b.refs[to[i]], 1);
-            to[i] = -1;
-          }
-          __syncwarp();
-          if (lane == 0) b.lens[row] = 0;
+      }
+      __syncwarp();
+      if (lane == 0) {
+        b.lens[row] = OP == kBookFork ? keep : 0;
+        if (OP == kBookFork) {
+          p.copy_src[j] = is_page(part) ? part : -1;
+          if (!is_page(part)) p.copy_dst[j] = -1;
         }
       }
     }
   } else if (OP == kBookFork) {
     for (int j = gw * 32 + lane; j < p.n; j += kScanWarps * 32) p.copy_src[j] = p.copy_dst[j] = -1;
   }
+  cl.sync();  // nobody reads the first block's shared memory, or a row's old length, any more
+  if (OP == kBookExtend && flags == 0)
+    for (int j = gw * 32 + lane; j < p.n; j += kScanWarps * 32) b.lens[p.l0[j]] += p.l1[j];
   if (OP == kBookFree) {  // the pages that this call freed are counted too
-    cl.sync();
     int n = 0, all;
 #pragma unroll 8
     for (int at = run.lo; at < run.hi; at += 32) n += __popc(__ballot_sync(~0u, at + lane < run.hi && b.refs[at + lane] <= 0));
@@ -465,7 +477,6 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)cl.block_rank(), gw = rank * kBookWarps + warp, all_threads = kCluster * kBookThreads;
   const mpt_kv_book& b = p.b;
-  int32_t* to = p.ws + kBookHeader;
   int per;
   const Scan run = my_run(b.n_pages, gw, &per);
   int live = 0, n_live;
@@ -499,7 +510,6 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
       const int ahead = before + __popc(f[u] & ((1u << lane) - 1u));  // live pages of a lower id
       if (in && !on && id < n_live) p.copy_dst[id - ahead] = id;
       if (on && id >= n_live) p.copy_src[ahead - stay] = id;
-      if (in && !on && id >= n_live) to[id] = id;
       before += __popc(f[u]);
     }
   }
@@ -507,33 +517,38 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   cl.sync();
   for (int k = rank * kBookThreads + tid; k < moves; k += all_threads) {
     const int s = p.copy_src[k], d = p.copy_dst[k];
-    to[s] = d;
     b.refs[d] = b.refs[s];
     b.refs[s] = 0;
   }
   if (gw == 0 && lane == 0) {
-    p.ws[0] = n_live;
     p.status[0] = 0;
     p.status[1] = b.n_pages - n_live;
   }
 }
 
-// Table entries of moved pages (id >= the number of live ones).
+// Table entries of moved pages (id >= the number of live ones): the moves are in
+// rising order of the old id, then -1.
 __global__ void __launch_bounds__(256) k_kv_remap(const __grid_constant__ BookParams p) {
   wait_for_primary();
-  const int n_live = p.ws[0];
-  const int32_t* to = p.ws + kBookHeader;
+  const int n_live = p.b.n_pages - p.status[1], half = p.b.n_pages / 2;
   for (int row = blockIdx.y; row < p.b.rows; row += gridDim.y)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.b.width; i += (int64_t)gridDim.x * 256) {
       int32_t* at = p.b.table + (int64_t)row * p.b.table_stride + i;
       const int id = *at;
-      if (id >= n_live && id < p.b.n_pages) *at = to[id];
+      if (id < n_live || id >= p.b.n_pages) continue;
+      int lo = 0, hi = half;  // the first move of an old id of at least `id`
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2, old = p.copy_src[mid];
+        if (old >= 0 && old < id) lo = mid + 1;
+        else hi = mid;
+      }
+      if (lo < half && p.copy_src[lo] == id) *at = p.copy_dst[lo];
     }
 }
 
 template <int OP>
 cudaError_t book(const BookParams& p, cudaStream_t stream) {
-  const size_t smem = (size_t)(p.b.rows + 31) / 32 * 4;
+  const size_t smem = (size_t)(p.b.rows + 31) / 32 * 4 + (OP == kBookFree ? 0 : (size_t)p.n * 4);
   cudaError_t e = cudaSuccess;
   if (smem > 40 * 1024) e = cudaFuncSetAttribute(k_kv_book<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;

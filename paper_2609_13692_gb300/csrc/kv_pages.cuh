@@ -44,9 +44,8 @@ struct BookParams {
   int32_t page_log2, n;
   const int32_t *l0, *l1, *l2;  // fork: src, dst, keep; extend: rows, more; free: rows
   int32_t *copy_src, *copy_dst, *status;
-  int32_t* ws;  // [kBookHeader], then [n_pages] (fresh pages, or where each page went), then [rows] (ranks)
 };
-constexpr int kBookHeader = 16;
+constexpr int kBookList = 16384;  // entries of a list, at most: 4 bytes of shared memory each, beside a bit per row
 enum BookOp { kBookFork, kBookExtend, kBookFree, kBookCompact };
 cudaError_t launch_kv_book(const BookParams& p, BookOp op, cudaStream_t stream);
 

@@ -229,15 +229,13 @@ mpt_status check_book(const mpt_kv_book* b, int32_t n, int* log2) {
       !page_log2(b->page_size, log2))
     return MPT_ERR_INVALID_ARG;
   if (!aligned(b->table, 4) || !aligned(b->lens, 4) || !aligned(b->refs, 4)) return MPT_ERR_INVALID_ARG;
-  if (b->rows > 1 << 20 || b->n_pages >= 1 << 30 || (int64_t)b->width << *log2 > INT32_MAX || n > b->rows) return MPT_ERR_TOO_LARGE;
+  if (b->rows > 1 << 20 || b->n_pages >= 1 << 30 || (int64_t)b->width << *log2 > INT32_MAX || n > b->rows || n > kBookList)
+    return MPT_ERR_TOO_LARGE;
   return MPT_OK;
 }
 
-size_t book_workspace(const mpt_kv_book& b) { return sizeof(int32_t) * ((size_t)kBookHeader + b.n_pages + b.rows); }
-
 mpt_status run_book(const mpt_kv_book* b, BookOp op, const int32_t* l0, const int32_t* l1, const int32_t* l2, int32_t lists,
-                    int32_t n, int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* ws, size_t ws_bytes,
-                    void* stream) {
+                    int32_t n, int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* stream) {
   int log2 = 0;
   const mpt_status st = check_book(b, n, &log2);
   if (st != MPT_OK) return st;
@@ -246,8 +244,7 @@ mpt_status run_book(const mpt_kv_book* b, BookOp op, const int32_t* l0, const in
     if (n > 0 && (!list[i] || !aligned(list[i], 4))) return MPT_ERR_INVALID_ARG;
   const bool copies = op == kBookFork ? n > 0 : op == kBookCompact && b->n_pages > 1;
   if (copies && (!copy_src || !copy_dst || !aligned(copy_src, 4) || !aligned(copy_dst, 4) || copy_src == copy_dst)) return MPT_ERR_INVALID_ARG;
-  if (!status || !aligned(status, 4) || !ws || !aligned(ws, 16)) return MPT_ERR_INVALID_ARG;
-  if (ws_bytes < book_workspace(*b)) return MPT_ERR_WORKSPACE_TOO_SMALL;
+  if (!status || !aligned(status, 4)) return MPT_ERR_INVALID_ARG;
   BookParams p;
   std::memset(&p, 0, sizeof(p));
   p.b = *b;
@@ -255,7 +252,6 @@ mpt_status run_book(const mpt_kv_book* b, BookOp op, const int32_t* l0, const in
   p.n = n;
   p.l0 = l0, p.l1 = l1, p.l2 = l2;
   p.copy_src = copy_src, p.copy_dst = copy_dst, p.status = status;
-  p.ws = (int32_t*)ws;
   return launch_kv_book(p, op, (cudaStream_t)stream) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 
@@ -264,33 +260,22 @@ mpt_status run_book(const mpt_kv_book* b, BookOp op, const int32_t* l0, const in
 
 extern "C" {
 
-mpt_status mpt_kv_pages_workspace_bytes(const mpt_kv_book* book, size_t* bytes) {
-  int log2 = 0;
-  if (!bytes) return MPT_ERR_INVALID_ARG;
-  const mpt_status st = mpt::check_book(book, 0, &log2);
-  if (st == MPT_OK) *bytes = mpt::book_workspace(*book);
-  return st;
-}
-
 mpt_status mpt_kv_fork(const mpt_kv_book* book, const int32_t* src, const int32_t* dst, const int32_t* keep, int32_t n,
-                       int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* workspace, size_t workspace_bytes,
-                       void* stream) {
-  return mpt::run_book(book, mpt::kBookFork, src, dst, keep, 3, n, copy_src, copy_dst, status, workspace, workspace_bytes, stream);
+                       int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* stream) {
+  return mpt::run_book(book, mpt::kBookFork, src, dst, keep, 3, n, copy_src, copy_dst, status, stream);
 }
 
 mpt_status mpt_kv_extend(const mpt_kv_book* book, const int32_t* rows, const int32_t* more, int32_t n, int32_t* status,
-                         void* workspace, size_t workspace_bytes, void* stream) {
-  return mpt::run_book(book, mpt::kBookExtend, rows, more, nullptr, 2, n, nullptr, nullptr, status, workspace, workspace_bytes, stream);
+                         void* stream) {
+  return mpt::run_book(book, mpt::kBookExtend, rows, more, nullptr, 2, n, nullptr, nullptr, status, stream);
 }
 
-mpt_status mpt_kv_free(const mpt_kv_book* book, const int32_t* rows, int32_t n, int32_t* status, void* workspace,
-                       size_t workspace_bytes, void* stream) {
-  return mpt::run_book(book, mpt::kBookFree, rows, nullptr, nullptr, 1, n, nullptr, nullptr, status, workspace, workspace_bytes, stream);
+mpt_status mpt_kv_free(const mpt_kv_book* book, const int32_t* rows, int32_t n, int32_t* status, void* stream) {
+  return mpt::run_book(book, mpt::kBookFree, rows, nullptr, nullptr, 1, n, nullptr, nullptr, status, stream);
 }
 
-mpt_status mpt_kv_compact(const mpt_kv_book* book, int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* workspace,
-                          size_t workspace_bytes, void* stream) {
-  return mpt::run_book(book, mpt::kBookCompact, nullptr, nullptr, nullptr, 0, 0, copy_src, copy_dst, status, workspace, workspace_bytes, stream);
+mpt_status mpt_kv_compact(const mpt_kv_book* book, int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* stream) {
+  return mpt::run_book(book, mpt::kBookCompact, nullptr, nullptr, nullptr, 0, 0, copy_src, copy_dst, status, stream);
 }
 
 mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, int32_t n_pages, int64_t page_stride,

@@ -260,7 +260,7 @@ def _write(s, *args):
 # ---------------------------------------------------------------------------
 
 def _book(table, lens, refs, page_size: int, *lists):
-    """The packed mpt_kv_book, the device, (rows, n_pages) and the length of the lists."""
+    """The packed mpt_kv_book, the device, the number of pages and the length of the lists."""
     index = _device(table, lens, refs, *lists)
     rows, width, stride = _table(table, "table")
     _ints(lens, "lens")
@@ -276,86 +276,66 @@ def _book(table, lens, refs, page_size: int, *lists):
             raise ValueError("the lists must be of one length")
     n_pages = len(refs)
     return _BOOK.pack(table.data_ptr(), stride, width, rows, lens.data_ptr(), refs.data_ptr(), n_pages,
-                      int(page_size)), index, rows, n_pages, n
+                      int(page_size)), index, n_pages, n
 
 
-def _pages_workspace(workspace, index, rows, n_pages, device):
-    if workspace is None:  # what mpt_kv_pages_workspace_bytes says: a header, one int per page and per row
-        return _empty(4 * (16 + n_pages + rows), dtype=_U8, device=device)
-    _check_workspace(workspace, index)
-    return workspace
-
-
-def mpt_kv_pages_workspace_bytes(table, lens, refs, page_size: int) -> int:
-    """Bytes of workspace of the bookkeeping calls."""
-    book = _book(table, lens, refs, page_size)[0]
-    out = ctypes.c_size_t()
-    _mpt._check(_load().mpt_kv_pages_workspace_bytes(book, ctypes.byref(out)), "mpt_kv_pages_workspace_bytes")
-    return int(out.value)
-
-
-def mpt_kv_fork(table, lens, refs, page_size: int, src, dst, keep, *, workspace=None, stream: Optional[int] = None):
+def mpt_kv_fork(table, lens, refs, page_size: int, src, dst, keep, *, stream: Optional[int] = None):
     """Row dst[j] (empty) gets the first keep[j] tokens of row src[j]: full pages shared, a part page
     copied to a fresh one.  Returns (old, fresh, status): int32[n] page pairs for
     :func:`mpt_kv_copy_pages` (-1 where nothing is to copy), and the device int32[2] status."""
-    book = _book(table, lens, refs, page_size, src, dst, keep)
-    return _run(book[1], stream, _fork, *book, table.device, src, dst, keep, workspace)
+    book, index, n_pages, n = _book(table, lens, refs, page_size, src, dst, keep)
+    return _run(index, stream, _fork, book, n, table.device, src, dst, keep)
 
 
-def _fork(s, book, index, rows, n_pages, n, device, src, dst, keep, workspace):
+def _fork(s, book, n, device, src, dst, keep):
     old, fresh = _empty(n, dtype=_INT, device=device), _empty(n, dtype=_INT, device=device)
     status = _empty(2, dtype=_INT, device=device)
-    ws = _pages_workspace(workspace, index, rows, n_pages, device)
     st = _load().mpt_kv_fork(book, src.data_ptr(), dst.data_ptr(), keep.data_ptr(), n, old.data_ptr(), fresh.data_ptr(),
-                                 status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+                             status.data_ptr(), s)
     if st:
         _mpt._check(st, "mpt_kv_fork")
     return old, fresh, status
 
 
-def mpt_kv_extend(table, lens, refs, page_size: int, rows, more, *, workspace=None, stream: Optional[int] = None):
+def mpt_kv_extend(table, lens, refs, page_size: int, rows, more, *, stream: Optional[int] = None):
     """Row rows[j] grows by more[j] tokens onto fresh pages; returns the device int32[2] status."""
-    book = _book(table, lens, refs, page_size, rows, more)
-    return _run(book[1], stream, _extend, *book, table.device, rows, more, workspace)
+    book, index, _, n = _book(table, lens, refs, page_size, rows, more)
+    return _run(index, stream, _extend, book, n, table.device, rows, more)
 
 
-def _extend(s, book, index, n_rows, n_pages, n, device, rows, more, workspace):
+def _extend(s, book, n, device, rows, more):
     status = _empty(2, dtype=_INT, device=device)
-    ws = _pages_workspace(workspace, index, n_rows, n_pages, device)
-    st = _load().mpt_kv_extend(book, rows.data_ptr(), more.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    st = _load().mpt_kv_extend(book, rows.data_ptr(), more.data_ptr(), n, status.data_ptr(), s)
     if st:
         _mpt._check(st, "mpt_kv_extend")
     return status
 
 
-def mpt_kv_free(table, lens, refs, page_size: int, rows, *, workspace=None, stream: Optional[int] = None):
+def mpt_kv_free(table, lens, refs, page_size: int, rows, *, stream: Optional[int] = None):
     """The pages of the listed rows lose a reference, the rows are emptied; returns the device int32[2] status."""
-    book = _book(table, lens, refs, page_size, rows)
-    return _run(book[1], stream, _free, *book, table.device, rows, workspace)
+    book, index, _, n = _book(table, lens, refs, page_size, rows)
+    return _run(index, stream, _free, book, n, table.device, rows)
 
 
-def _free(s, book, index, n_rows, n_pages, n, device, rows, workspace):
+def _free(s, book, n, device, rows):
     status = _empty(2, dtype=_INT, device=device)
-    ws = _pages_workspace(workspace, index, n_rows, n_pages, device)
-    st = _load().mpt_kv_free(book, rows.data_ptr(), n, status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    st = _load().mpt_kv_free(book, rows.data_ptr(), n, status.data_ptr(), s)
     if st:
         _mpt._check(st, "mpt_kv_free")
     return status
 
 
-def mpt_kv_compact(table, lens, refs, page_size: int, *, workspace=None, stream: Optional[int] = None):
+def mpt_kv_compact(table, lens, refs, page_size: int, *, stream: Optional[int] = None):
     """Moves the live pages to the lowest ids; returns (old, fresh, status): int32[n_pages // 2] page
     pairs for :func:`mpt_kv_copy_pages` (the moves, then -1), and the device int32[2] status."""
-    book = _book(table, lens, refs, page_size)
-    return _run(book[1], stream, _compact, *book, table.device, workspace)
+    book, index, n_pages, _ = _book(table, lens, refs, page_size)
+    return _run(index, stream, _compact, book, n_pages // 2, table.device)
 
 
-def _compact(s, book, index, rows, n_pages, _, device, workspace):
-    n = n_pages // 2
+def _compact(s, book, n, device):
     old, fresh = _empty(n, dtype=_INT, device=device), _empty(n, dtype=_INT, device=device)
     status = _empty(2, dtype=_INT, device=device)
-    ws = _pages_workspace(workspace, index, rows, n_pages, device)
-    st = _load().mpt_kv_compact(book, old.data_ptr(), fresh.data_ptr(), status.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    st = _load().mpt_kv_compact(book, old.data_ptr(), fresh.data_ptr(), status.data_ptr(), s)
     if st:
         _mpt._check(st, "mpt_kv_compact")
     return old, fresh, status

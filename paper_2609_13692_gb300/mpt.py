@@ -47,7 +47,7 @@ EXPORTED = [
     "mpt_cache_costs", "mpt_layout_pinned", "mpt_solve_steps", "mpt_solve_begin", "mpt_solve_layers",
     "mpt_solve_end", "mpt_solve_resume", "mpt_set_tables", "mpt_tables32", "mpt_gather_bandwidth",
     "mpt_alu_addmin_peak", "mpt_build_info", "mpt_kv_attend_workspace_bytes", "mpt_kv_attend", "mpt_kv_merge",
-    "mpt_kv_write", "mpt_kv_pages_workspace_bytes", "mpt_kv_fork", "mpt_kv_extend", "mpt_kv_free", "mpt_kv_compact",
+    "mpt_kv_write", "mpt_kv_fork", "mpt_kv_extend", "mpt_kv_free", "mpt_kv_compact",
     "mpt_kv_copy_pages", "mpt_kv_check",
 ]
 
@@ -144,11 +144,10 @@ def load() -> ctypes.CDLL:
         "mpt_kv_attend": ([vp, vp, vp, i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp], ctypes.c_int),
         "mpt_kv_merge": ([vp, vp, i32, i64, i32, i32, vp, vp, vp], ctypes.c_int),
         "mpt_kv_write": ([vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
-        "mpt_kv_pages_workspace_bytes": ([vp, ctypes.POINTER(sz)], ctypes.c_int),
-        "mpt_kv_fork": ([vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
-        "mpt_kv_extend": ([vp, vp, vp, i32, vp, vp, sz, vp], ctypes.c_int),
-        "mpt_kv_free": ([vp, vp, i32, vp, vp, sz, vp], ctypes.c_int),
-        "mpt_kv_compact": ([vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "mpt_kv_fork": ([vp, vp, vp, vp, i32, vp, vp, vp, vp], ctypes.c_int),
+        "mpt_kv_extend": ([vp, vp, vp, i32, vp, vp], ctypes.c_int),
+        "mpt_kv_free": ([vp, vp, i32, vp, vp], ctypes.c_int),
+        "mpt_kv_compact": ([vp, vp, vp, vp, vp], ctypes.c_int),
         "mpt_kv_copy_pages": ([vp, i32, i64, i32, i64, i64, vp, vp, i32, vp], ctypes.c_int),
         "mpt_kv_check": ([vp], ctypes.c_int),
     }

@@ -93,20 +93,18 @@ def test_book_checks(lib):
         d.update(more)
         return kv._BOOK.pack(*d.values())
 
-    def free(b, n=1, rows=A, status=A, ws=A, ws_bytes=1 << 20):
-        return lib.mpt_kv_free(b, rows, n, status, ws, ws_bytes, 0)
+    def free(b, n=1, rows=A, status=A):
+        return lib.mpt_kv_free(b, rows, n, status, 0)
 
     for more, status in ((dict(table=0), 1), (dict(stride=4), 1), (dict(width=0), 1), (dict(rows=0), 1), (dict(rows=(1 << 20) + 1), 2),
                          (dict(lens=0), 1), (dict(refs=A + 1), 1), (dict(n_pages=0), 1), (dict(n_pages=1 << 30), 2), (dict(page=20), 1),
                          (dict(width=1 << 28, stride=1 << 28), 2)):
         assert free(book(**more)) == status, more
     assert free(book(), n=-1) == 1 and free(book(), n=9) == 2 and free(book(), rows=0) == 1 and free(book(), status=0) == 1
-    assert free(book(), ws=0) == 1 and free(book(), ws_bytes=4 * (16 + 10 + 8) - 1) == 5
-    n = ctypes.c_size_t()
-    assert lib.mpt_kv_pages_workspace_bytes(book(), ctypes.byref(n)) == 0 and n.value == 4 * (16 + 10 + 8)
-    assert lib.mpt_kv_fork(book(), A, A, A, 1, A, A, A, A, 1 << 20, 0) == 1  # one list for both pages of the pairs
-    assert lib.mpt_kv_extend(book(), A, 0, 1, A, A, 1 << 20, 0) == 1
-    assert lib.mpt_kv_compact(book(), 0, A, A, A, 1 << 20, 0) == 1
+    assert free(book(rows=1 << 15), n=16_385) == 2
+    assert lib.mpt_kv_fork(book(), A, A, A, 1, A, A, A, 0) == 1  # one list for both pages of the pairs
+    assert lib.mpt_kv_extend(book(), A, 0, 1, A, 0) == 1
+    assert lib.mpt_kv_compact(book(), 0, A, A, 0) == 1
 
 
 def test_copy_checks(lib):

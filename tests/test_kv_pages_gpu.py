@@ -203,6 +203,37 @@ def test_bookkeeping(kv, rows, width, n_pages, page, stride):
         assert same(book, t), (step, kind)
 
 
+def test_bookkeeping_of_long_lists(kv):
+    """As many entries as a call takes, in a table of many rows."""
+    rows, page, n = 100_000, 8, 16_384
+    t = (torch.full((rows, 2), -1, **I32).cuda(), torch.zeros(rows, **I32).cuda(), torch.zeros(60_000, **I32).cuda())
+    pick = torch.randperm(rows)[:2 * n].to(torch.int32)
+    first, second = pick[:n].cuda(), pick[n:].cuda()
+    more = torch.randint(0, 16, (n,)).to(torch.int32)
+    assert kv.mpt_kv_extend(*t, page, first, more.cuda()).tolist()[0] == 0
+    need = -(-more // page)
+    at = need.cumsum(0) - need
+    for i in range(2):  # pages in list order, the lowest first
+        want = torch.where(need > i, at + i, -1).to(torch.int32)
+        assert torch.equal(t[0][first.long(), i].cpu(), want)
+    keep = torch.minimum(more, torch.randint(0, 16, (n,)).to(torch.int32))
+    old, fresh, status = kv.mpt_kv_fork(*t, page, first, second, keep.cuda())
+    part = keep % page > 0
+    used = int(need.sum())
+    assert status.tolist() == [0, 60_000 - used - int(part.sum())]
+    rank = part.cumsum(0) - 1
+    assert torch.equal(fresh.cpu(), torch.where(part, used + rank, -1).to(torch.int32))
+    assert torch.equal(old.cpu(), torch.where(part, at + keep // page, -1).to(torch.int32))
+    assert torch.equal(t[1][second.long()].cpu(), keep)
+    refs = torch.zeros(60_000, **I32)
+    refs[:used + int(part.sum())] = 1
+    full = keep // page
+    refs[at[full > 0]] += 1
+    assert torch.equal(t[2].cpu(), refs)
+    assert kv.mpt_kv_free(*t, page, first).tolist()[0] == 0
+    assert kv.mpt_kv_free(*t, page, second).tolist() == [0, 60_000]
+
+
 def test_bookkeeping_of_holes(kv):
     """Entries that the cache does not hold stay holes and hold no reference."""
     book = M.Book(4, 4, 20, 8)
@@ -255,9 +286,9 @@ def test_bookkeeping_refusals(kv):
     from paper_2609_13692_gb300.mpt import MPTError
 
     t = M.Book(4, 4, 10, 16).tensors("cuda")
-    assert kv.mpt_kv_pages_workspace_bytes(*t, 16) == 4 * (16 + 10 + 4)
+    wide = (torch.full((20_000, 1), -1, **I32).cuda(), torch.zeros(20_000, **I32).cuda(), t[2])
     for call, st in ((lambda: kv.mpt_kv_free(*t, 12, dev([0])), 1), (lambda: kv.mpt_kv_free(*t, 16, dev([0, 1, 2, 3, 0])), 2),
-                     (lambda: kv.mpt_kv_extend(*t, 16, dev([0]), dev([1]), workspace=torch.empty(16, dtype=torch.uint8, device="cuda")), 5)):
+                     (lambda: kv.mpt_kv_free(*wide, 16, torch.arange(16_385, **I32).cuda()), 2)):
         with pytest.raises(MPTError) as e:
             call()
         assert e.value.status == st
