@@ -14,15 +14,24 @@
 // products run, the other's probabilities are computed.
 //
 // Measured (one GB300, 32 query heads on 8 KV heads of 128, pages of 16): 4,096
-// tokens over 20,480 keys 0.81 ms, 1.53 PFLOP/s, 0.82 of the measured matrix
-// rate (28 requests of 28 to 685 tokens over 700 to 6,000 keys, 24 heads of 96,
-// a tenth of the pages absent: 0.41 ms).  On a smaller case at full clocks the
-// tensor pipe is busy 60 % of the time: a row tile's chain of scores,
-// probabilities (about 1,300 cycles, half of it exponentials), outputs and the
-// hand-over between warps takes 2,600 to 3,000 cycles, and only two such chains
-// fit in tensor memory.  Tried and slower: P handed over in halves (the products
-// wait for the second half), P against the last maximum while the new one is
-// found (1.20 ms), one code path for an item's first scores (0.87 ms).
+// tokens over 20,480 keys 0.78 ms, 1.60 PFLOP/s, 0.86 of the measured matrix
+// rate (0.84 ms after a second of it, when the clock has dropped); 28 requests
+// of 28 to 685 tokens over 700 to 6,000 keys, 24 heads of 96, a tenth of the
+// pages absent: 0.38 ms.  On a smaller case at full clocks the tensor pipe is
+// busy 63 % of the time: a row tile's chain of scores, probabilities (about
+// 1,300 cycles, half of it exponentials), outputs and the hand-over between
+// warps takes 2,600 to 3,200 cycles, and only two such chains fit in tensor
+// memory.  Per key tile warp 8 spends 2,400 cycles on the pipe's 2,048 and 780
+// waiting for P.  An item costs 8 us besides (7 a block in the 0.38 ms): its last
+// outputs, queries and first scores follow one another.
+//
+// Tried and slower: P handed over in halves (the products wait for the second
+// half), P against the last maximum while the new one is found (1.20 ms), one
+// code path for an item's first scores (0.87 ms); an item's first keys copied
+// before its queries (0.38 -> 0.40 ms), the second row tile's first scores
+// issued once the first's P stands (0.89 and 0.40 ms), what the roles compute of
+// an item kept in its list entry (few tokens 1 to 4 % faster, but the long chunk
+// 2 % and heads of 64 9 % slower).
 //
 //   warps 0-3, 4-7  one row tile each, one thread per row (no exchange between
 //                   threads): S from tensor memory, running maximum, P back
