@@ -27,7 +27,8 @@
 //
 // Tried and slower: P handed over in halves (the products wait for the second
 // half), P against the last maximum while the new one is found (1.20 ms), one
-// code path for an item's first scores (0.87 ms); an item's first keys copied
+// code path for an item's first scores (0.87 ms); two threads a row, sixteen
+// warps of rows that exchange maxima (0.94 ms); an item's first keys copied
 // before its queries (0.38 -> 0.40 ms), the second row tile's first scores
 // issued once the first's P stands (0.89 and 0.40 ms), what the roles compute of
 // an item kept in its list entry (few tokens 1 to 4 % faster, but the long chunk
