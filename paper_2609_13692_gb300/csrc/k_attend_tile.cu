@@ -15,9 +15,9 @@
 //
 // Measured (one GB300, 32 query heads on 8 KV heads of 128, pages of 16): 4,096
 // tokens over 20,480 keys 0.78 ms, 1.60 PFLOP/s, 0.86 of the measured matrix
-// rate (0.84 ms after a second of it, when the clock has dropped); 28 requests
-// of 28 to 685 tokens over 700 to 6,000 keys, 24 heads of 96, a tenth of the
-// pages absent: 0.38 ms.  On a smaller case at full clocks the tensor pipe is
+// rate; call after call 0.82 ms at the power limit (1,365 W, 1,950 MHz), 1.51
+// PFLOP/s, 0.87 of the sustained matrix rate.  28 requests of 28 to 685 tokens
+// over 700 to 6,000 keys, 24 heads of 96, a tenth of the pages absent: 0.38 ms.  On a smaller case at full clocks the tensor pipe is
 // busy 63 % of the time: a row tile's chain of scores, probabilities (about
 // 1,300 cycles, half of it exponentials), outputs and the hand-over between
 // warps takes 2,600 to 3,200 cycles, and only two such chains fit in tensor
