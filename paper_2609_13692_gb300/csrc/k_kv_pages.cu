@@ -550,7 +550,9 @@ template <int OP>
 cudaError_t book(const BookParams& p, cudaStream_t stream) {
   const size_t smem = (size_t)(p.b.rows + 31) / 32 * 4 + (OP == kBookFree ? 0 : (size_t)p.n * 4);
   cudaError_t e = cudaSuccess;
-  if (smem > 40 * 1024) e = cudaFuncSetAttribute(k_kv_book<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  // the most that a call may need, whatever this one does: another thread's call may be between its own two steps
+  constexpr int kMost = (1 << 20) / 8 + kBookList * 4;
+  if (smem > 40 * 1024) e = cudaFuncSetAttribute(k_kv_book<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
   if (e != cudaSuccess) return e;
   k_kv_book<OP><<<kCluster, kBookThreads, smem, stream>>>(p);
   return cudaGetLastError();
