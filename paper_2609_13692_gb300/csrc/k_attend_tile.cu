@@ -1099,7 +1099,7 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
 #pragma unroll 8
   for (int k = 0; k < d.w; ++k) top = fmaxf(top, (k ? rest + 2 * (k - 1) * kSlot : first)[C::kRows * HDP + slot_row]);
   const float safe = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
+#pragma unroll 8  // reads in flight: 20 parts of 8 items 42.5 -> 40.6 us a call (4); 16, or rounds with absent parts, no better
   for (int k = 0; k < d.w; ++k) {
     const float* at = k ? rest + 2 * (k - 1) * kSlot : first;
     const float f = ex2(at[C::kRows * HDP + slot_row] - safe);
