@@ -62,7 +62,7 @@ __device__ int g_tile_flags;
 
 constexpr int kKeys = 128;     // keys of a tile
 constexpr int kThreads = 384;
-constexpr int kOddSets = 4;    // items whose notes are kept apart (warp 11 is at most two ahead of the rows)
+constexpr int kOddSets = 4;    // items whose notes are kept apart
 constexpr int kList = 32;      // items listed at a time
 constexpr int kHeldSets = 16;  // key tiles whose page marks are kept apart
 
@@ -95,6 +95,7 @@ struct alignas(16) TileEntry {
 
 struct TileShared {
   unsigned long long full[8], empty[8], q_full, q_empty, s_full[3], p_ready[3], o_full[2], o_step, drain;
+  unsigned long long odd_read[2][kOddSets];  // a row tile's warps have done with the notes of a set
   uint32_t tmem;
   int gave_up;
   uint32_t held[kHeldSets];
@@ -436,6 +437,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     mbar_init(&sh.o_full[1], 1);
     mbar_init(&sh.o_step, 1);
     mbar_init(&sh.drain, 1);
+    for (int s = 0; s < 2; ++s)
+      for (int i = 0; i < kOddSets; ++i) mbar_init(&sh.odd_read[s][i], 4);
     sh.gave_up = 0;
     mbar_init_fence();
   }
@@ -799,11 +802,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       TileItem w;
       int k = 0;
       uint32_t idx = 0, item = 0, ready = 0, due = 0;  // idx: ring use of tile j's keys; due: score buffers with a phase to end
+      // Of each set of notes, a bit for each row tile that reads its last item's,
+      // and the parity of that row tile's next phase.  The rows of an item wait
+      // for this warp's arrivals, so a set's barrier is never two phases on.
+      uint32_t reads = 0, read_phase = 0;
       bool ok = true;
       do {
         w.load(p, &sh.list[k]);
         if (w.tiles == 0) continue;
-        uint32_t* odd = sh.odd[item % kOddSets];
+        // A row tile that adds keys one by one may be several items behind the
+        // other one, where those have no part of it: a set is written again only
+        // once both have read it.
+        const uint32_t set = item % kOddSets;
+        for (int s = 0; s < 2 && ok; ++s) {
+          const uint32_t bit = 1u << (2 * set + s);
+          if (!(reads & bit)) continue;
+          ok = wait_spaced<100>(&sh.odd_read[s][set], (read_phase & bit) != 0, gave_up);
+          read_phase ^= bit;
+        }
+        if (!ok) break;
+        reads = (reads & ~(3u << 2 * set)) | ((w.n0 > 0 ? 1u : 0u) | (w.n1 > 0 ? 2u : 0u)) << 2 * set;
+        uint32_t* odd = sh.odd[set];
         ++item;
         if (lane < 9) odd[lane] = 0;
         __syncwarp();
@@ -1060,6 +1079,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           part[C::kRows * HDP + s * 128 + r] = m;
           part[C::kRows * HDP + C::kRows + s * 128 + r] = l;
         }
+      }
+      if (w.count(s) > 0) {  // the notes are read
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.odd_read[s][(item - 1) % kOddSets]);
       }
       if (starts && !ends && tid == 0) {
         const int64_t first = range.end - w.e.seg;  // the item's first unit

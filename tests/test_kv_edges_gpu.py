@@ -1,0 +1,43 @@
+"""The paged-cache operators at the edges of their ranges, against the models of tests/kv_model.py."""
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests import kv_model as M
+from tests.test_kv_attend_gpu import BF16, F16, args, kv, make  # noqa: F401 (kv: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def bits(x):
+    return x.view(torch.int32 if x.dtype is torch.float32 else torch.int16)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,dtype", [(8, 2, 128, BF16), (8, 2, 64, F16), (4, 4, 96, BF16), (6, 1, 200, BF16)])
+def test_noted_values_beside_items_of_one_row_tile(kv, heads, kv_heads, dim, dtype):  # noqa: F811
+    """Requests of two row tiles whose new values are not finite, each before several of one row tile: the rows
+    that add such keys one by one are still at it while the others go on, and keep their own notes."""
+    toks = 128 // (heads // kv_heads)
+    q_lens, kv_lens = [], []
+    for i in range(120):
+        q_lens += [toks + 1 + i % toks, 1, 1, 3, 1, 2, 1]
+        kv_lens += [toks + 9 + i % toks + i % 50, 1 + i % 40, 7, 3, 30, 2 + i % 9, 1]
+    c = make(31, q_lens, kv_lens, heads, kv_heads, dim, 16, dtype)
+    for i in range(0, len(q_lens), 7):
+        keys = torch.arange(kv_lens[i] - q_lens[i] + 1, kv_lens[i], 2 if i % 2 else 3, device="cuda")
+        pages = c["table"][i].long()[keys // 16]
+        c["v"][pages, keys % 16, :, 5] = math.inf
+        c["v"][pages[-1], keys[-1] % 16, :, 33] = math.nan
+    want, want_lse, tol, tol_lse = M.attend(*args(c), True, 1 / math.sqrt(dim))
+    out, lse = kv.mpt_kv_attend(*args(c), max_q_len=2 * toks)
+    kv.mpt_kv_check()
+    assert bool(((lse.double() - want_lse).abs() <= tol_lse).all())
+    finite = torch.isfinite(want)
+    assert bool(((out.double() - want).abs()[finite] <= tol[finite]).all())
+    assert torch.equal(torch.isnan(out), torch.isnan(want)) and torch.equal(torch.isposinf(out), torch.isposinf(want))
+    for _ in range(5):
+        again = kv.mpt_kv_attend(*args(c), max_q_len=2 * toks)
+        assert torch.equal(bits(again[0]), bits(out)) and torch.equal(bits(again[1]), bits(lse))
