@@ -95,7 +95,7 @@ struct alignas(16) TileEntry {
 
 struct TileShared {
   unsigned long long full[8], empty[8], q_full, q_empty, s_full[3], p_ready[3], o_full[2], o_step, drain;
-  unsigned long long odd_read[2][kOddSets];  // a row tile's warps have done with the notes of a set
+  unsigned long long odd_read[kOddSets];  // the rows of both tiles have done with a set of notes
   uint32_t tmem;
   int gave_up;
   uint32_t held[kHeldSets];
@@ -131,6 +131,10 @@ __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parit
   return __all_sync(~0u, mbar_try_wait(bar, parity)) || wait_on(bar, parity, gave_up);
 }
 
+// Several arrivals at once.
+__device__ __forceinline__ void mbar_arrive_n(unsigned long long* bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
+}
 __device__ __forceinline__ void bar_all() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
 
 // The same for the warps that have time: polls take issue slots that the rows'
@@ -437,8 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     mbar_init(&sh.o_full[1], 1);
     mbar_init(&sh.o_step, 1);
     mbar_init(&sh.drain, 1);
-    for (int s = 0; s < 2; ++s)
-      for (int i = 0; i < kOddSets; ++i) mbar_init(&sh.odd_read[s][i], 4);
+    for (int i = 0; i < kOddSets; ++i) mbar_init(&sh.odd_read[i], 8);
     sh.gave_up = 0;
     mbar_init_fence();
   }
@@ -569,7 +572,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   };
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // 2 x 216 + 72 = 3 x 168
+    // 2 x 208 + 88 = 3 x 168.  With 72 for these warps and 216 for the rows' the
+    // long chunk took 775 to 870 us, by how little the warps' code differed; with
+    // 88, 784 to 786.
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9 || warp == 10) {
       // ---- copies: warp 9 queries and keys, warp 10 values ----
       // Tile g of the block (over all its items) has its keys in use 2 g of the
@@ -599,6 +605,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
               for (int b = 0; b < C::kBlk; ++b)
                 tma_load_3d(qbuf + (s * C::kBlk + b) * 128 * 128, &p.map_q, b * 64, head * p.group, tok + s * toks, &sh.q_full);
           __syncwarp();
+          ++item;
+        } else {
+          // Warp 11 writes an item's notes once its first values are there, and
+          // they are copied once the set's last notes have been read: a row tile
+          // that adds keys one by one may be several items behind the other,
+          // where those have no part of it.  For an absent row tile this warp arrives.
+          const uint32_t set = item % kOddSets;
+          if (item >= kOddSets) ok = ok && wait_spaced<100>(&sh.odd_read[set], (item / kOddSets - 1) & 1, gave_up);
+          if (!ok) break;
+          if (lane == 0 && (w.n0 == 0 || w.n1 == 0)) mbar_arrive_n(&sh.odd_read[set], 4);
           ++item;
         }
         const int32_t* row = p.table + (int64_t)w.e.req * p.table_stride;
@@ -802,35 +818,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       TileItem w;
       int k = 0;
       uint32_t idx = 0, item = 0, ready = 0, due = 0;  // idx: ring use of tile j's keys; due: score buffers with a phase to end
-      // Of each set of notes, a bit for each row tile that reads its last item's,
-      // and the parity of that row tile's next phase.  The rows of an item wait
-      // for this warp's arrivals, so a set's barrier is never two phases on.
-      uint32_t reads = 0, read_phase = 0;
       bool ok = true;
       do {
         w.load(p, &sh.list[k]);
         if (w.tiles == 0) continue;
-        // A row tile that adds keys one by one may be several items behind the
-        // other one, where those have no part of it: a set is written again only
-        // once both have read it.
-        const uint32_t set = item % kOddSets;
-        for (int s = 0; s < 2 && ok; ++s) {
-          const uint32_t bit = 1u << (2 * set + s);
-          if (!(reads & bit)) continue;
-          ok = wait_spaced<100>(&sh.odd_read[s][set], (read_phase & bit) != 0, gave_up);
-          read_phase ^= bit;
-        }
-        if (!ok) break;
-        reads = (reads & ~(3u << 2 * set)) | ((w.n0 > 0 ? 1u : 0u) | (w.n1 > 0 ? 2u : 0u)) << 2 * set;
-        uint32_t* odd = sh.odd[set];
+        uint32_t* odd = sh.odd[item % kOddSets];
         ++item;
-        if (lane < 9) odd[lane] = 0;
-        __syncwarp();
         for (int j = 0; j < w.tiles && ok; ++j, idx += 2) {
           const uint32_t vi = idx + 1, ki = idx + 2;
           const int s = vi % C::kSlots;
           ok = wait_spaced<100>(&sh.full[s], (vi / C::kSlots) & 1, gave_up);
           if (!ok) break;
+          if (j == 0) {
+            if (lane < 9) odd[lane] = 0;
+            __syncwarp();
+          }
           if (w.partly(j)) {
             const uint32_t at = smem_u32(ring + s * C::kSlot);
             const int key0 = (w.e.t0 + j) * kKeys;
@@ -889,7 +891,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       if (!ok) leave();
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---- one row per thread ----
     TileItem w;
     int k = 0;
@@ -1082,7 +1084,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       }
       if (w.count(s) > 0) {  // the notes are read
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.odd_read[s][(item - 1) % kOddSets]);
+        if (lane == 0) mbar_arrive(&sh.odd_read[(item - 1) % kOddSets]);
       }
       if (starts && !ends && tid == 0) {
         const int64_t first = range.end - w.e.seg;  // the item's first unit
@@ -1155,11 +1157,11 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
 template <int HDP, bool F16>
 cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream) {
   using C = TileCfg<HDP>;
-  // the warpgroups' shares (2 x 216 + 72) have to fit the registers of the launch, or they would wait for ever
+  // the warpgroups' shares (2 x 208 + 88) have to fit the registers of the launch, or they would wait for ever
   static const cudaError_t fits = [] {
     cudaFuncAttributes a;
     const cudaError_t e = cudaFuncGetAttributes(&a, k_attend_tile<HDP, F16>);
-    return e != cudaSuccess ? e : a.numRegs * 3 >= 2 * 216 + 72 ? cudaSuccess : cudaErrorInvalidConfiguration;
+    return e != cudaSuccess ? e : a.numRegs * 3 >= 2 * 208 + 88 ? cudaSuccess : cudaErrorInvalidConfiguration;
   }();
   if (fits != cudaSuccess) return fits;
   static std::atomic<uint64_t> allowed;

@@ -2,12 +2,14 @@
 paper_2609_13692_gb300/csrc/k_attend_tile.cu), run on random interleavings of its roles.
 
 An item has n0 key tiles for its first row tile and n1 for its second (0: it has none).  Per item, the
-watching warp waits until both row tiles have read what its set of notes held for the item four before,
-where they had a part of that, then writes the set; per key tile it waits until the last phase that it
-gave each score buffer has ended and arrives on "P ready" of those that the tile concerns.  The issuing
-warp makes the first scores, then per key tile waits for P of each row tile and issues its outputs and
-next scores.  A row tile takes its scores, arrives on "P ready", and after its last waits for its
-outputs, reads the item's notes (for as long as it takes) and arrives on the set's barrier.
+warp that copies values waits until both row tiles have read what its set of notes held for the item
+four before, arrives on the set's barrier for a row tile that has no part of the item, and copies the
+values of its key tiles.  Per key tile the watching warp waits for the values, at the item's first writes
+the set, then waits until the last phase that it gave each score buffer has ended and arrives on
+"P ready" of those that the tile concerns.  The issuing warp makes the first scores, then per key tile
+waits for P of each row tile and issues its outputs and next scores.  A row tile takes its scores,
+arrives on "P ready", and after its last waits for its outputs, reads the item's notes (for as long as
+it takes) and arrives on the set's barrier.
 
 Checked on every interleaving: no deadlock; a parity wait never sees two phases pass; the notes that a
 row tile reads are its own item's from its first look to its last.  The planted mistakes must be caught.
@@ -20,8 +22,8 @@ import pytest
 SETS = 4
 
 
-def simulate(items, rng, waits_for=lambda s, item: True, sets=SETS):
-    need = {"p": 2}  # the rows' arrival and the watching warp's
+def simulate(items, rng, waits=True, stands_in=True, sets=SETS):
+    need = {"p": 2, "read": 2}  # the rows' arrival and the watching warp's; both row tiles'
     done, arrived = {}, {}
     notes = [None] * sets
     reading = {}  # (row tile, set) -> item
@@ -37,21 +39,28 @@ def simulate(items, rng, waits_for=lambda s, item: True, sets=SETS):
         assert n <= phase + 1, f"parity wait on {bar} for phase {phase} after {n}"
         return n > phase
 
-    def watch():
-        owed, phase, given, due = {}, {}, [0, 0], []
+    def copies():
         for i, n in enumerate(items):
             c = i % sets
+            if i >= sets and waits:
+                yield ("read", c), i // sets - 1
             for s in (0, 1):
-                if owed.get((s, c)):
-                    if waits_for(s, i):
-                        yield ("read", s, c), phase.get((s, c), 0)
-                    phase[s, c] = phase.get((s, c), 0) + 1
-                owed[s, c] = n[s] > 0
-            for s in (0, 1):
-                assert (s, c) not in reading, f"notes of item {reading.get((s, c))} written over by item {i}"
-            notes[c] = i
-            yield None
+                if stands_in and n[s] == 0:
+                    arrive(("read", c))
             for j in range(max(n)):
+                yield None
+                arrive(("v", (i, j)))
+
+    def watch():
+        given, due = [0, 0], []
+        for i, n in enumerate(items):
+            c = i % sets
+            for j in range(max(n)):
+                yield ("v", (i, j)), 0
+                if j == 0:
+                    for s in (0, 1):
+                        assert (s, c) not in reading, f"notes of item {reading.get((s, c))} written over by item {i}"
+                    notes[c] = i
                 for s in due:
                     yield ("p", s), given[s] - 1
                 due = [s for s in (0, 1) if j < n[s]]
@@ -93,21 +102,21 @@ def simulate(items, rng, waits_for=lambda s, item: True, sets=SETS):
                 assert notes[c] == i, f"row tile {s} reads item {notes[c]}'s notes for item {i}'s"
                 yield None
             del reading[s, c]
-            arrive(("read", s, c))
+            arrive(("read", c))
             yield None
 
-    progs = [watch(), issue(), rows(0), rows(1)]
-    waits, over = [next(p, "end") for p in progs], [False] * 4
+    progs = [copies(), watch(), issue(), rows(0), rows(1)]
+    at, over = [next(p, "end") for p in progs], [False] * 5
     pace = [rng.choice([1, 1, 8, 60]) for _ in progs]  # some roles far slower than others
     while True:
-        for w, at in enumerate(waits):
-            over[w] = at == "end"
-        ready = [w for w in range(4) if not over[w] and (waits[w] is None or passable(*waits[w]))]
+        for w, wait in enumerate(at):
+            over[w] = wait == "end"
+        ready = [w for w in range(5) if not over[w] and (at[w] is None or passable(*at[w]))]
         if not ready:
-            assert all(over), f"deadlock: {waits}"
+            assert all(over), f"deadlock: {at}"
             return
         w = rng.choices(ready, [1 / pace[w] for w in ready])[0]
-        waits[w] = next(progs[w], "end")
+        at[w] = next(progs[w], "end")
 
 
 def lists(rng, count):
@@ -143,9 +152,7 @@ def caught(**planted):
 
 
 def test_planted_protocol_mistakes_are_caught():
-    # no wait at all: only the score buffers hold the watching warp back
-    assert caught(waits_for=lambda s, i: False)
-    # the first row tile alone
-    assert caught(waits_for=lambda s, i: s == 0)
-    # the second alone
-    assert caught(waits_for=lambda s, i: s == 1, sets=1)
+    # no wait: only the score buffers hold the watching warp back
+    assert caught(waits=False)
+    # nobody arrives for a row tile that has no part of an item
+    assert caught(stands_in=False)
