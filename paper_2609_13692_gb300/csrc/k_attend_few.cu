@@ -207,9 +207,9 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
         const int s = it % C::kStages;
         const int id = next;
         next = page_of(t + C::kCopyWarps, mine);
-        if (it >= C::kStages && !wait_bar(&empty[s], (it / C::kStages - 1) & 1, &gave_up, &g_few_flags)) {
-          ok = false;
-          break;
+        if (it >= C::kStages) {  // a stage that was handed back by warps that gave up may still be filling
+          ok = __all_sync(~0u, wait_bar(&empty[s], (it / C::kStages - 1) & 1, &gave_up, &g_few_flags) && *(volatile int*)&gave_up == 0);
+          if (!ok) break;
         }
         const unsigned held = __ballot_sync(~0u, id >= 0);  // bit q: box q % per
         if (lane == 0) {
@@ -243,12 +243,11 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
         if (req >= p.batch) break;
       }
     }
-    if (!ok) {
-      // let the copies in flight land before the block ends
-      for (uint32_t k = done > C::kStages ? done - C::kStages : 0; k < done; ++k)
-        for (int i = 0; k % C::kCopyWarps == me && i < 1 << 16 && !mbar_try_wait(&full[k % C::kStages], (k / C::kStages) & 1); ++i) {
-        }
-    }
+    // The block ends after this warp's copies have landed, also where the warps
+    // that take them have given up.  (Its last use of a stage is that stage's
+    // last phase.)
+    for (uint32_t k = done > C::kStages ? done - C::kStages : 0; k < done; ++k)
+      if (k % C::kCopyWarps == me) wait_landed(&full[k % C::kStages], (k / C::kStages) & 1);
     return;
   }
 
@@ -306,7 +305,8 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
 
     for (int t = t0; t < last; ++t, ++it) {
       const int s = it % C::kStages;
-      wait_bar(&full[s], (it / C::kStages) & 1, &gave_up, &g_few_flags);  // having given up, the block still ends in order
+      // having given up, the block still ends in order
+      (void)__all_sync(~0u, wait_bar(&full[s], (it / C::kStages) & 1, &gave_up, &g_few_flags));
       const uint32_t kbase = smem_u32(ring + s * C::kStage), vbase = kbase + C::kStage / 2;
 
       // S = Q K^T for 16 keys

@@ -97,6 +97,7 @@ struct TileShared {
   unsigned long long full[8], empty[8], q_full, q_empty, s_full[3], p_ready[3], o_full[2], o_step, drain;
   unsigned long long odd_read[kOddSets];  // the rows of both tiles have done with a set of notes
   uint32_t tmem;
+  uint32_t sent[2], asked;  // copies issued, for the block's end: tiles of keys and of values, items' queries
   int gave_up;
   uint32_t held[kHeldSets];
   uint32_t odd[kOddSets][9];  // 8 words of keys from the item's first ambiguous one, and whether any is set
@@ -656,14 +657,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           __syncwarp();
         }
       } while (ok && uniform(next_item(k)));
-      if (!ok) {  // copies in flight land before the block ends
-        for (uint32_t k = gt > C::kSlots ? gt - C::kSlots : 0; k < gt; ++k) {
-          const uint32_t idx = 2 * k + v;
-          for (int i = 0; i < 1 << 16 && !mbar_try_wait(&sh.full[idx % C::kSlots], (idx / C::kSlots) & 1); ++i) {
-          }
-        }
-        leave();
+      if (lane == 0) {
+        sh.sent[v] = gt;
+        if (v == 0) sh.asked = item;
       }
+      if (!ok) leave();
     } else if (warp == 8) {
       // ---- products ----
       // The whole warp takes every step and one lane issues, with operands that
@@ -1096,6 +1094,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   }
 
   __syncthreads();
+  // Where a role gave up, copies may be in flight that nobody waited for: the
+  // last uses of the ring (all before them were released, so they have landed)
+  // and the last queries.  They land before the block ends.
+  if ((warp == 9 || warp == 10) && *(volatile int*)gave_up) {
+    const uint32_t v = warp - 9, n = sh.sent[v], last = (C::kSlots + 1) / 2;
+    for (uint32_t k = n > last ? n - last : 0; k < n; ++k) {
+      const uint32_t idx = 2 * k + v;
+      wait_landed(&sh.full[idx % C::kSlots], (idx / C::kSlots) & 1);
+    }
+    if (v == 0 && sh.asked > 0) wait_landed(&sh.q_full, (sh.asked - 1) & 1);
+  }
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 

@@ -122,6 +122,16 @@ __device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parit
   }
 }
 
+// For copies in flight when a block ends early: a second at most.
+__device__ __forceinline__ void wait_landed(unsigned long long* bar, uint32_t parity) {
+  unsigned long long start = 0;
+  while (!mbar_try_wait(bar, parity)) {
+    const unsigned long long now = now_ns();
+    if (start == 0) start = now;
+    if (now - start > 1000000000ull) return;
+  }
+}
+
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
