@@ -164,6 +164,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
   }
   launch_dependents();
   const AttnRange range = attn_range<C::kThreads>(p.batch, blockIdx.x, gridDim.x, scratch, [&](int i) -> int64_t {
+    if (attn_falls(p, i)) return -1;
     const AttnReq r = attn_req(p, i);
     return (int64_t)p.kv_heads * row_tiles(p, r) * key_tiles(r);
   });

@@ -451,8 +451,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   int4* const reqs = (int4*)ring;
   {
     const int per = (p.batch + kThreads - 1) / kThreads, lo = min(tid * per, p.batch), hi = min(lo + per, p.batch);
-    int64_t sum = 0, keys = 0;  // items (fewer than 2^31: q would not fit in memory) and keys
+    int64_t sum = 0, keys = 0;  // items and keys
+    bool bad = false;
     for (int i = lo; i < hi; ++i) {
+      bad |= attn_falls(p, i);
       const AttnReq r = attn_req(p, i);
       const int pairs = pairs_of(p, r.ql);
       reqs[i] = make_int4((int)sum, r.ql, r.kvl, pairs);
@@ -470,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       sh.scratch[warp] = inc;
       sh.scratch[16 + warp] = keys;
     }
-    __syncthreads();
+    bad = __syncthreads_or(bad);
     int64_t before = inc - sum, all = 0;
     keys = 0;
     for (int w = 0; w < kThreads / 32; ++w) {
@@ -480,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     }
     for (int i = lo; i < hi; ++i) reqs[i].x += (int)before;
     if (tid == 0) {
-      sh.items = (int)all;
+      sh.items = bad || all > INT32_MAX ? 0 : (int)all;  // (2^31 items: q would not fit in memory)
       sh.stride = keys * p.kv_heads * p.dim * 4 > kNaturalBytes ? (int)gridDim.x : 1;
     }
     __syncthreads();

@@ -75,6 +75,10 @@ __device__ __forceinline__ AttnReq attn_req(const AttnParams& p, int i) {
   return r;
 }
 
+// Offsets that decrease could give many requests the same tokens, and a call
+// more work than its tensors can hold: such a call does nothing.
+__device__ __forceinline__ bool attn_falls(const AttnParams& p, int i) { return p.q_offsets[i + 1] < p.q_offsets[i]; }
+
 // Keys that token t of the request may see: j < the returned value.
 __device__ __forceinline__ int attn_limit(const AttnParams& p, const AttnReq& r, int t) {
   if (!p.causal) return r.kvl;
@@ -148,7 +152,9 @@ struct AttnRange {
 };
 
 // All threads of the block call it; `scratch` holds 40 int64.  units(i): units
-// of request i.
+// of request i; where one is negative, or the line is too long for its products
+// with the number of blocks, there is no work.
+constexpr int64_t kMostUnits = 1ll << 53;
 template <int kThreads, typename Units>
 __device__ AttnRange attn_range(int batch, int block, int blocks, int64_t* scratch, Units units) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -156,7 +162,12 @@ __device__ AttnRange attn_range(int batch, int block, int blocks, int64_t* scrat
   const int per = (batch + kThreads - 1) / kThreads;
   const int lo = tid * per < batch ? tid * per : batch, hi = lo + per < batch ? lo + per : batch;
   int64_t sum = 0;
-  for (int i = lo; i < hi; ++i) sum += units(i);
+  bool bad = false;
+  for (int i = lo; i < hi; ++i) {
+    const int64_t u = units(i);
+    bad |= u < 0;
+    sum = sum + u < kMostUnits ? sum + u : kMostUnits;
+  }
   int64_t inc = sum;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -164,13 +175,14 @@ __device__ AttnRange attn_range(int batch, int block, int blocks, int64_t* scrat
     if (lane >= d) inc += v;
   }
   if (lane == 31) scratch[warp] = inc;
-  __syncthreads();
+  bad = __syncthreads_or(bad);
   int64_t before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
     if (w < warp) before += scratch[w];
     total += scratch[w];
   }
+  if (bad || total >= kMostUnits) total = 0;
   AttnRange r;
   r.total = total;
   r.nc = total < blocks ? (int)total : blocks;

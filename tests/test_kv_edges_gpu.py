@@ -41,3 +41,27 @@ def test_noted_values_beside_items_of_one_row_tile(kv, heads, kv_heads, dim, dty
     for _ in range(5):
         again = kv.mpt_kv_attend(*args(c), max_q_len=2 * toks)
         assert torch.equal(bits(again[0]), bits(out)) and torch.equal(bits(again[1]), bits(lse))
+
+
+@pytest.mark.parametrize("hint", [0, 1])
+def test_offsets_that_decrease_do_nothing(kv, hint):  # noqa: F811
+    """Offsets that give every second of 8,192 requests the same 2^17 tokens, 2^31 items in all."""
+    batch, tokens, heads, kv_heads, dim = 8192, 1 << 17, 1024, 8, 8
+    assert batch // 2 * (tokens // (2 * (128 // (heads // kv_heads)))) * kv_heads == 1 << 31
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pool = torch.zeros((2, 8, kv_heads, dim), dtype=BF16, device="cuda")
+    at = torch.zeros(batch + 1, **i32)
+    at[1::2] = tokens
+    q = torch.zeros((tokens, heads, dim), dtype=BF16, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((tokens, heads), 7.0, device="cuda")
+    kv.mpt_kv_attend(q, pool, pool, torch.zeros((batch, 1), **i32), at, torch.full((batch,), 8, **i32), max_q_len=hint, out=out,
+                     lse=lse)
+    kv.mpt_kv_check()
+    assert bool((out == 7.0).all()) and bool((lse == 7.0).all())
+    # one step back among few requests
+    c = make(32, [3, 4, 60], [30, 40, 70], 4, 2, 64, 16, BF16)
+    c["at"][2] = 2
+    out = torch.full_like(c["q"], 7.0)
+    kv.mpt_kv_attend(*args(c), max_q_len=hint, out=out)
+    kv.mpt_kv_check()
+    assert bool((out == 7.0).all())
