@@ -117,8 +117,10 @@ struct FewItem {
 __device__ __forceinline__ int row_tiles(const AttnParams& p, const AttnReq& r) {
   return (int)(((int64_t)r.ql * p.group + kRows - 1) / kRows);
 }
+// Key tiles of n keys (n + kKeys may not fit in 32 bits).
+__device__ __forceinline__ int tiles_of(int n) { return n < 1 ? 0 : (n - 1) / kKeys + 1; }
 __device__ __forceinline__ int key_tiles(const AttnReq& r) {
-  const int n = (r.kvl + kKeys - 1) / kKeys;
+  const int n = tiles_of(r.kvl);
   return n < 1 ? 1 : n;
 }
 
@@ -130,7 +132,7 @@ __device__ __forceinline__ FewItem few_item(const AttnParams& p, const AttnReq& 
   const int64_t left = (int64_t)r.ql * p.group - it.row0;
   it.rows = left < kRows ? (int)left : kRows;
   it.r = r;
-  it.tiles = (attn_limit(p, r, (it.row0 + it.rows - 1) / p.group) + kKeys - 1) / kKeys;
+  it.tiles = tiles_of(attn_limit(p, r, (it.row0 + it.rows - 1) / p.group));
   return it;
 }
 
@@ -333,7 +335,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
       }
 
       const uint32_t held = there[s];
-      const bool partly = t * kKeys + kKeys > lim_lo || held != 0xFFu;
+      const bool partly = lim_lo - t * kKeys < kKeys || held != 0xFFu;
       if (partly) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)

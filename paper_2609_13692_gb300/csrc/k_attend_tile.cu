@@ -933,7 +933,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
               for (int c = 8 * g; c < 8 * g + 8; ++c) f[c] = -INFINITY;
             }
         }
-        if (key0 + kKeys > lim_tile) {
+        if (lim_tile - key0 < kKeys) {
           const int sees = lim - key0;
 #pragma unroll
           for (int c = 0; c < 128; ++c) f[c] = c < sees ? f[c] : -INFINITY;
@@ -1032,8 +1032,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             // seen keys whose values were blanked for the other rows
             const char* q = p.q + 2 * (tok_at * p.q_tok + head * p.q_head);
             for (int a = 0; a < 256; ++a) {
+              if (!(odd[a >> 5] >> (a & 31) & 1u) || a >= lim - w.lim_first) continue;
               const int key = w.lim_first + a;
-              if (!(odd[a >> 5] >> (a & 31) & 1u) || key >= lim) continue;
               const int64_t id = p.table[(int64_t)w.e.req * p.table_stride + (key >> p.page_log2)];
               if (id < 0 || id >= p.n_pages) continue;
               const int64_t slot = key & ((1 << p.page_log2) - 1);

@@ -65,3 +65,29 @@ def test_offsets_that_decrease_do_nothing(kv, hint):  # noqa: F811
     kv.mpt_kv_attend(*args(c), max_q_len=hint, out=out)
     kv.mpt_kv_check()
     assert bool((out == 7.0).all())
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("page,dim,q_len,rest", [(32, 64, 1, 32), (32, 128, 40, 27), (16, 128, 2, 16), (8, 256, 50, 5)])
+def test_keys_up_to_the_last_of_32_bits(kv, page, dim, q_len, rest, causal):  # noqa: F811
+    """A sparse table as wide as it may be, its last page beside 2^31; the keys that are there, as a cache of their own."""
+    width = (2 ** 31 - 1) // page
+    gen = torch.Generator(device="cuda").manual_seed(page)
+    pool = torch.randn((2, 7, page, 2, dim), generator=gen, device="cuda").to(BF16)
+    pool[:, 5, rest:] = math.nan  # beyond the last key
+    i32 = dict(dtype=torch.int32, device="cuda")
+    near = -(-q_len // page) + 1  # the pages of the new tokens, one more
+    table = torch.full((1, width), -1, **i32)
+    there = [0, 12_345_678 // page, *range(width - near, width)]
+    pages = [3, 6, *([1, 0, 2, 4, 1, 0, 2] * 2)[:near - 1], 5]
+    table[0, torch.tensor(there, device="cuda")] = torch.tensor(pages, **i32)
+    q = torch.randn((q_len, 4, dim), generator=gen, device="cuda").to(BF16)
+    at = torch.tensor([0, q_len], **i32)
+    lens = (width - 1) * page + rest
+    assert lens > 2 ** 31 - 64
+    out, lse = kv.mpt_kv_attend(q, pool[0], pool[1], table, at, torch.tensor([lens], **i32), causal=causal, max_q_len=q_len)
+    kv.mpt_kv_check()
+    want, want_lse, tol, tol_lse = M.attend(q, pool[0], pool[1], torch.tensor([pages], **i32), at,
+                                            torch.tensor([(len(pages) - 1) * page + rest], **i32), causal, 1 / math.sqrt(dim))
+    assert bool(((out.double() - want).abs() <= tol).all())
+    assert bool(((lse.double() - want_lse).abs() <= tol_lse).all())
