@@ -89,8 +89,9 @@ mpt_status mpt_kv_attend_workspace_bytes(int32_t head_dim, size_t* bytes);
  *   workspace: device, 256-byte aligned, at least
  *     mpt_kv_attend_workspace_bytes(); not shared with another call in flight.
  * Scores, maxima, sums and the accumulated output are 32-bit; probabilities
- * are rounded to `type` for the product with the values, the output once at
- * the end.  The same call gives the same bits.
+ * are rounded to `type` for the product with the values (f16: at 2^11 times
+ * their size at least, so that many small ones keep their weight), the output
+ * once at the end.  The same call gives the same bits.
  * A bounded wait inside a kernel that gives up shows in mpt_kv_check.
  * Errors: INVALID_ARG, TOO_LARGE, WORKSPACE_TOO_SMALL, CUDA. */
 mpt_status mpt_kv_attend(const mpt_kv_cache* cache, const void* q, const int64_t* q_stride, int64_t tokens,

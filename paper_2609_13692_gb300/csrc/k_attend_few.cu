@@ -84,6 +84,9 @@ __device__ __forceinline__ void ldsm4t(uint32_t* r, uint32_t addr) {
 }
 
 template <bool F16>
+using L = Lift<F16, 0>;
+
+template <bool F16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;
   if (F16)
@@ -351,7 +354,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
         float mx = fmaxf(fmaxf(sc[0][2 * h], sc[0][2 * h + 1]), fmaxf(sc[1][2 * h], sc[1][2 * h + 1]));
         mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
-        const float mn = fmaxf(m[h], mx * p.scale_log2);
+        const float mn = L<F16>::reference(fmaxf(m[h], mx * p.scale_log2));
         const float safe = mn == -INFINITY ? 0.f : mn;
         alpha[h] = ex2(m[h] - safe);
         m[h] = mn;
@@ -360,7 +363,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float v = ex2(fmaf(sc[n][2 * h + e], p.scale_log2, -safe));
+            const float v = ex2(fmaf(sc[n][2 * h + e], p.scale_log2, L<F16>::kLift - safe));
             sc[n][2 * h + e] = v;
             sum += v;
           }
@@ -506,7 +509,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
           w.w = pack2<F16>(v[6] * inv, v[7] * inv);
           *(uint4*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) = w;
         }
-        if (p.lse && col == 0) p.lse[tok * p.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
+        if (p.lse && col == 0) p.lse[tok * p.heads + head] = L<F16>::lse(top, sum);
       } else {
         float4* to = (float4*)(part + row * HDP + col);
         to[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -585,7 +588,7 @@ __global__ void __launch_bounds__(128) k_attend_few_join(const __grid_constant__
       const float b = (acc[0][col + 1] + acc[1][col + 1]) + (acc[2][col + 1] + acc[3][col + 1]);
       *(uint32_t*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) = pack2<F16>(a * inv, b * inv);
     }
-    if (p.lse && threadIdx.x == 0) p.lse[tok * p.heads + head] = (top + log2f(s)) * 0.6931471805599453f;
+    if (p.lse && threadIdx.x == 0) p.lse[tok * p.heads + head] = L<F16>::lse(top, s);
     __syncthreads();
   }
 }

@@ -45,8 +45,8 @@
 //                   the values of tiles with masked keys (below)
 //
 // Rescaling O costs a pass over its 128 columns, so it waits until the maximum
-// has grown by 2^8: any reference below the maximum gives the same quotient,
-// and with 2^8 of room neither P nor its sum can overflow.
+// has grown by 2^8 (f16: 2^4, below): any reference below the maximum gives the
+// same quotient, and with 2^8 of room neither P nor its sum can overflow.
 //
 // A masked key's probability is 0, but 0 times an infinite or NaN value is NaN.
 // Tiles with masked keys are few (the last of an item); warp 11 looks at the
@@ -255,6 +255,14 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+
+// Scores may exceed a row's reference by 2^kLag before its outputs are rescaled
+// (f16: the less, the further down probabilities are rounded; 28 ragged chunks
+// take 381, 385 and 400 us with 8, 4 and 2).
+template <bool F16>
+constexpr int kLag = F16 ? 4 : 8;
+template <bool F16>
+using L = Lift<F16, kLag<F16>>;
 
 template <bool F16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -947,10 +955,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], f[c + q], f[c + 4 + q]);
 #pragma unroll
         for (int q = 0; q < 4; ++q) mx[q] = fmaxf(mx[q], f[124 + q]);
-        const float top = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2);
+        const float top = L<F16>::reference(fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2));
         if (j == 0) {
           m = top;
-        } else if (__any_sync(~0u, top - m > 8.f)) {
+        } else if (__any_sync(~0u, top - m > kLag<F16>)) {
           if (C::kTiles == 1 && j + 1 < w.n0) {
             // These scores did not wait for the outputs of the tile before; the
             // next ones, issued after those outputs, do.
@@ -958,7 +966,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             if (!ok) break;
             fence_after();
           }
-          const bool grows = top - m > 8.f;
+          const bool grows = top - m > kLag<F16>;
           const float a = grows ? ex2(m - top) : 1.f;
           m = grows ? top : m;
           l *= a;
@@ -977,7 +985,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         const float ref = m == -INFINITY ? 0.f : m;
         // P, rounded to the cache's type (the operand's), over S
         uint64_t sum[2] = {0, 0};  // pairs of 32-bit sums
-        const uint64_t mul = pair(p.scale_log2, p.scale_log2), off = pair(-ref, -ref);
+        const uint64_t mul = pair(p.scale_log2, p.scale_log2), off = pair(L<F16>::kLift - ref, L<F16>::kLift - ref);
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
           uint32_t x[16];
@@ -1044,7 +1052,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
                 const float2 a2 = unpack2<F16>(*(const uint32_t*)(q + 2 * d)), b2 = unpack2<F16>(*(const uint32_t*)(kp + 2 * d));
                 dot = fmaf(a2.x, b2.x, fmaf(a2.y, b2.y, dot));
               }
-              const float pr = ex2(fmaf(dot, p.scale_log2, -(m == -INFINITY ? 0.f : m)));
+              const float pr = ex2(fmaf(dot, p.scale_log2, L<F16>::kLift - (m == -INFINITY ? 0.f : m)));
 #pragma unroll
               for (int e = 0; e < 32; e += 2)
                 if (32 * c + e < p.dim) {
@@ -1076,7 +1084,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           }
         }
         if (whole) {
-          if (valid && p.lse) p.lse[tok_at * p.heads + head] = (m + log2f(l)) * 0.6931471805599453f;
+          if (valid && p.lse) p.lse[tok_at * p.heads + head] = L<F16>::lse(m, l);
         } else {
           part[C::kRows * HDP + s * 128 + r] = m;
           part[C::kRows * HDP + C::kRows + s * 128 + r] = l;
@@ -1162,7 +1170,7 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
     v.w = pack2<F16>(acc[c + 6] * inv, acc[c + 7] * inv);
     *(uint4*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) = v;
   }
-  if (p.lse && warp == 0) p.lse[tok * p.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
+  if (p.lse && warp == 0) p.lse[tok * p.heads + head] = L<F16>::lse(top, sum);
 }
 
 template <int HDP, bool F16>

@@ -214,6 +214,22 @@ __device__ __forceinline__ int attn_block_of(const AttnRange& r, int64_t u) {
   return (int)(((u + 1) * r.nc + r.total - 1) / r.total) - 1;
 }
 
+// f16 has no bits below 2^-24: of a probability against a reference of 1 the
+// product with the values would see nothing below 2^-25, but the sum would, and
+// many keys in such a tail would lose their weight.  So f16 probabilities are
+// rounded at 2^kLift times their value, of which output and sum are both made;
+// references are whole numbers there, so the lift adds no rounding.  The largest
+// probability, 2^kLag above the reference in the kernel that rescales seldom,
+// stays below 2^16.
+template <bool F16, int kLag>
+struct Lift {
+  static constexpr float kLift = F16 ? 15 - kLag : 0;
+  static __device__ __forceinline__ float reference(float top) { return F16 ? ceilf(top) : top; }
+  static __device__ __forceinline__ float lse(float top, float sum) {
+    return (top + log2f(sum) - kLift) * 0.6931471805599453f;
+  }
+};
+
 // Few query rows per KV head (k_attend_few.cu): bytes of workspace and launch.
 constexpr int kFewPerSm = 3;  // blocks per SM, at most
 size_t attend_few_workspace(int sms);

@@ -91,3 +91,39 @@ def test_keys_up_to_the_last_of_32_bits(kv, page, dim, q_len, rest, causal):  # 
                                             torch.tensor([(len(pages) - 1) * page + rest], **i32), causal, 1 / math.sqrt(dim))
     assert bool(((out.double() - want).abs() <= tol).all())
     assert bool(((lse.double() - want_lse).abs() <= tol_lse).all())
+
+
+@pytest.mark.parametrize("q_len,group", [(1, 4), (40, 2), (40, 1)])
+@pytest.mark.parametrize("dtype,dim", [(F16, 64), (F16, 128), (F16, 256), (BF16, 128)])
+def test_many_keys_of_small_weight(kv, dtype, dim, q_len, group):  # noqa: F811
+    """The first 128 keys outweigh each of the other 131,072 by 2^25 and more; together those are a part of the
+    output.  So many requests that most are some block's alone."""
+    n, page, batch = 131_200, 64, 1000 if q_len == 1 else 400
+    i32 = dict(dtype=torch.int32, device="cuda")
+    for weight in (2.9e-8, 2.0 ** -26, 1e-9):
+        pool = torch.zeros((2, n // page + 1, page, 1, dim), dtype=dtype, device="cuda")
+        k, v = pool
+        q = torch.zeros((batch * q_len, group, dim), dtype=dtype, device="cuda")
+        q[..., 0] = 4.0
+        # scores are 4 times the key's first element at scale 1: 0 for the far keys, -ln(weight) for the first
+        k[:2, :, 0, 0] = -math.log(weight) / 4
+        v.normal_(generator=torch.Generator(device="cuda").manual_seed(dim))
+        v += 1.0
+        v[:2] = 0
+        c = (q, k, v, torch.arange(n // page, **i32).repeat(batch, 1), torch.arange(0, batch * q_len + 1, q_len, **i32),
+             torch.full((batch,), n, **i32))
+        out, lse = kv.mpt_kv_attend(*c, causal=False, scale=1.0, max_q_len=q_len)
+        kv.mpt_kv_check()
+        s = torch.zeros(n, dtype=torch.float64, device="cuda")
+        s[:128] = 4 * float(k[0, 0, 0, 0])
+        z = torch.logsumexp(s, 0)
+        p, x = torch.exp(s - z), v.view(-1, dim)[:n].double()
+        want = p @ x
+        # each probability rounded once, relatively or (f16) by 2^-25 of 2^11 times its value; the sums' and
+        # exponentials' errors as in tests/kv_model.py; the result rounded, relatively or by half the least f16
+        u, err = M.UNIT[dtype], 2.0 ** -20 + n * 2.0 ** -24
+        tol = u * want.abs() + (u + 2 * err) * (1 + u) * (p @ x.abs()) + 2.0 ** -25
+        if dtype is F16:
+            tol = tol + 2.0 ** -36 * p[0] * x.abs().sum(0)
+        assert bool(((out.double() - want).abs() <= tol).all()), weight
+        assert float((lse.double() - z).abs().max()) <= err + 2.0 ** -20 + 2.0 ** -21 * float(z)
