@@ -184,10 +184,11 @@ mpt_status mpt_kv_compact(const mpt_kv_book* book, int32_t* copy_src, int32_t* c
 mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, int32_t n_pages, int64_t page_stride,
                              int64_t page_bytes, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
 
-/* Waits for `stream`, then reports what the kernels of this header flagged on
- * the current device since the last call, and clears it: MPT_ERR_TIMEOUT when
- * a bounded wait on a shared-memory barrier gave up (the results of the calls
- * since then are not to be used), MPT_OK otherwise.  Errors also: CUDA. */
+/* Waits for `stream`, then reports what kernels of this header met on the
+ * current device, on any stream, that no call has reported: MPT_ERR_TIMEOUT
+ * when a bounded wait on a shared-memory barrier gave up (the results of the
+ * calls since the last MPT_OK are not to be used), MPT_OK otherwise.
+ * Errors also: CUDA. */
 mpt_status mpt_kv_check(void* stream);
 
 #ifdef __cplusplus

@@ -41,7 +41,7 @@ def build(force: bool = False, verbose: bool = False, bounds: bool = False) -> P
     (with bounds=True the bounds-checked variant, in its own directory)."""
     out_dir, lib = (BOUNDS_BUILD, BOUNDS_LIB) if bounds else (BUILD, LIB)
     out_dir.mkdir(exist_ok=True)
-    headers = [*CSRC.glob("*.cuh"), *(ROOT / "include").glob("*.h")]
+    headers = [*CSRC.glob("*.cuh"), *CSRC.glob("*.h"), *(ROOT / "include").glob("*.h")]
     flags = ["-std=c++17", "-O3", "-lineinfo", *ARCH, "-Xcompiler", "-fPIC", "-I", str(ROOT / "include")]
     if bounds:
         flags.append("-DMPT_BOUNDS")

@@ -31,7 +31,7 @@
 namespace mpt {
 namespace {
 
-__device__ int g_few_flags;
+__device__ uint32_t g_few_counts[kKvCounts];
 
 constexpr int kKeys = 64;      // keys of a stage
 constexpr int kRows = 16;      // query rows of an item
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
         const int id = next;
         next = page_of(t + C::kCopyWarps, mine);
         if (it >= C::kStages) {  // a stage that was handed back by warps that gave up may still be filling
-          ok = __all_sync(~0u, wait_bar(&empty[s], (it / C::kStages - 1) & 1, &gave_up, &g_few_flags) && *(volatile int*)&gave_up == 0);
+          ok = __all_sync(~0u, wait_bar(&empty[s], (it / C::kStages - 1) & 1, &gave_up, g_few_counts) && *(volatile int*)&gave_up == 0);
           if (!ok) break;
         }
         const unsigned held = __ballot_sync(~0u, id >= 0);  // bit q: box q % per
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
     for (int t = t0; t < last; ++t, ++it) {
       const int s = it % C::kStages;
       // having given up, the block still ends in order
-      (void)__all_sync(~0u, wait_bar(&full[s], (it / C::kStages) & 1, &gave_up, &g_few_flags));
+      (void)__all_sync(~0u, wait_bar(&full[s], (it / C::kStages) & 1, &gave_up, g_few_counts));
       const uint32_t kbase = smem_u32(ring + s * C::kStage), vbase = kbase + C::kStage / 2;
 
       // S = Q K^T for 16 keys
@@ -628,13 +628,10 @@ cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int 
   return f16 ? launch<256, true>(p, rows_hint, sms, device, stream) : launch<256, false>(p, rows_hint, sms, device, stream);
 }
 
-cudaError_t attend_few_flags(cudaStream_t stream, int* flags) {
+cudaError_t attend_few_counts(cudaStream_t stream, uint32_t* counts) {
   void* at = nullptr;
-  cudaError_t e = cudaGetSymbolAddress(&at, g_few_flags);
-  if (e != cudaSuccess) return e;
-  if ((e = cudaMemcpyAsync(flags, at, sizeof(int), cudaMemcpyDeviceToHost, stream)) != cudaSuccess) return e;
-  if ((e = cudaMemsetAsync(at, 0, sizeof(int), stream)) != cudaSuccess) return e;
-  return cudaStreamSynchronize(stream);
+  const cudaError_t e = cudaGetSymbolAddress(&at, g_few_counts);
+  return e != cudaSuccess ? e : cudaMemcpyAsync(counts, at, sizeof(g_few_counts), cudaMemcpyDeviceToHost, stream);
 }
 
 }  // namespace mpt

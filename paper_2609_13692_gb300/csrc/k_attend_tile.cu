@@ -58,7 +58,7 @@
 namespace mpt {
 namespace {
 
-__device__ int g_tile_flags;
+__device__ uint32_t g_tile_counts[kKvCounts];
 
 constexpr int kKeys = 128;     // keys of a tile
 constexpr int kThreads = 384;
@@ -123,7 +123,7 @@ __device__ __forceinline__ bool wait_on(unsigned long long* bar, uint32_t parity
     if (now - start > 4000000000ull) {
       over = true;
       *(volatile int*)gave_up = 1;
-      atomicOr(&g_tile_flags, kErrTimeout);
+      atomicAdd(&g_tile_counts[kKvGaveUp], 1u);
     }
     if (__any_sync(~0u, over)) return false;
   }
@@ -156,7 +156,7 @@ __device__ __forceinline__ bool wait_spaced(unsigned long long* bar, uint32_t pa
     if (now - start > 4000000000ull) {
       over = true;
       *(volatile int*)gave_up = 1;
-      atomicOr(&g_tile_flags, kErrTimeout);
+      atomicAdd(&g_tile_counts[kKvGaveUp], 1u);
     }
     if (__any_sync(~0u, over)) return false;
   }
@@ -1212,13 +1212,10 @@ cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int devic
   return f16 ? launch<256, true>(p, sms, device, stream) : launch<256, false>(p, sms, device, stream);
 }
 
-cudaError_t attend_tile_flags(cudaStream_t stream, int* flags) {
+cudaError_t attend_tile_counts(cudaStream_t stream, uint32_t* counts) {
   void* at = nullptr;
-  cudaError_t e = cudaGetSymbolAddress(&at, g_tile_flags);
-  if (e != cudaSuccess) return e;
-  if ((e = cudaMemcpyAsync(flags, at, sizeof(int), cudaMemcpyDeviceToHost, stream)) != cudaSuccess) return e;
-  if ((e = cudaMemsetAsync(at, 0, sizeof(int), stream)) != cudaSuccess) return e;
-  return cudaStreamSynchronize(stream);
+  const cudaError_t e = cudaGetSymbolAddress(&at, g_tile_counts);
+  return e != cudaSuccess ? e : cudaMemcpyAsync(counts, at, sizeof(g_tile_counts), cudaMemcpyDeviceToHost, stream);
 }
 
 }  // namespace mpt

@@ -57,6 +57,9 @@ cudaError_t kv_allow_smem(Kernel kernel, int bytes, int device, std::atomic<uint
   return e;
 }
 
+// Events that kernels count on a device, for mpt_kv_check; nothing clears them.
+enum KvCount { kKvGaveUp, kKvCounts };  // blocks' waits that gave up
+
 // One request's lengths, clamped to what the token axis and the table hold.
 struct AttnReq {
   int q0, ql, kvl;  // first token, new tokens, keys
@@ -108,9 +111,9 @@ __device__ __forceinline__ unsigned long long now_ns() {
 }
 
 // Bounded wait of one thread: false once the block has given up, or after four
-// seconds (which it then flags).  The clock is looked at after the first polls
+// seconds (which it then counts).  The clock is looked at after the first polls
 // only: reading it takes longer than most waits.
-__device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up, int* flags) {
+__device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parity, int* gave_up, uint32_t* counts) {
   unsigned long long start = 0;
   for (;;) {
     for (int i = 0; i < 256; ++i)
@@ -120,7 +123,7 @@ __device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parit
     if (*(volatile int*)gave_up) return false;
     if (now - start > 4000000000ull) {
       *(volatile int*)gave_up = 1;
-      atomicOr(flags, kErrTimeout);
+      atomicAdd(&counts[kKvGaveUp], 1u);
       return false;
     }
   }
@@ -234,8 +237,8 @@ struct Lift {
 constexpr int kFewPerSm = 3;  // blocks per SM, at most
 size_t attend_few_workspace(int sms);
 cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, int device, cudaStream_t stream);
-// Flags of the kernels since the last call (waits for the stream).
-cudaError_t attend_few_flags(cudaStream_t stream, int* flags);
+// The kernels' counts, read in the stream's order.
+cudaError_t attend_few_counts(cudaStream_t stream, uint32_t* counts);
 
 // Whole tiles of query rows on tcgen05 (k_attend_tile.cu); at
 // most kTileBatch requests (its list of them, 16 bytes each, is in the room of
@@ -243,6 +246,6 @@ cudaError_t attend_few_flags(cudaStream_t stream, int* flags);
 constexpr int kTileBatch = 8192;
 size_t attend_tile_workspace(int sms);
 cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int device, cudaStream_t stream);
-cudaError_t attend_tile_flags(cudaStream_t stream, int* flags);
+cudaError_t attend_tile_counts(cudaStream_t stream, uint32_t* counts);
 
 }  // namespace mpt

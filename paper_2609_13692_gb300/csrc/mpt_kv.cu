@@ -4,6 +4,7 @@
 #include <cstring>
 
 #include "kv_pages.cuh"
+#include "kv_report.h"
 
 namespace mpt {
 namespace {
@@ -296,12 +297,16 @@ mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, i
   return mpt::launch_kv_copy_pages(p, (cudaStream_t)stream) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 
-mpt_status mpt_kv_check(void* stream) {
-  int few = 0, tile = 0;
-  if (mpt::attend_few_flags((cudaStream_t)stream, &few) != cudaSuccess ||
-      mpt::attend_tile_flags((cudaStream_t)stream, &tile) != cudaSuccess)
+mpt_status mpt_kv_check(void* stream_ptr) {
+  static mpt::Reported few, tile;
+  cudaStream_t stream = (cudaStream_t)stream_ptr;
+  uint32_t f[mpt::kKvCounts], t[mpt::kKvCounts];
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || mpt::attend_few_counts(stream, f) != cudaSuccess ||
+      mpt::attend_tile_counts(stream, t) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
     return MPT_ERR_CUDA;
-  return few | tile ? MPT_ERR_TIMEOUT : MPT_OK;
+  const bool in_few = few.news(device, f[mpt::kKvGaveUp]), in_tile = tile.news(device, t[mpt::kKvGaveUp]);
+  return in_few || in_tile ? MPT_ERR_TIMEOUT : MPT_OK;
 }
 
 }  // extern "C"
