@@ -106,7 +106,8 @@ mpt_status mpt_kv_attend(const mpt_kv_cache* cache, const void* q, const int64_t
  *   outs: host array of n_parts device pointers, each `type`
  *     [rows][head_dim] contiguous, 16-byte aligned; lses: likewise float[rows];
  *   type: BF16, F16 or F32; out the same type; lse may be NULL;
- *   out (lse) may be one of the outs (lses).
+ *   out may be one of the outs; no other overlap of out or lse with one another,
+ *   an out or an lse of a part (INVALID_ARG).
  * Limits: 1 <= n_parts <= 16, rows >= 0, head_dim a multiple of 8 in 8..1024.
  * Errors: INVALID_ARG, TOO_LARGE, CUDA. */
 mpt_status mpt_kv_merge(const void* const* outs, const float* const* lses, int32_t n_parts, int64_t rows,

@@ -93,6 +93,12 @@ bool make_query_map(CUtensorMap* map, const AttnParams& p, bool f16) {
             promotion(p.dim), CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Whether [a, a + an) and [b, b + bn) share a byte.
+bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y ? y - x < (uint64_t)an : x - y < (uint64_t)bn;
+}
+
 size_t attend_workspace(int sms) {
   const size_t few = attend_few_workspace(sms), tile = attend_tile_workspace(sms);
   return few > tile ? few : tile;
@@ -183,8 +189,15 @@ mpt_status mpt_kv_merge(const void* const* outs, const float* const* lses, int32
   if (!out || !mpt::aligned(out, 16) || !mpt::aligned(lse, 4)) return MPT_ERR_INVALID_ARG;
   mpt::MergeParams p;
   std::memset(&p, 0, sizeof(p));
+  // A thread reads its own 16 bytes of every part's out and writes them at one
+  // address: out may be a part.  A row's sums are read by all its threads.
+  const int64_t out_bytes = rows * head_dim * (type == MPT_KV_F32 ? 4 : 2), lse_bytes = rows * (int64_t)sizeof(float);
+  if (lse && mpt::overlap(out, out_bytes, lse, lse_bytes)) return MPT_ERR_INVALID_ARG;
   for (int i = 0; i < n_parts; ++i) {
-    if (!outs[i] || !lses[i] || !mpt::aligned(outs[i], 16) || !mpt::aligned(lses[i], 4) || lses[i] == lse)
+    if (!outs[i] || !lses[i] || !mpt::aligned(outs[i], 16) || !mpt::aligned(lses[i], 4)) return MPT_ERR_INVALID_ARG;
+    if ((outs[i] != out && mpt::overlap(outs[i], out_bytes, out, out_bytes)) || mpt::overlap(lses[i], lse_bytes, out, out_bytes))
+      return MPT_ERR_INVALID_ARG;
+    if (lse && (mpt::overlap(lses[i], lse_bytes, lse, lse_bytes) || mpt::overlap(outs[i], out_bytes, lse, lse_bytes)))
       return MPT_ERR_INVALID_ARG;
     p.outs[i] = outs[i];
     p.lses[i] = lses[i];
