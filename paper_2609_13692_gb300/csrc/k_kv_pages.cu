@@ -174,13 +174,11 @@ __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ WriteP
 // rate)
 // ---------------------------------------------------------------------------
 
-constexpr int kCopyThreads = 256, kCopyVecs = 4, kCopySeg = kCopyThreads * kCopyVecs * 16;
-
 __global__ void __launch_bounds__(kCopyThreads) k_kv_copy_pages(const __grid_constant__ CopyParams p) {
   __shared__ int64_t from[kCopyThreads], to[kCopyThreads];
   __shared__ int left[kCopyThreads], count;
   const int tid = threadIdx.x;
-  const int64_t segs = (p.page_bytes + kCopySeg - 1) / kCopySeg, units = (int64_t)p.n * p.planes * segs;
+  const int64_t segs = copy_segments(p.page_bytes), units = (int64_t)p.n * p.planes * segs;
   for (int64_t first = blockIdx.x; first < units; first += (int64_t)gridDim.x * kCopyThreads) {
     if (tid == 0) count = 0;
     __syncthreads();
@@ -571,7 +569,7 @@ cudaError_t launch_kv_write(const WriteParams& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_kv_copy_pages(const CopyParams& p, cudaStream_t stream) {
-  const int64_t segs = (p.page_bytes + kCopySeg - 1) / kCopySeg, units = (int64_t)p.n * p.planes * segs;
+  const int64_t segs = copy_segments(p.page_bytes), units = (int64_t)p.n * p.planes * segs;
   const int64_t most = sm_count() * 8;
   k_kv_copy_pages<<<(unsigned)(units < most ? units : most), kCopyThreads, 0, stream>>>(p);
   return cudaGetLastError();

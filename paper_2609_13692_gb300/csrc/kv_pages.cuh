@@ -37,6 +37,9 @@ struct CopyParams {
   const int32_t *src, *dst;
   int32_t planes, n_pages, n;
 };
+constexpr int kCopyThreads = 256, kCopyVecs = 4, kCopySeg = kCopyThreads * kCopyVecs * 16;
+// Units of a page in one plane; the units of all pairs and planes are counted in 64 bits.
+__host__ __device__ constexpr int64_t copy_segments(int64_t page_bytes) { return (page_bytes + kCopySeg - 1) / kCopySeg; }
 cudaError_t launch_kv_copy_pages(const CopyParams& p, cudaStream_t stream);
 
 struct BookParams {

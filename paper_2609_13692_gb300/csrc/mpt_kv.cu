@@ -298,7 +298,7 @@ mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, i
     return MPT_ERR_INVALID_ARG;
   if (!mpt::aligned(pool, 16) || plane_stride % 16 || page_stride % 16 || page_bytes % 16) return MPT_ERR_INVALID_ARG;
   if (n_pages >= 1 << 30 || n >= 1 << 30 || planes > 1 << 16 || page_bytes > (int64_t)1 << 32 || page_stride > (int64_t)1 << 32 ||
-      plane_stride > (int64_t)1 << 46)
+      plane_stride > (int64_t)1 << 46 || (int64_t)n * planes > (INT64_MAX >> 1) / mpt::copy_segments(page_bytes))
     return MPT_ERR_TOO_LARGE;
   if (n == 0) return MPT_OK;
   if (!src || !dst || !mpt::aligned(src, 4) || !mpt::aligned(dst, 4)) return MPT_ERR_INVALID_ARG;
