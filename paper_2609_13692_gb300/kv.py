@@ -9,6 +9,9 @@ every step runs in the kernels of ``libmpt.so``.
 Calls enqueue on ``stream`` (a raw stream address; default: torch's current stream) and return
 without waiting.  What a call allocates (its outputs and workspace) belongs to that stream; inputs
 that other streams write have to be ready in it, as for any torch operation.
+
+There is no backward pass: where gradients are recorded, a tensor that requires one is refused
+(use ``torch.no_grad()`` or ``torch.inference_mode()``).
 """
 
 from __future__ import annotations
@@ -64,6 +67,13 @@ def _device(first, *others) -> int:
     if index < 0:
         raise ValueError("every tensor must be on the same CUDA device")
     return index
+
+
+def _no_grad(*tensors):
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("there is no backward pass: call it under torch.no_grad(), or detach what requires gradients")
 
 
 def _ints(t, name: str):
@@ -137,6 +147,7 @@ def mpt_kv_attend(q, k_pages, v_pages, page_table, q_offsets, kv_lens, *, max_q_
     out: [tokens, heads, head_dim] of q's type; lse: float32[tokens, heads], natural logarithm.
     A row that sees no key gets out = 0, lse = -inf; tokens of no request are not written."""
     index = _device(q, k_pages, v_pages, page_table, q_offsets, kv_lens)
+    _no_grad(q, k_pages, v_pages, out, lse)
     cache, dtype, _, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
     shape = q.shape
     if len(shape) != 3 or q.dtype is not dtype or shape[2] != dim:
@@ -192,6 +203,7 @@ def mpt_kv_merge(outs, lses, *, out=None, lse=None, stream: Optional[int] = None
     if n != nl or rows != shape[:-1] or ldtype is not _F32:
         raise ValueError("lses must be as many float32 tensors as outs, of their shape without the last axis")
     index = _device(o, z)
+    _no_grad(out, lse)
     if out is not None:
         _device(o, out)
         if out.shape != shape or out.dtype is not dtype or not out.is_contiguous():
@@ -210,6 +222,7 @@ def _addresses(at: list) -> bytes:
 def _parts(parts, name: str):
     """(number, packed addresses, shape, type, a tensor) of equal contiguous parts."""
     if isinstance(parts, torch.Tensor):
+        _no_grad(parts)
         shape = parts.shape
         if not shape or shape[0] < 1 or not parts.is_contiguous():
             raise ValueError(f"{name} must be contiguous parts, one at least")
@@ -220,6 +233,7 @@ def _parts(parts, name: str):
         raise ValueError(f"{name} must not be empty")
     first, n = parts[0], len(parts)
     _device(first, *parts)
+    _no_grad(*parts)
     for t in parts:
         if t.shape != first.shape or t.dtype is not first.dtype or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous and of one shape and type")
@@ -241,6 +255,7 @@ def mpt_kv_write(k_new, v_new, k_pages, v_pages, page_table, q_offsets, kv_lens,
     """Write the new tokens' keys and values ([tokens, kv_heads, head_dim], the cache's type) into
     their pages: the last q_offsets[i+1] - q_offsets[i] of request i's kv_lens[i] positions."""
     index = _device(k_pages, v_pages, page_table, q_offsets, kv_lens, k_new, v_new)
+    _no_grad(k_new, v_new, k_pages, v_pages)
     cache, dtype, kv_heads, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
     shape = k_new.shape
     if len(shape) != 3 or shape[1] != kv_heads or shape[2] != dim or v_new.shape != shape or k_new.dtype is not dtype or v_new.dtype is not dtype:
@@ -345,6 +360,7 @@ def mpt_kv_copy_pages(pool, src, dst, *, stream: Optional[int] = None) -> None:
     """Copy pages src[j] -> dst[j] in every plane of ``pool`` ([planes, n_pages, ...], a page
     contiguous); pairs with an id out of range (-1) are skipped.  No dst may be a page of another pair."""
     index = _device(pool, src, dst)
+    _no_grad(pool)
     _ints(src, "src")
     _ints(dst, "dst")
     if src.shape != dst.shape:

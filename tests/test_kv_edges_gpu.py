@@ -127,3 +127,35 @@ def test_many_keys_of_small_weight(kv, dtype, dim, q_len, group):  # noqa: F811
             tol = tol + 2.0 ** -36 * p[0] * x.abs().sum(0)
         assert bool(((out.double() - want).abs() <= tol).all()), weight
         assert float((lse.double() - z).abs().max()) <= err + 2.0 ** -20 + 2.0 ** -21 * float(z)
+
+
+def test_gradients_are_refused(kv):  # noqa: F811
+    """There is no backward pass: tensors that require gradients are taken only where none are recorded."""
+    c = make(33, [1, 40], [30, 70], 4, 2, 64, 16, BF16)
+    out, lse = kv.mpt_kv_attend(*args(c))
+    parts, sums = torch.stack([out, out]), torch.stack([lse, lse])
+    want = kv.mpt_kv_merge(parts, sums)
+    new = c["k"][0, :1].clone()
+    one = (c["table"][:1], torch.tensor([0, 1], dtype=torch.int32, device="cuda"), c["lens"][:1])
+    pages = torch.zeros((1, 4, 16, 2, 64), dtype=BF16, device="cuda")
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def req(t):
+        return t.detach().clone().requires_grad_()
+
+    calls = [lambda: kv.mpt_kv_attend(*args(dict(c, q=req(c["q"])))), lambda: kv.mpt_kv_attend(*args(dict(c, k=req(c["k"])))),
+             lambda: kv.mpt_kv_attend(*args(dict(c, v=req(c["v"])))), lambda: kv.mpt_kv_attend(*args(c), out=req(out)),
+             lambda: kv.mpt_kv_attend(*args(c), lse=req(lse)), lambda: kv.mpt_kv_merge(req(parts), sums),
+             lambda: kv.mpt_kv_merge(parts, req(sums)), lambda: kv.mpt_kv_merge([out, req(out)], [lse, lse]),
+             lambda: kv.mpt_kv_merge(iter([out, out]), iter([req(lse), lse])), lambda: kv.mpt_kv_merge(parts, sums, out=req(out)),
+             lambda: kv.mpt_kv_write(req(new), new, c["k"], c["v"], *one), lambda: kv.mpt_kv_write(new, req(new), c["k"], c["v"], *one),
+             lambda: kv.mpt_kv_copy_pages(req(pages), ids, ids)]
+    for call in calls:
+        with pytest.raises(ValueError, match="no backward"):
+            call()
+    with torch.no_grad():
+        got = kv.mpt_kv_attend(*args(dict(c, q=req(c["q"]))))
+        assert torch.equal(got[0], out) and not got[0].requires_grad
+        assert torch.equal(kv.mpt_kv_merge(req(parts), sums)[0], want[0])
+    with torch.inference_mode():
+        assert torch.equal(kv.mpt_kv_attend(*args(c))[0], out)
