@@ -110,8 +110,9 @@ struct TileShared {
 static_assert(sizeof(TileShared) <= 2048);
 
 // Bounded wait of a whole warp: false once the block has given up, or after four
-// seconds.  The clock is looked at after the first polls only: reading it takes
-// longer than most waits.
+// seconds.  The block's end counts it (with an atomic at each of the waits the
+// long chunk took 20 to 40 us more).  The clock is looked at after the first
+// polls only: reading it takes longer than most waits.
 __device__ __forceinline__ bool wait_on(unsigned long long* bar, uint32_t parity, int* gave_up) {
   unsigned long long start = 0;
   for (;;) {
@@ -123,7 +124,6 @@ __device__ __forceinline__ bool wait_on(unsigned long long* bar, uint32_t parity
     if (now - start > 4000000000ull) {
       over = true;
       *(volatile int*)gave_up = 1;
-      atomicAdd(&g_tile_counts[kKvGaveUp], 1u);
     }
     if (__any_sync(~0u, over)) return false;
   }
@@ -156,7 +156,6 @@ __device__ __forceinline__ bool wait_spaced(unsigned long long* bar, uint32_t pa
     if (now - start > 4000000000ull) {
       over = true;
       *(volatile int*)gave_up = 1;
-      atomicAdd(&g_tile_counts[kKvGaveUp], 1u);
     }
     if (__any_sync(~0u, over)) return false;
   }
@@ -583,9 +582,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   };
 
   if (warp >= 8) {
-    // 2 x 208 + 88 = 3 x 168.  With 72 for these warps and 216 for the rows' the
-    // long chunk took 775 to 870 us, by how little the warps' code differed; with
-    // 88, 784 to 786.
+    // 2 x 208 + 88 = 3 x 168.  (72 for these warps and 216 for the rows': the
+    // ragged chunks 383 us, not 372, the long one 768, not 765.)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9 || warp == 10) {
       // ---- copies: warp 9 queries and keys, warp 10 values ----
@@ -1108,6 +1106,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   // last uses of the ring (all before them were released, so they have landed)
   // and the last queries.  They land before the block ends.
   if ((warp == 9 || warp == 10) && *(volatile int*)gave_up) {
+    if (tid == 9 * 32) atomicAdd(&g_tile_counts[kKvGaveUp], 1u);
     const uint32_t v = warp - 9, n = sh.sent[v], last = (C::kSlots + 1) / 2;
     for (uint32_t k = n > last ? n - last : 0; k < n; ++k) {
       const uint32_t idx = 2 * k + v;
