@@ -436,9 +436,9 @@ mpt_status mpt_alu_addmin_peak(int64_t ops, void* stream, double* ops_per_s);
 /* How this copy of the library was built, as bits in *flags: bit 0 set
  * means the bounds-checked variant (compiled with MPT_BOUNDS), whose kernels
  * test table indices, window offsets and split entries, skip any access that
- * fails and report MPT_ERR_INTERNAL from mpt_solve -- a stand-in for a
- * device memory checker, slower than the default build.  Not part of the
- * method.  Errors: INVALID_ARG (flags NULL). */
+ * fails and report MPT_ERR_INTERNAL from mpt_solve (from mpt_kv_check for the
+ * kernels of mpt_kv.h) -- a stand-in for a device memory checker, slower than
+ * the default build.  Not part of the method.  Errors: INVALID_ARG (flags NULL). */
 mpt_status mpt_build_info(int32_t* flags);
 
 /* Free the context and any workspace the library allocated.  NULL is a no-op. */

@@ -188,8 +188,9 @@ mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, i
 /* Waits for `stream`, then reports what kernels of this header met on the
  * current device, on any stream, that no call has reported: MPT_ERR_TIMEOUT
  * when a bounded wait on a shared-memory barrier gave up (the results of the
- * calls since the last MPT_OK are not to be used), MPT_OK otherwise.
- * Errors also: CUDA. */
+ * calls since the last MPT_OK are not to be used), MPT_ERR_INTERNAL when an
+ * index failed its check in the bounds-checked build (mpt_build_info; the
+ * access was left out), MPT_OK otherwise.  Errors also: CUDA. */
 mpt_status mpt_kv_check(void* stream);
 
 #ifdef __cplusplus

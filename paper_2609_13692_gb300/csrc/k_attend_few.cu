@@ -139,6 +139,11 @@ __device__ __forceinline__ FewItem few_item(const AttnParams& p, const AttnReq& 
   return it;
 }
 
+// Bounds-checked build: row `row` of the item's request lies in the call's tensors.
+__device__ __forceinline__ bool few_inside(const AttnParams& p, const FewItem& x, int row) {
+  return attn_inside(p, x.req, x.head, x.r.q0, x.r.ql, x.r.kvl) && row >= 0 && row / p.group < x.r.ql;
+}
+
 template <int HDP, bool F16>
 __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_attend_few(const __grid_constant__ AttnParams p) {
   using C = FewCfg<HDP>;
@@ -229,6 +234,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
         const int slot = ((t * kKeys) & ((1 << p.page_log2) - 1));  // pages larger than a stage
         for (int q = lane; q < per * kBlk * 2; q += 32) {
           const int b = q / per % kBlk, v = q / per / kBlk;
+          if (KV_BAD(g_few_counts, id >= -1 && id < p.n_pages && x.head < p.kv_heads && slot < 1 << p.page_log2 && b < kBlk)) continue;
           tma_load_4d(dst + v * (C::kStage / 2) + b * kKeys * 128 + mine * box * 128, v ? &p.map_v : &p.map_k, b * 64,
                       slot, x.head, id, &full[s]);
         }
@@ -273,7 +279,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int row = x.row0 + g + 8 * h;
-      const bool valid = g + 8 * h < x.rows;
+      const bool valid = g + 8 * h < x.rows && !KV_BAD(g_few_counts, few_inside(p, x, row));
       lim[h] = valid ? attn_limit(p, r, row / p.group) : 0;
       qrow[h] = valid ? p.q + 2 * ((int64_t)(r.q0 + row / p.group) * p.q_tok +
                                    ((int64_t)x.head * p.group + row % p.group) * p.q_head)
@@ -294,7 +300,7 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
       for (int e = tid; e < kRows * (HDP / 8); e += C::kWarps * 32) {
         const int row = e / (HDP / 8), col = e % (HDP / 8) * 8, abs = x.row0 + row;
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < x.rows && col < p.dim)
+        if (row < x.rows && col < p.dim && !KV_BAD(g_few_counts, few_inside(p, x, abs)))
           v = *(const uint4*)(p.q + 2 * ((int64_t)(r.q0 + abs / p.group) * p.q_tok +
                                          ((int64_t)x.head * p.group + abs % p.group) * p.q_head + col));
         *(uint4*)(qs + row * C::kQPad + col) = v;
@@ -485,10 +491,12 @@ __global__ void __launch_bounds__(FewCfg<HDP>::kThreads, FewCfg<HDP>::kPerSm) k_
     }
     const bool whole = starts && ends;
     const int slot = blockIdx.x * 2 + (starts ? 1 : 0);
+    const bool outside = KV_BAD(g_few_counts, x.rows >= 1 && x.rows <= kRows && few_inside(p, x, x.row0) && few_inside(p, x, x.row0 + x.rows - 1) &&
+                                                  slot < 2 * (int)gridDim.x);
     float* part = p.part + (int64_t)slot * (kRows * HDP + 2 * kRows);
     for (int e = tid; e < kRows * (HDP / 8); e += C::kWarps * 32) {
       const int row = e / (HDP / 8), col = e % (HDP / 8) * 8;
-      if (row >= x.rows) continue;
+      if (row >= x.rows || outside) continue;
       float top = -INFINITY, sum = 0.f, v[8];
 #pragma unroll
       for (int w = 0; w < C::kWarps; ++w) top = fmaxf(top, ml[(w * 2) * kRows + row]);
@@ -550,7 +558,11 @@ __global__ void __launch_bounds__(128) k_attend_few_join(const __grid_constant__
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_for_primary();
   const int4 d = p.desc[blockIdx.x];
-  const int rows = d.z >> 16, head0 = d.z & 0xFFFF, parts = d.w;
+  const int rows = d.z >> 16, head0 = d.z & 0xFFFF;
+  const int parts = KV_BAD(g_few_counts, d.w >= 0 && d.w <= (int)(gridDim.x - blockIdx.x) && rows <= kRows && head0 < p.kv_heads &&
+                                             d.x + (d.y + rows - (d.w > 0)) / p.group < p.tokens)
+                        ? 0
+                        : d.w;
   // part k: block c's last segment, then the first segments of the following blocks
   const float* const base = p.part + (int64_t)blockIdx.x * 2 * kSlot;
   auto slot = [&](int k) { return base + (int64_t)(k == 0 ? 1 : 2 * k) * kSlot; };

@@ -407,6 +407,11 @@ __device__ void fill_list(const AttnParams& p, TileShared& sh) {
   }
   const int64_t left = sh.left, open = left - (inc - mine);
   e.seg = (int)(open < 0 ? 0 : open < mine ? open : mine);
+  if (kBoundsChecked) {  // the list ends before an entry that is out of range
+    const bool bad = KV_BAD(g_tile_counts, e.seg == 0 || (attn_inside(p, e.req, e.head, e.q0, e.ql, e.kvl) && e.pair >= 0 &&
+                                                          (int64_t)e.pair * p.item_toks < e.ql && e.t0 >= 0 && e.t0 + e.seg <= cost));
+    if (__ballot_sync(~0u, bad) & ((2u << lane) - 1u)) e.seg = 0;
+  }
   const int n_used = __popc(__ballot_sync(~0u, e.seg > 0));  // a run from lane 0
   __syncwarp();
   if (e.seg > 0) sh.list[lane] = e;
@@ -416,6 +421,10 @@ __device__ void fill_list(const AttnParams& p, TileShared& sh) {
     sh.count = n_used;
     sh.left = left - taken;
     sh.more = n_used == kList && left > taken;
+    if (kBoundsChecked && n_used == 0) {  // a list has an entry: one without rows
+      sh.list[0] = {0, 0, 0, 0, 0, 0, 1, 0};
+      sh.count = 1;
+    }
     // after a full list whose last item is whole: the one that follows it in its column
     sh.t0 = 0;
     sh.item = item + n < items ? item + n : column + 1;
@@ -659,6 +668,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             if (elect_one()) {
 #pragma unroll
               for (int b = 0; b < C::kBlk; ++b)
+                if (!KV_BAD(g_tile_counts, page >= -1 && page < p.n_pages && slot < 1 << p.page_log2 && i < per))
                 tma_load_4d(dst + b * kKeys * 128 + i * box * 128, map, b * 64, slot, head, page, &sh.full[s]);
             }
           }
@@ -869,7 +879,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
                 wrote = true;
                 if (lane < kChunks) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(mine + row * 128), "r"(0) : "memory");
                 const int key = key0 + row, a = key - w.lim_first;  // a < 256 for every token of the item
-                if (lane == 0 && key < w.e.kvl && a < 256) {
+                if (lane == 0 && key < w.e.kvl && a < 256 && !KV_BAD(g_tile_counts, a >= 0 && row < kKeys)) {
                   odd[a >> 5] |= 1u << (a & 31);
                   odd[8] = 1;
                 }
@@ -1023,6 +1033,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         const bool extra = odd && w.count(s) > 0 && odd[8];
         const float inv = l == 0.f ? 0.f : 1.f / l, scale = whole ? inv : 1.f;
         const int64_t tok_at = (int64_t)w.e.q0 + tok, head = (int64_t)w.e.head * p.group + sub;
+        const bool inside = valid && !KV_BAD(g_tile_counts, tok_at >= 0 && tok_at < p.tokens && head >= 0 && head < p.heads);
         char* const out = p.out + 2 * (tok_at * p.out_tok + head * p.out_head);
         float* part = p.part + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * (C::kRows * HDP + 2 * C::kRows);
         for (int c = 0; c < HDP / 32; ++c) {
@@ -1040,6 +1051,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             for (int a = 0; a < 256; ++a) {
               if (!(odd[a >> 5] >> (a & 31) & 1u) || a >= lim - w.lim_first) continue;
               const int key = w.lim_first + a;
+              if (KV_BAD(g_tile_counts, key >= 0 && key < w.e.kvl)) continue;
               const int64_t id = p.table[(int64_t)w.e.req * p.table_stride + (key >> p.page_log2)];
               if (id < 0 || id >= p.n_pages) continue;
               const int64_t slot = key & ((1 << p.page_log2) - 1);
@@ -1064,11 +1076,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             uint32_t v[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] = pack2<F16>(o[2 * e] * scale, o[2 * e + 1] * scale);
-            if (valid && p.wide) {  // whole 32-byte sectors
+            if (inside && p.wide) {  // whole 32-byte sectors
 #pragma unroll
               for (int e = 0; e < 2; ++e)
                 if (32 * c + 16 * e < p.dim) store32(out + 2 * (32 * c + 16 * e), v + 8 * e);
-            } else if (valid) {
+            } else if (inside) {
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (32 * c + 8 * e < p.dim)
@@ -1082,7 +1094,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           }
         }
         if (whole) {
-          if (valid && p.lse) p.lse[tok_at * p.heads + head] = L<F16>::lse(m, l);
+          if (inside && p.lse) p.lse[tok_at * p.heads + head] = L<F16>::lse(m, l);
         } else {
           part[C::kRows * HDP + s * 128 + r] = m;
           part[C::kRows * HDP + C::kRows + s * 128 + r] = l;
@@ -1126,6 +1138,8 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
   wait_for_primary();
   const int4 d = p.desc[blockIdx.x];
   if (d.w == 0) return;
+  if (KV_BAD(g_tile_counts, d.w > 0 && d.w <= (int)(gridDim.x - blockIdx.x) && d.x >= 0 && d.x < p.batch && d.y >= 0 && d.y < p.kv_heads && d.z >= 0))
+    return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const AttnReq r = attn_req(p, d.x);
   const int slot_row = blockIdx.y * 32 + lane, s = slot_row >> 7, row = slot_row & 127;

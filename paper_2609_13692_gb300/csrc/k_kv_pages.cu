@@ -12,6 +12,8 @@ namespace cg = cooperative_groups;
 namespace mpt {
 namespace {
 
+__device__ uint32_t g_pages_counts[kKvCounts];
+
 // ---------------------------------------------------------------------------
 // Merge: out = sum_p exp(lse_p - lse) out_p
 // ---------------------------------------------------------------------------
@@ -73,6 +75,7 @@ __global__ void __launch_bounds__(256) k_kv_merge(const __grid_constant__ MergeP
   const int64_t all = p.rows * p.vecs;
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
     const int64_t row = all < (1ll << 32) ? (int64_t)((uint32_t)at / (uint32_t)p.vecs) : at / p.vecs;
+    if (KV_BAD(g_pages_counts, row >= 0 && row < p.rows && at - row * p.vecs >= 0 && at - row * p.vecs < p.vecs)) continue;
     uint4 u[kParts ? kParts : 1];
     float s[kParts ? kParts : 1];
     float top = -INFINITY, sum = 0.f, acc[V::kN];
@@ -148,6 +151,7 @@ __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ WriteP
   const int page = p.table[(int64_t)lo * p.table_stride + (pos >> p.page_log2)];
   if (page < 0 || page >= p.n_pages) return;
   const int64_t slot = pos & ((1 << p.page_log2) - 1);
+  if (KV_BAD(g_pages_counts, q0 >= 0 && t < q1 && lo < p.batch && pos < (int64_t)p.width << p.page_log2 && slot >> p.page_log2 == 0)) return;
   const uint4* from;
   uint4* to;
   int64_t from_head, to_head;
@@ -187,7 +191,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_kv_copy_pages(const __grid_con
       const int64_t seg = unit % segs, pp = unit / segs;
       const int plane = (int)(pp % p.planes), j = (int)(pp / p.planes);
       const int s = p.src[j], d = p.dst[j];
-      if (s >= 0 && s < p.n_pages && d >= 0 && d < p.n_pages && s != d) {
+      if (s >= 0 && s < p.n_pages && d >= 0 && d < p.n_pages && s != d && !KV_BAD(g_pages_counts, j < p.n && plane < p.planes && seg * kCopySeg < p.page_bytes)) {
         const int at = atomicAdd(&count, 1);  // any order: each unit has bytes of its own
         const int64_t base = plane * p.plane_stride + seg * kCopySeg, rest = p.page_bytes - seg * kCopySeg;
         from[at] = base + s * p.page_stride;
@@ -411,6 +415,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
       for (int u = 0; u < 8; ++u) {
         if (r[u] < 0) continue;
         const int id = id0 + 32 * u + lane;
+        if (KV_BAD(g_pages_counts, x[u] >= 0 && x[u] < b.rows && y[u] >= 0 && y[u] < b.width && id < b.n_pages && j[u] < p.n)) continue;
         b.table[(int64_t)x[u] * b.table_stride + y[u]] = id;
         b.refs[id] = 1;
         if (OP == kBookFork) p.copy_dst[j[u]] = id;
@@ -420,7 +425,10 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   if (OP == kBookFork) cl.sync();  // counts are read above: a row may name a page whose count is 0
   if (flags == 0 && OP != kBookExtend) {
     for (int j = kScanWarps - 1 - gw; j < p.n; j += kScanWarps) {  // the last warps have no pages to hand out
-      const int row = OP == kBookFork ? p.l1[j] : p.l0[j], keep = OP == kBookFork ? p.l2[j] : b.lens[row];
+      const int row = OP == kBookFork ? p.l1[j] : p.l0[j];
+      if (KV_BAD(g_pages_counts, row >= 0 && row < b.rows && (OP != kBookFork || (p.l0[j] >= 0 && p.l0[j] < b.rows)))) continue;
+      const int keep = OP == kBookFork ? p.l2[j] : b.lens[row];
+      if (KV_BAD(g_pages_counts, keep >= 0 && keep <= room)) continue;
       int32_t* to = b.table + (int64_t)row * b.table_stride;
       const int32_t* from = OP == kBookFork ? b.table + (int64_t)p.l0[j] * b.table_stride : to;
       // Fork: the full pages, beside which entry `have` is written above if the rest is on a page.
@@ -452,7 +460,10 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
   }
   cl.sync();  // nobody reads the first block's shared memory, or a row's old length, any more
   if (OP == kBookExtend && flags == 0)
-    for (int j = gw * 32 + lane; j < p.n; j += kScanWarps * 32) b.lens[p.l0[j]] += p.l1[j];
+    for (int j = gw * 32 + lane; j < p.n; j += kScanWarps * 32) {
+      if (KV_BAD(g_pages_counts, p.l0[j] >= 0 && p.l0[j] < b.rows && (int64_t)b.lens[p.l0[j]] + p.l1[j] <= room)) continue;
+      b.lens[p.l0[j]] += p.l1[j];
+    }
   if (OP == kBookFree) {  // the pages that this call freed are counted too
     int n = 0, all;
 #pragma unroll 8
@@ -506,15 +517,17 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kBookThreads)
       const int id = id0 + 32 * u + lane;
       const bool in = id < run.hi, on = f[u] >> lane & 1u;
       const int ahead = before + __popc(f[u] & ((1u << lane) - 1u));  // live pages of a lower id
-      if (in && !on && id < n_live) p.copy_dst[id - ahead] = id;
-      if (on && id >= n_live) p.copy_src[ahead - stay] = id;
+      if (in && !on && id < n_live && !KV_BAD(g_pages_counts, id - ahead >= 0 && id - ahead < half)) p.copy_dst[id - ahead] = id;
+      if (on && id >= n_live && !KV_BAD(g_pages_counts, ahead - stay >= 0 && ahead - stay < half)) p.copy_src[ahead - stay] = id;
       before += __popc(f[u]);
     }
   }
   for (int k = moves + rank * kBookThreads + tid; k < half; k += all_threads) p.copy_src[k] = p.copy_dst[k] = -1;
   cl.sync();
   for (int k = rank * kBookThreads + tid; k < moves; k += all_threads) {
+    if (KV_BAD(g_pages_counts, k < half)) continue;
     const int s = p.copy_src[k], d = p.copy_dst[k];
+    if (KV_BAD(g_pages_counts, s >= n_live && s < b.n_pages && d >= 0 && d < n_live)) continue;
     b.refs[d] = b.refs[s];
     b.refs[s] = 0;
   }
@@ -592,6 +605,12 @@ cudaError_t launch_kv_book(const BookParams& p, BookOp op, cudaStream_t stream) 
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, k_kv_remap, p);
+}
+
+cudaError_t kv_pages_counts(cudaStream_t stream, uint32_t* counts) {
+  void* at = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&at, g_pages_counts);
+  return e != cudaSuccess ? e : cudaMemcpyAsync(counts, at, sizeof(g_pages_counts), cudaMemcpyDeviceToHost, stream);
 }
 
 }  // namespace mpt

@@ -58,7 +58,19 @@ cudaError_t kv_allow_smem(Kernel kernel, int bytes, int device, std::atomic<uint
 }
 
 // Events that kernels count on a device, for mpt_kv_check; nothing clears them.
-enum KvCount { kKvGaveUp, kKvCounts };  // blocks' waits that gave up
+enum KvCount {
+  kKvGaveUp,   // waits that gave up
+  kKvOutside,  // bounds-checked build: indices that failed their check
+  kKvCounts
+};
+
+// Bounds-checked build: counts an index that is out of range; the caller then
+// skips the access.  The constant false in the default build.
+#ifdef MPT_BOUNDS
+#define KV_BAD(counts, ok) (!(ok) && (atomicAdd(&(counts)[::mpt::kKvOutside], 1u), true))
+#else
+#define KV_BAD(counts, ok) false
+#endif
 
 // One request's lengths, clamped to what the token axis and the table hold.
 struct AttnReq {
@@ -81,6 +93,12 @@ __device__ __forceinline__ AttnReq attn_req(const AttnParams& p, int i) {
 // Offsets that decrease could give many requests the same tokens, and a call
 // more work than its tensors can hold: such a call does nothing.
 __device__ __forceinline__ bool attn_falls(const AttnParams& p, int i) { return p.q_offsets[i + 1] < p.q_offsets[i]; }
+
+// Bounds-checked build: an item's request and rows lie in the call's tensors.
+__device__ __forceinline__ bool attn_inside(const AttnParams& p, int req, int head, int q0, int ql, int kvl) {
+  return req >= 0 && req < p.batch && head >= 0 && head < p.kv_heads && q0 >= 0 && ql > 0 && (int64_t)q0 + ql <= p.tokens && kvl >= 0 &&
+         kvl <= (int64_t)p.width << p.page_log2;
+}
 
 // Keys that token t of the request may see: j < the returned value.
 __device__ __forceinline__ int attn_limit(const AttnParams& p, const AttnReq& r, int t) {

@@ -52,4 +52,7 @@ constexpr int kBookList = 16384;  // entries of a list, at most: 4 bytes of shar
 enum BookOp { kBookFork, kBookExtend, kBookFree, kBookCompact };
 cudaError_t launch_kv_book(const BookParams& p, BookOp op, cudaStream_t stream);
 
+// The kernels' counts (in the default build they have none to make).
+cudaError_t kv_pages_counts(cudaStream_t stream, uint32_t* counts);
+
 }  // namespace mpt

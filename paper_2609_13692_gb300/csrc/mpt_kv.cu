@@ -311,15 +311,18 @@ mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, i
 }
 
 mpt_status mpt_kv_check(void* stream_ptr) {
-  static mpt::Reported few, tile;
+  static mpt::Reported few, tile, outside[3];
   cudaStream_t stream = (cudaStream_t)stream_ptr;
-  uint32_t f[mpt::kKvCounts], t[mpt::kKvCounts];
+  uint32_t f[mpt::kKvCounts], t[mpt::kKvCounts], g[mpt::kKvCounts];
   int device = 0;
   if (cudaGetDevice(&device) != cudaSuccess || mpt::attend_few_counts(stream, f) != cudaSuccess ||
-      mpt::attend_tile_counts(stream, t) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
+      mpt::attend_tile_counts(stream, t) != cudaSuccess || mpt::kv_pages_counts(stream, g) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
     return MPT_ERR_CUDA;
   const bool in_few = few.news(device, f[mpt::kKvGaveUp]), in_tile = tile.news(device, t[mpt::kKvGaveUp]);
-  return in_few || in_tile ? MPT_ERR_TIMEOUT : MPT_OK;
+  bool bad = false;
+  const uint32_t* const counts[3] = {f, t, g};
+  for (int i = 0; i < 3; ++i) bad |= outside[i].news(device, counts[i][mpt::kKvOutside]);
+  return bad ? MPT_ERR_INTERNAL : in_few || in_tile ? MPT_ERR_TIMEOUT : MPT_OK;
 }
 
 }  // extern "C"
