@@ -1,13 +1,14 @@
 """The paged-cache operators at the edges of their ranges, against the models of tests/kv_model.py."""
 
 import math
+import random
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
 from tests import kv_model as M
-from tests.test_kv_attend_gpu import BF16, F16, args, kv, make  # noqa: F401 (kv: the fixture)
+from tests.test_kv_attend_gpu import BF16, F16, args, check, kv, make  # noqa: F401 (kv: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -159,3 +160,53 @@ def test_gradients_are_refused(kv):  # noqa: F811
         assert torch.equal(kv.mpt_kv_merge(req(parts), sums)[0], want[0])
     with torch.inference_mode():
         assert torch.equal(kv.mpt_kv_attend(*args(c))[0], out)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(82, 2, 64), (43, 1, 256), (65, 1, 128), (200, 2, 96), (128, 1, 128), (128, 1, 200)])
+def test_large_groups(kv, heads, kv_heads, dim):  # noqa: F811
+    """41 to 128 query heads of a KV head: row tiles of three, two and one whole tokens."""
+    for causal in (True, False):
+        check(kv, make(34, [1, 1, 0, 1], [300, 1, 5, 130], heads, kv_heads, dim, 16, BF16, poison=True), causal, hint=1)
+        check(kv, make(35, [1, 7, 2, 30], [64, 7, 1, 257], heads, kv_heads, dim, 32, F16, holes=0.2, poison=True), causal, hint=30)
+
+
+def test_chunks_of_more_requests_than_the_large_kernel_lists(kv):  # noqa: F811
+    """Above 8,192 requests the small kernel takes chunks too."""
+    rng = random.Random(36)
+    q_lens = [rng.choice([1, 3, 17, 70]) if i % 41 == 0 else 0 for i in range(8_200)]
+    kv_lens = [max(0, n + rng.choice([-2, 0, 9, 150])) if n else i % 2 for i, n in enumerate(q_lens)]
+    for dim, dtype in ((64, BF16), (256, F16)):
+        check(kv, make(36, q_lens, kv_lens, 4, 2, dim, 16, dtype, poison=True), hint=70)
+
+
+def test_calls_on_two_streams_at_once(kv):  # noqa: F811
+    """Two streams in turn and together, each with outputs and a workspace of its own."""
+    cases = [make(37, [1] * 20, [3_000] * 20, 8, 2, 128, 16, BF16), make(38, [300, 1, 40], [4_000, 900, 333], 8, 2, 128, 16, BF16),
+             make(39, [1, 1], [60_000, 5], 4, 4, 64, 64, F16), make(40, [90], [9_000], 4, 2, 256, 16, F16)]
+    hints = [1, 300, 1, 90]
+    want = [kv.mpt_kv_attend(*args(c), max_q_len=h) for c, h in zip(cases, hints)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for first, second in ((0, 1), (1, 2), (3, 1), (1, 1), (0, 0)):
+        mine = []
+        for i in (first, second):
+            c = cases[i]
+            ws = torch.empty(kv.mpt_kv_attend_workspace_bytes(c["q"].shape[2]), dtype=torch.uint8, device="cuda")
+            mine.append((i, [(torch.empty_like(c["q"]), torch.empty(c["q"].shape[:2], device="cuda")) for _ in range(8)], ws))
+        torch.cuda.synchronize()
+        for n in range(8):
+            for s, (i, outs, ws) in zip(streams, mine):
+                kv.mpt_kv_attend(*args(cases[i]), max_q_len=hints[i], out=outs[n][0], lse=outs[n][1], workspace=ws, stream=s.cuda_stream)
+        torch.cuda.synchronize()
+        kv.mpt_kv_check()
+        for i, outs, _ in mine:
+            for out, lse in outs:
+                assert torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1]), (first, second, i)
+
+
+@pytest.mark.parametrize("q_len,dim", [(1, 128), (1, 256), (50, 64), (50, 256)])
+def test_heads_before_tokens(kv, q_len, dim):  # noqa: F811
+    """q and out stored head by head: the heads' stride is the larger one."""
+    c = make(41, [q_len, 1, q_len], [77, 500, 250], 6, 2, dim, 16, BF16, "head")
+    c["q"] = c["q"].transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.empty((6, c["q"].shape[0], dim), dtype=BF16, device="cuda").transpose(0, 1)
+    check(kv, c, hint=q_len, out=out)
