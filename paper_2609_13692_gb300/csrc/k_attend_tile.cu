@@ -84,6 +84,11 @@ struct TileCfg {
   // two slots the next key tile is the slot's next phase, and a wait for it
   // before the one at hand has landed would pass at once.
   static constexpr bool kWatchKeys = kSlots > 2;
+  // Registers a thread: of the four warps without rows, and of the rows' eight.
+  // (Of 88 with 208 and 72 with 216: 2,048 tokens over 10,000 keys, heads of 64,
+  // 200 and 180 us; 28 ragged chunks, heads of 96, 372 and 383.)
+  static constexpr int kRoleRegs = HDP == 64 ? 72 : 88, kRowRegs = HDP == 64 ? 216 : 208;
+  static_assert(kRoleRegs + 2 * kRowRegs <= 3 * 168);
   static constexpr int kSmem = 1024 + kQ + kSlots * kSlot + 2048;
 };
 
@@ -591,9 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   };
 
   if (warp >= 8) {
-    // 2 x 208 + 88 = 3 x 168.  (72 for these warps and 216 for the rows': the
-    // ragged chunks 383 us, not 372, the long one 768, not 765.)
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
     if (warp == 9 || warp == 10) {
       // ---- copies: warp 9 queries and keys, warp 10 values ----
       // Tile g of the block (over all its items) has its keys in use 2 g of the
@@ -907,7 +910,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       if (!ok) leave();
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRowRegs));
     // ---- one row per thread ----
     TileItem w;
     int k = 0;
@@ -1189,11 +1192,11 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
 template <int HDP, bool F16>
 cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream) {
   using C = TileCfg<HDP>;
-  // the warpgroups' shares (2 x 208 + 88) have to fit the registers of the launch, or they would wait for ever
+  // the warpgroups' shares have to fit the registers of the launch, or they would wait for ever
   static const cudaError_t fits = [] {
     cudaFuncAttributes a;
     const cudaError_t e = cudaFuncGetAttributes(&a, k_attend_tile<HDP, F16>);
-    return e != cudaSuccess ? e : a.numRegs * 3 >= 2 * 208 + 88 ? cudaSuccess : cudaErrorInvalidConfiguration;
+    return e != cudaSuccess ? e : a.numRegs * 3 >= C::kRoleRegs + 2 * C::kRowRegs ? cudaSuccess : cudaErrorInvalidConfiguration;
   }();
   if (fits != cudaSuccess) return fits;
   static std::atomic<uint64_t> allowed;
