@@ -61,7 +61,7 @@ typedef struct mpt_kv_cache {
   const int32_t* page_table; /* [batch][table_stride] */
   int64_t table_stride;
   int32_t table_width; /* entries of a row, >= 1; table_width * page_size < 2^31 */
-  const int32_t* q_offsets; /* [batch + 1], from 0, not decreasing (or attention does nothing) */
+  const int32_t* q_offsets; /* [batch + 1], from 0, not decreasing (or attention does nothing, and writes drop tokens) */
   const int32_t* kv_lens;   /* [batch] */
 } mpt_kv_cache;
 

@@ -145,13 +145,13 @@ __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ WriteP
   }
   if (lo >= p.batch) return;
   const int64_t q0 = p.q_offsets[lo], q1 = p.q_offsets[lo + 1];
-  if (t < q0) return;
+  if (t < q0 || t >= q1) return;  // the latter only where offsets decrease
   const int64_t pos = (int64_t)p.kv_lens[lo] - (q1 - q0) + (t - q0);
   if (pos < 0 || pos >> p.page_log2 >= p.width) return;
   const int page = p.table[(int64_t)lo * p.table_stride + (pos >> p.page_log2)];
   if (page < 0 || page >= p.n_pages) return;
   const int64_t slot = pos & ((1 << p.page_log2) - 1);
-  if (KV_BAD(g_pages_counts, q0 >= 0 && t < q1 && lo < p.batch && pos < (int64_t)p.width << p.page_log2 && slot >> p.page_log2 == 0)) return;
+  if (KV_BAD(g_pages_counts, t < p.tokens && pos >= 0 && pos < (int64_t)p.width << p.page_log2 && slot >> p.page_log2 == 0)) return;
   const uint4* from;
   uint4* to;
   int64_t from_head, to_head;

@@ -13,8 +13,8 @@ import pytest
 torch = pytest.importorskip("torch")
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
-CASES = ("page_sizes or holes or see_nothing or not_finite or many_requests or long_keys or out_of_range or noted_values or decrease "
-         "or large_groups or more_requests or write or bookkeeping or copy_pages or merge or layout_is_served")
+CASES = ("page_sizes or holes or see_nothing or not_finite or many_requests or long_keys or out_of_range or noted_values "
+         "or decrease or large_groups or more_requests or write or bookkeeping or copy_pages or merge or layout_is_served")
 
 CHILD = textwrap.dedent(r"""
     import sys

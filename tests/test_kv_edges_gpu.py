@@ -210,3 +210,19 @@ def test_heads_before_tokens(kv, q_len, dim):  # noqa: F811
     c["q"] = c["q"].transpose(0, 1).contiguous().transpose(0, 1)
     out = torch.empty((6, c["q"].shape[0], dim), dtype=BF16, device="cuda").transpose(0, 1)
     check(kv, c, hint=q_len, out=out)
+
+
+def test_writes_by_offsets_that_decrease(kv):  # noqa: F811
+    """Tokens that the offsets give to no request, as they are looked up, are dropped."""
+    at = [4, 6, 2, 3]
+    batch, tokens, page = 3, 8, 8
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pool = torch.zeros((2, 9, page, 1, 8), dtype=BF16, device="cuda")
+    new = torch.ones((tokens, 1, 8), dtype=BF16, device="cuda")
+    kv.mpt_kv_write(new, new, pool[0], pool[1], torch.arange(9, **i32).view(3, 3), torch.tensor(at, **i32),
+                    torch.full((batch,), 20, **i32))
+    kv.mpt_kv_check()
+    for side in pool:
+        written = side[:, :, 0, 0].reshape(batch, 3 * page).nonzero().tolist()
+        allowed = {(i, 20 - (at[i + 1] - at[i]) + t - at[i]) for i in range(batch) for t in range(max(at[i], 0), min(at[i + 1], tokens))}
+        assert {tuple(x) for x in written} <= allowed
