@@ -20,9 +20,10 @@
 // of 200 to 400 keys: 57 us, 78 with one block of eight such warps).
 //
 // Measured (one GB300, 8 KV heads of 128): 3 requests of 100,001 to 131,072 keys,
-// pages of 64: 204 us, 6.6 TB/s, 0.97 of the measured copy rate; 28 of 2,000 to
-// 6,000, pages of 16: 79 us, 5.8 TB/s, 12 us of it start, end and join; one of
-// 777: 9.9 us, launches and a chain of dependent reads.
+// pages of 64: 203 us, 6.6 TB/s, 0.97 of the measured copy rate; 28 of 2,000 to
+// 6,000, pages of 16: 79 us, 5.8 TB/s, 12 us of it start, end and join (16 KV heads
+// of 64, 64 requests: 207 us, 5.2 TB/s; 8 of 256: 148 us, 6.2 TB/s); one of 777:
+// 9.8 us, launches and a chain of dependent reads.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -14,15 +14,17 @@
 // products run, the other's probabilities are computed.
 //
 // Measured (one GB300, 32 query heads on 8 KV heads of 128, pages of 16): 4,096
-// tokens over 20,480 keys 0.78 ms, 1.60 PFLOP/s, 0.86 of the measured matrix
-// rate; call after call 0.82 ms at the power limit (1,365 W, 1,950 MHz), 1.51
-// PFLOP/s, 0.87 of the sustained matrix rate.  28 requests of 28 to 685 tokens
-// over 700 to 6,000 keys, 24 heads of 96, a tenth of the pages absent: 0.38 ms.  On a smaller case at full clocks the tensor pipe is
-// busy 63 % of the time: a row tile's chain of scores, probabilities (about
+// tokens over 20,480 keys, call after call at the power limit, 0.83 ms, 1.49
+// PFLOP/s, 0.87 of the sustained matrix rate; a few calls at full clocks 0.77 ms,
+// 1.61 PFLOP/s, 0.86 of the burst rate.  28 requests of 28 to 685 tokens over 700
+// to 6,000 keys, 24 heads of 96, a tenth of the pages absent: 0.37 ms.  2,048
+// tokens over 10,000 keys: heads of 64, 128 and 256 180, 220 and 600 us (floors
+// 81, 162 and 323).  On a smaller case at full clocks the tensor pipe is busy 63 %
+// of the time: a row tile's chain of scores, probabilities (about
 // 1,300 cycles, half of it exponentials), outputs and the hand-over between
 // warps takes 2,600 to 3,200 cycles, and only two such chains fit in tensor
 // memory.  Per key tile warp 8 spends 2,400 cycles on the pipe's 2,048 and 780
-// waiting for P.  An item costs 8 us besides (7 a block in the 0.38 ms): its last
+// waiting for P.  An item costs 8 us besides (7 a block in the 0.37 ms): its last
 // outputs, queries and first scores follow one another.
 //
 // Tried and slower: P handed over in halves (the products wait for the second
@@ -71,7 +73,7 @@ struct TileCfg {
   static constexpr int kBlk = HDP / 64;
   // Row tiles of an item: O takes HDP columns each, S 128, of 512.  With one, S
   // has two buffers, and the scores of the next key tile are made while P of this
-  // one is (2,048 tokens over 10,000 keys, 32 heads of 256: 719 -> 610 us).  For
+  // one is (2,048 tokens over 10,000 keys, 32 heads of 256: 719 -> 600 us).  For
   // single row tiles of smaller heads the same was slower (28 rows over 20,001
   // keys 43 -> 50 us): the ring then holds less ahead.
   static constexpr int kTiles = HDP == 256 ? 1 : 2;
@@ -146,7 +148,7 @@ __device__ __forceinline__ void bar_all() { asm volatile("bar.sync 1, 384;" ::: 
 // The same for the warps that have time: polls take issue slots that the rows'
 // arithmetic needs.  (4,096 tokens over 20,480 keys: 797 us with warp 11's polls
 // back to back, 770 with 20 to 400 ns between them; 20 ns between the copying
-// warps' polls for free slots: heads of 64 149 -> 141 us, the rest 0 to 1 %.  The
+// warps' polls for free slots: 772 -> 765 us, 28 ragged chunks 380 -> 372.  The
 // others' waits are on the chain, and any longer sleep costs.)
 template <int kNs>
 __device__ __forceinline__ bool wait_spaced(unsigned long long* bar, uint32_t parity, int* gave_up) {

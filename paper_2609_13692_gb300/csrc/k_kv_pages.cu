@@ -20,8 +20,11 @@ __device__ uint32_t g_pages_counts[kKvCounts];
 
 // One thread per 16 bytes of the result; the parts' loads are issued together.
 // Four parts of 8,192 x 32 rows of 128 bf16: 54 us, 6.3 TB/s (0.93 of the copy
-// rate); two of 28 x 32 rows: 2.3 us, a launch.  The weights are recomputed by each of a row's threads (n_parts reads that hit
-// L1, n_parts exponentials): cheaper than handing them round.
+// rate); two of 28 x 32 rows: 2.3 us, a launch.  Above four parts at most four
+// parts' loads are in flight and the sums are read twice: 5, 8 and 16 parts of
+// 4,096 x 32 rows 45, 58 and 101 us, 0.68, 0.78 and 0.85 of the copy rate.  The
+// weights are recomputed by each of a row's threads (n_parts reads that hit L1,
+// n_parts exponentials): cheaper than handing them round.
 template <int kType>
 struct Vec;  // 16 bytes as 32-bit floats and back
 template <>
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_kv_copy_pages(const __grid_con
 // shared memory) plus its own ballots.  The counts are whole, so the ranks and
 // everything that follows do not depend on the order of anything.
 // Bound: launch, cluster barriers and dependent reads; 7 to 10 us with 4,096
-// pages, 13 to 23 us with 200,000.  One, two or four blocks are no faster with
+// pages, 13 to 24 us with 200,000.  One, two or four blocks are no faster with
 // 4,096 pages and take 35, 24 and 18 us for a fork with 65,536 (eight: 13).
 // ---------------------------------------------------------------------------
 
