@@ -386,6 +386,7 @@ def _copy_pages(s, pool, planes, plane_stride, n_pages, page_stride, page_bytes,
 
 
 def mpt_kv_check(stream: Optional[int] = None) -> None:
-    """Waits for the stream and raises if a kernel of this module gave up a bounded wait since the last check."""
+    """Waits for the stream and raises if a kernel of this module, on any stream of the current device, gave up a
+    bounded wait (or, in the bounds-checked build, left out an access) that no check has told of."""
     s = _mpt._default_stream_ptr() if stream is None else int(stream)
     _mpt._check(_load().mpt_kv_check(s), "mpt_kv_check")
