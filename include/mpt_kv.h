@@ -121,6 +121,106 @@ mpt_status mpt_kv_merge(const void* const* outs, const float* const* lses, int32
 mpt_status mpt_kv_write(const mpt_kv_cache* cache, const void* k_new, const int64_t* k_stride, const void* v_new,
                         const int64_t* v_stride, int64_t tokens, void* stream);
 
+/* How positions turn new keys and queries: elements x_i and x_{i + rot/2}
+ * (adjacent == 0), or x_{2i} and x_{2i+1}, i < rot / 2, of each head become
+ *     x c - y s,   y c + x s      (x the first, y the second of the two)
+ * with c = table[row][i], s = table[row][rot / 2 + i]; elements from rot on
+ * stay.  A token's row is positions[token], or its position in its request's
+ * cache where positions is NULL.  A token whose row the table does not have
+ * has no place: its key and value are dropped, its query is not turned. */
+typedef struct mpt_kv_turn {
+  const float* table; /* device [rows][stride], 16-byte aligned */
+  int64_t stride;     /* a multiple of 4, >= rot */
+  int32_t rows;
+  int32_t rot; /* a multiple of 16 (adjacent: of 8), up to head_dim */
+  int32_t adjacent;
+  int32_t heads;            /* of q, 1 to 2^17 */
+  const int32_t* positions; /* device [tokens], or NULL */
+  const void* q;            /* device, the type of the keys, [tokens][heads][head_dim], or NULL */
+  void* q_out;              /* q turned; q itself (with its strides), or no overlap with it */
+  int64_t q_stride[2];      /* elements between tokens and heads, multiples of 8 */
+  int64_t q_out_stride[2];
+} mpt_kv_turn;
+
+/* mpt_kv_write with the keys, and the queries where turn->q is given, turned on
+ * the way: products and sums in 32 bits, one rounding to the type.  Queries of
+ * every token of a request are turned, also of tokens that the cache drops;
+ * q_out of tokens of no request is not written.
+ * Errors: INVALID_ARG, TOO_LARGE, CUDA. */
+mpt_status mpt_kv_write_rotated(const mpt_kv_cache* cache, const mpt_kv_turn* turn, const void* k_new,
+                                const int64_t* k_stride, const void* v_new, const int64_t* v_stride, int64_t tokens,
+                                void* stream);
+
+/* ---------------------------------------------------------------------------
+ * A cache in 4 bits.  Per token and KV head, each group of 32 elements (the
+ * last one may be short) holds x as codes 0..15 with a step s and an offset z:
+ *     s = max((max x - min x) / 15, max |x| / 120, 2^-18), rounded up to four
+ *         significant bits,
+ *     z = rint(min x / s),   c = min(max(rint(x / s) - z, 0), 15),
+ * and c stands for (c + z) s, which f16 holds exactly; x is clamped to
+ * +-3360 first, NaN becomes 0.  Every step is a 32-bit operation, rounded to
+ * nearest even.  4.5 bits an element: 288 n bytes for 8 tokens' keys and values
+ * of a head, n = ceil(head_dim / 32).
+ * A page is [kv_heads][page_size / 8 tiles][288 n bytes]; a tile of 8 tokens:
+ *     keys    [8 tokens][8 n pieces][2 bytes]
+ *     marks   [8 tokens][n groups][step, offset]
+ *     values  [4 pairs of tokens][8 n pieces][2 tokens][2 bytes]
+ *     marks   [4 pairs][n groups][step, offset][2 tokens]
+ * a piece being 4 elements in 16 bits, the first the lowest, rotated left by 6;
+ * the step's byte the upper bits of 16 s as a positive f16 (5 of exponent, 3 of
+ * mantissa), the offset's z + 128.  Missing elements of the last group are
+ * written as its first one is.  What reads a step's byte takes those above 222
+ * (16 s = 7168) for 222, so no bytes stand for an infinity or a NaN.
+ * ------------------------------------------------------------------------- */
+typedef struct mpt_kv4_cache {
+  void* pages;       /* device, 16-byte aligned */
+  int64_t stride[2]; /* bytes between pages and KV heads, multiples of 16 */
+  int32_t n_pages;
+  int32_t page_size;  /* power of two, 8 to 256 */
+  int32_t kv_heads;   /* 1 to 1024 */
+  int32_t head_dim;   /* multiple of 8, 8 to 256 */
+  int32_t batch;      /* as in mpt_kv_cache, with what follows */
+  const int32_t* page_table;
+  int64_t table_stride;
+  int32_t table_width;
+  const int32_t* q_offsets;
+  const int32_t* kv_lens;
+} mpt_kv4_cache;
+
+/* Bytes of one KV head of a page.  Errors: INVALID_ARG. */
+mpt_status mpt_kv4_page_bytes(int32_t page_size, int32_t head_dim, int64_t* bytes);
+
+/* Write the new tokens' keys and values (`type`: BF16 or F16) as codes, the
+ * keys and queries turned first where `turn` is given (NULL: not; the turned
+ * keys are not rounded to `type` in between).  Otherwise as mpt_kv_write and
+ * mpt_kv_write_rotated.  Errors: INVALID_ARG, TOO_LARGE, CUDA. */
+mpt_status mpt_kv4_write(const mpt_kv4_cache* cache, const mpt_kv_turn* turn, int32_t type, const void* k_new,
+                         const int64_t* k_stride, const void* v_new, const int64_t* v_stride, int64_t tokens,
+                         void* stream);
+
+/* Read the new tokens' keys and values (what their codes stand for, rounded to
+ * `type`: BF16, F16 or F32) back out of their pages, for a request that is
+ * handed to another cache or a check.  0 where the cache has no place for a
+ * token; rows of no request are not written.
+ *   k_out, v_out: device [tokens][kv_heads][head_dim], strides as in mpt_kv_write.
+ * Errors: INVALID_ARG, TOO_LARGE, CUDA. */
+mpt_status mpt_kv4_read(const mpt_kv4_cache* cache, int32_t type, void* k_out, const int64_t* k_stride, void* v_out,
+                        const int64_t* v_stride, int64_t tokens, void* stream);
+
+/* Bytes of workspace mpt_kv4_attend needs on the current device, whatever the
+ * sizes.  Errors: INVALID_ARG, CUDA. */
+mpt_status mpt_kv4_attend_workspace_bytes(size_t* bytes);
+
+/* mpt_kv_attend over a cache in 4 bits; q and out are `type` (BF16 or F16).
+ * Keys and values enter the products as the f16 values that their codes stand
+ * for, queries as f16 (bf16 ones times a power of two of their row, which is
+ * exact down to 2^-24 of the row's largest), probabilities as f16 at 2^11 times
+ * their size at least.  Errors: as mpt_kv_attend. */
+mpt_status mpt_kv4_attend(const mpt_kv4_cache* cache, int32_t type, const void* q, const int64_t* q_stride,
+                          int64_t tokens, int32_t heads, int32_t max_q_len, int32_t causal, float scale, void* out,
+                          const int64_t* out_stride, float* lse, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
 /* ---------------------------------------------------------------------------
  * Bookkeeping of pages, on the device.  A page is free iff its reference count
  * is <= 0; table row r holds lens[r] tokens on its first

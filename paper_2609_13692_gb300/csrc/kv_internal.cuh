@@ -29,6 +29,7 @@ struct alignas(128) AttnParams {
   int32_t width, n_pages, page_log2, batch, heads, kv_heads, group, dim, causal;
   int32_t box, toks, item_toks;  // page slots per copy; whole tokens of 128 rows, and of an item
   int32_t wide;                  // out's heads are whole 32-byte pieces
+  int32_t f16;                   // 4-bit cache: q and out are f16, else bf16 (k: its pages; k_page, k_head: bytes)
   float scale_log2;  // scale * log2(e)
 };
 
@@ -257,6 +258,13 @@ size_t attend_few_workspace(int sms);
 cudaError_t launch_attend_few(const AttnParams& p, bool f16, int rows_hint, int sms, int device, cudaStream_t stream);
 // The kernels' counts, read in the stream's order.
 cudaError_t attend_few_counts(cudaStream_t stream, uint32_t* counts);
+
+// The same over a cache in 4 bits (k_attend4_few.cu).
+constexpr int kFew4PerSm = 4;  // blocks per SM, at most
+inline size_t attn4_part_offset(int sms) { return ((size_t)sms * kFew4PerSm * sizeof(int4) + 255) / 256 * 256; }
+size_t attend4_few_workspace(int sms);
+cudaError_t launch_attend4_few(const AttnParams& p, int rows_hint, int sms, int device, cudaStream_t stream);
+cudaError_t attend4_few_counts(cudaStream_t stream, uint32_t* counts);
 
 // Whole tiles of query rows on tcgen05 (k_attend_tile.cu); at
 // most kTileBatch requests (its list of them, 16 bytes each, is in the room of

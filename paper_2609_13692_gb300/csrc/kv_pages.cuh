@@ -31,6 +31,33 @@ struct WriteParams {
 };
 cudaError_t launch_kv_write(const WriteParams& p, cudaStream_t stream);
 
+// Writes with a turn and the cache in 4 bits (k_kv_append.cu).  Strides of 16-bit
+// tensors in 16-byte pieces, of outputs in 32 bits in pairs of them.
+struct AppendParams {
+  const char *k_new, *v_new;  // mpt_kv4_read: the outputs
+  char *k, *v;                // the cache in 16 bits
+  char* pages;                // the cache in 4 bits: bytes between pages and heads
+  int64_t page_bytes, head_bytes;
+  const char* q;  // or nullptr
+  char* q_out;
+  int64_t q_tok, q_head, q_out_tok, q_out_head;
+  int64_t k_new_tok, k_new_head, v_new_tok, v_new_head, k_page, k_slot, k_head, v_page, v_slot, v_head;
+  const float* turn;  // or nullptr
+  int64_t turn_stride;
+  const int32_t* positions;
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* q_offsets;
+  const int32_t* kv_lens;
+  int64_t tokens;
+  int32_t rows, rot, adjacent, q_heads;
+  int32_t width, n_pages, page_log2, batch, kv_heads, dim;
+  int32_t lane_log2, parts;  // the launcher's
+};
+cudaError_t launch_kv_append(AppendParams p, bool f16, bool codes, int sms, cudaStream_t stream);
+cudaError_t launch_kv4_read(AppendParams p, int type, int sms, cudaStream_t stream);
+cudaError_t kv_append_counts(cudaStream_t stream, uint32_t* counts);
+
 struct CopyParams {
   char* pool;
   int64_t plane_stride, page_stride, page_bytes;

@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "kv4.cuh"
 #include "kv_pages.cuh"
 #include "kv_report.h"
 
@@ -98,6 +99,71 @@ bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return x < y ? y - x < (uint64_t)an : x - y < (uint64_t)bn;
 }
+
+mpt_status check_cache4(const mpt_kv4_cache* c, int64_t tokens, int* log2) {
+  if (!c || !c->pages || !aligned(c->pages, 16)) return MPT_ERR_INVALID_ARG;
+  if (!page_log2(c->page_size, log2) || c->n_pages < 1 || c->kv_heads < 1 || c->batch < 0 || c->table_width < 1)
+    return MPT_ERR_INVALID_ARG;
+  if (c->head_dim < 8 || c->head_dim % 8 != 0 || tokens < 0) return MPT_ERR_INVALID_ARG;
+  if (c->head_dim > 256 || c->kv_heads > 1024 || c->batch > 1 << 20 || tokens > INT32_MAX) return MPT_ERR_TOO_LARGE;
+  if ((int64_t)c->table_width << *log2 > INT32_MAX) return MPT_ERR_TOO_LARGE;
+  const int64_t head = (int64_t)(c->page_size / kCodeTokens) * kv4_tile(kv4_groups(c->head_dim));
+  const int64_t most = (int64_t)1 << 38;
+  if (c->n_pages > 1 && (c->stride[0] < head || c->stride[0] % 16 != 0 || c->stride[0] >= most)) return MPT_ERR_INVALID_ARG;
+  if (c->kv_heads > 1 && (c->stride[1] < head || c->stride[1] % 16 != 0 || c->stride[1] >= most)) return MPT_ERR_INVALID_ARG;
+  if (c->batch > 0 && (!c->page_table || !c->q_offsets || !c->kv_lens || c->table_stride < c->table_width))
+    return MPT_ERR_INVALID_ARG;
+  if (!aligned(c->page_table, 4) || !aligned(c->q_offsets, 4) || !aligned(c->kv_lens, 4)) return MPT_ERR_INVALID_ARG;
+  return MPT_OK;
+}
+
+mpt_status check_turn(const mpt_kv_turn* u, int32_t dim, int64_t tokens) {
+  if (!u || !u->table || !aligned(u->table, 16) || u->rows < 1 || u->rot < 8 || u->rot % (u->adjacent ? 8 : 16) != 0 || u->rot > dim)
+    return MPT_ERR_INVALID_ARG;
+  if (u->rows > 1 && (u->stride < u->rot || u->stride % 4 != 0 || u->stride >= (int64_t)1 << 38)) return MPT_ERR_INVALID_ARG;
+  if (!aligned(u->positions, 4)) return MPT_ERR_INVALID_ARG;
+  if (!u->q) return MPT_OK;
+  if (!u->q_out || !aligned(u->q, 16) || !aligned(u->q_out, 16) || u->heads < 1) return MPT_ERR_INVALID_ARG;
+  if (u->heads > 1 << 17) return MPT_ERR_TOO_LARGE;
+  const int64_t entries[2] = {tokens, u->heads};
+  for (int i = 0; i < 2; ++i)
+    if (!stride_ok(u->q_stride[i], entries[i]) || !stride_ok(u->q_out_stride[i], entries[i])) return MPT_ERR_INVALID_ARG;
+  if (u->q == u->q_out && ((tokens > 1 && u->q_stride[0] != u->q_out_stride[0]) || (u->heads > 1 && u->q_stride[1] != u->q_out_stride[1])))
+    return MPT_ERR_INVALID_ARG;
+  return MPT_OK;
+}
+
+// What the writes with a turn, the writes of codes and their reads share.
+template <typename Cache>
+void fill_append(AppendParams& p, const Cache& c, const mpt_kv_turn* u, const void* k, const int64_t* k_stride, const void* v,
+                 const int64_t* v_stride, int64_t tokens, int log2) {
+  std::memset(&p, 0, sizeof(p));
+  p.k_new = (const char*)k, p.v_new = (const char*)v;
+  p.k_new_tok = k_stride[0] / 8, p.k_new_head = k_stride[1] / 8, p.v_new_tok = v_stride[0] / 8, p.v_new_head = v_stride[1] / 8;
+  if (u) {
+    p.turn = u->table, p.turn_stride = u->stride, p.positions = u->positions;
+    p.rows = u->rows, p.rot = u->rot, p.adjacent = u->adjacent != 0;
+    if (u->q) {
+      p.q = (const char*)u->q, p.q_out = (char*)u->q_out, p.q_heads = u->heads;
+      p.q_tok = u->q_stride[0] / 8, p.q_head = u->q_stride[1] / 8;
+      p.q_out_tok = u->q_out_stride[0] / 8, p.q_out_head = u->q_out_stride[1] / 8;
+    }
+  }
+  p.table = c.page_table, p.table_stride = c.table_stride, p.q_offsets = c.q_offsets, p.kv_lens = c.kv_lens;
+  p.tokens = tokens, p.width = c.table_width, p.n_pages = c.n_pages, p.page_log2 = log2, p.batch = c.batch;
+  p.kv_heads = c.kv_heads, p.dim = c.head_dim;
+}
+
+mpt_status check_new(const void* k, const int64_t* k_stride, const void* v, const int64_t* v_stride, int64_t tokens, int32_t heads) {
+  if (!k_stride || !v_stride) return MPT_ERR_INVALID_ARG;
+  const int64_t entries[2] = {tokens, heads};
+  for (int i = 0; i < 2; ++i)
+    if (!stride_ok(k_stride[i], entries[i]) || !stride_ok(v_stride[i], entries[i])) return MPT_ERR_INVALID_ARG;
+  if (tokens > 0 && (!k || !v || !aligned(k, 16) || !aligned(v, 16))) return MPT_ERR_INVALID_ARG;
+  return MPT_OK;
+}
+
+size_t attend4_workspace(int sms) { return attend4_few_workspace(sms); }
 
 size_t attend_workspace(int sms) {
   const size_t few = attend_few_workspace(sms), tile = attend_tile_workspace(sms);
@@ -233,6 +299,107 @@ mpt_status mpt_kv_write(const mpt_kv_cache* c, const void* k_new, const int64_t*
   return mpt::launch_kv_write(p, (cudaStream_t)stream) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 
+mpt_status mpt_kv_write_rotated(const mpt_kv_cache* c, const mpt_kv_turn* turn, const void* k_new, const int64_t* k_stride,
+                                const void* v_new, const int64_t* v_stride, int64_t tokens, void* stream) {
+  int log2 = 0, device = 0;
+  mpt_status st = mpt::check_cache(c, tokens, &log2);
+  if (st == MPT_OK) st = mpt::check_turn(turn, c->head_dim, tokens);
+  if (st == MPT_OK) st = mpt::check_new(k_new, k_stride, v_new, v_stride, tokens, c->kv_heads);
+  if (st != MPT_OK || tokens == 0 || c->batch == 0) return st;
+  mpt::AppendParams p;
+  mpt::fill_append(p, *c, turn, k_new, k_stride, v_new, v_stride, tokens, log2);
+  p.k = (char*)c->k, p.v = (char*)c->v;
+  p.k_page = c->k_stride[0] / 8, p.k_slot = c->k_stride[1] / 8, p.k_head = c->k_stride[2] / 8;
+  p.v_page = c->v_stride[0] / 8, p.v_slot = c->v_stride[1] / 8, p.v_head = c->v_stride[2] / 8;
+  const int sms = mpt::kv_sm_count(&device);
+  return mpt::launch_kv_append(p, c->type == MPT_KV_F16, false, sms, (cudaStream_t)stream) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
+}
+
+mpt_status mpt_kv4_page_bytes(int32_t page_size, int32_t head_dim, int64_t* bytes) {
+  int log2 = 0;
+  if (!bytes || !mpt::page_log2(page_size, &log2) || head_dim < 8 || head_dim > 256 || head_dim % 8 != 0) return MPT_ERR_INVALID_ARG;
+  *bytes = (int64_t)(page_size / mpt::kCodeTokens) * mpt::kv4_tile(mpt::kv4_groups(head_dim));
+  return MPT_OK;
+}
+
+mpt_status mpt_kv4_write(const mpt_kv4_cache* c, const mpt_kv_turn* turn, int32_t type, const void* k_new, const int64_t* k_stride,
+                         const void* v_new, const int64_t* v_stride, int64_t tokens, void* stream) {
+  int log2 = 0, device = 0;
+  mpt_status st = mpt::check_cache4(c, tokens, &log2);
+  if (st == MPT_OK && type != MPT_KV_BF16 && type != MPT_KV_F16) st = MPT_ERR_INVALID_ARG;
+  if (st == MPT_OK && turn) st = mpt::check_turn(turn, c->head_dim, tokens);
+  if (st == MPT_OK) st = mpt::check_new(k_new, k_stride, v_new, v_stride, tokens, c->kv_heads);
+  if (st != MPT_OK || tokens == 0 || c->batch == 0) return st;
+  mpt::AppendParams p;
+  mpt::fill_append(p, *c, turn, k_new, k_stride, v_new, v_stride, tokens, log2);
+  p.pages = (char*)c->pages, p.page_bytes = c->stride[0], p.head_bytes = c->stride[1];
+  const int sms = mpt::kv_sm_count(&device);
+  return mpt::launch_kv_append(p, type == MPT_KV_F16, true, sms, (cudaStream_t)stream) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
+}
+
+mpt_status mpt_kv4_read(const mpt_kv4_cache* c, int32_t type, void* k_out, const int64_t* k_stride, void* v_out,
+                        const int64_t* v_stride, int64_t tokens, void* stream) {
+  int log2 = 0, device = 0;
+  mpt_status st = mpt::check_cache4(c, tokens, &log2);
+  if (st == MPT_OK && type != MPT_KV_BF16 && type != MPT_KV_F16 && type != MPT_KV_F32) st = MPT_ERR_INVALID_ARG;
+  if (st == MPT_OK) st = mpt::check_new(k_out, k_stride, v_out, v_stride, tokens, c->kv_heads);
+  if (st != MPT_OK || tokens == 0 || c->batch == 0) return st;
+  mpt::AppendParams p;
+  mpt::fill_append(p, *c, nullptr, k_out, k_stride, v_out, v_stride, tokens, log2);
+  p.pages = (char*)c->pages, p.page_bytes = c->stride[0], p.head_bytes = c->stride[1];
+  const int sms = mpt::kv_sm_count(&device);
+  return mpt::launch_kv4_read(p, type, sms, (cudaStream_t)stream) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
+}
+
+mpt_status mpt_kv4_attend_workspace_bytes(size_t* bytes) {
+  if (!bytes) return MPT_ERR_INVALID_ARG;
+  int device = 0;
+  *bytes = mpt::attend4_workspace(mpt::kv_sm_count(&device));
+  return MPT_OK;
+}
+
+mpt_status mpt_kv4_attend(const mpt_kv4_cache* c, int32_t type, const void* q, const int64_t* q_stride, int64_t tokens, int32_t heads,
+                          int32_t max_q_len, int32_t causal, float scale, void* out, const int64_t* out_stride, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  int log2 = 0;
+  const mpt_status st = mpt::check_cache4(c, tokens, &log2);
+  if (st != MPT_OK) return st;
+  if (type != MPT_KV_BF16 && type != MPT_KV_F16) return MPT_ERR_INVALID_ARG;
+  if (heads < 1 || heads % c->kv_heads != 0 || max_q_len < 0 || !std::isfinite(scale) || !(scale > 0.f) || !q_stride || !out_stride)
+    return MPT_ERR_INVALID_ARG;
+  if (heads / c->kv_heads > 128 || tokens * (heads / c->kv_heads) > INT32_MAX) return MPT_ERR_TOO_LARGE;
+  const int64_t entries[2] = {tokens, heads};
+  for (int i = 0; i < 2; ++i)
+    if (!mpt::stride_ok(q_stride[i], entries[i]) || !mpt::stride_ok(out_stride[i], entries[i])) return MPT_ERR_INVALID_ARG;
+  if (tokens == 0 || c->batch == 0) return MPT_OK;
+  if (!q || !out || !mpt::aligned(q, 16) || !mpt::aligned(out, 16) || !mpt::aligned(lse, 4)) return MPT_ERR_INVALID_ARG;
+  int device = 0;
+  const int sms = mpt::kv_sm_count(&device);
+  if (!workspace || !mpt::aligned(workspace, 256)) return MPT_ERR_INVALID_ARG;
+  if (workspace_bytes < mpt::attend4_workspace(sms)) return MPT_ERR_WORKSPACE_TOO_SMALL;
+
+  mpt::AttnParams p;
+  std::memset((void*)&p, 0, sizeof(p));
+  p.q = (const char*)q;
+  p.out = (char*)out;
+  p.lse = lse;
+  p.q_tok = q_stride[0], p.q_head = q_stride[1], p.out_tok = out_stride[0], p.out_head = out_stride[1];
+  p.k = (const char*)c->pages, p.k_page = c->stride[0], p.k_head = c->stride[1];
+  p.table = c->page_table, p.table_stride = c->table_stride, p.q_offsets = c->q_offsets, p.kv_lens = c->kv_lens;
+  p.desc = (int4*)workspace;
+  p.part = (float*)((char*)workspace + mpt::attn4_part_offset(sms));
+  p.tokens = tokens;
+  p.width = c->table_width, p.n_pages = c->n_pages, p.page_log2 = log2, p.batch = c->batch;
+  p.heads = heads, p.kv_heads = c->kv_heads, p.group = heads / c->kv_heads, p.dim = c->head_dim;
+  p.causal = causal != 0;
+  p.f16 = type == MPT_KV_F16;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  const int64_t most = max_q_len > 0 ? max_q_len : tokens <= c->batch ? 1 : 129;
+  p.box = c->page_size < 64 ? c->page_size : 64;
+  const cudaError_t e = mpt::launch_attend4_few(p, most * p.group < 16 ? (int)(most * p.group) : 16, sms, device, (cudaStream_t)stream);
+  return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
+}
+
 }  // extern "C"
 
 namespace mpt {
@@ -311,18 +478,20 @@ mpt_status mpt_kv_copy_pages(void* pool, int32_t planes, int64_t plane_stride, i
 }
 
 mpt_status mpt_kv_check(void* stream_ptr) {
-  static mpt::Reported few, tile, outside[3];
+  static mpt::Reported few, tile, few4, outside[5];
   cudaStream_t stream = (cudaStream_t)stream_ptr;
-  uint32_t f[mpt::kKvCounts], t[mpt::kKvCounts], g[mpt::kKvCounts];
+  uint32_t f[mpt::kKvCounts], t[mpt::kKvCounts], g[mpt::kKvCounts], a[mpt::kKvCounts], f4[mpt::kKvCounts];
   int device = 0;
   if (cudaGetDevice(&device) != cudaSuccess || mpt::attend_few_counts(stream, f) != cudaSuccess ||
-      mpt::attend_tile_counts(stream, t) != cudaSuccess || mpt::kv_pages_counts(stream, g) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
+      mpt::attend_tile_counts(stream, t) != cudaSuccess || mpt::kv_pages_counts(stream, g) != cudaSuccess ||
+      mpt::kv_append_counts(stream, a) != cudaSuccess || mpt::attend4_few_counts(stream, f4) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
     return MPT_ERR_CUDA;
-  const bool in_few = few.news(device, f[mpt::kKvGaveUp]), in_tile = tile.news(device, t[mpt::kKvGaveUp]);
+  const bool in_few = few.news(device, f[mpt::kKvGaveUp]), in_tile = tile.news(device, t[mpt::kKvGaveUp]),
+             in_few4 = few4.news(device, f4[mpt::kKvGaveUp]);
   bool bad = false;
-  const uint32_t* const counts[3] = {f, t, g};
-  for (int i = 0; i < 3; ++i) bad |= outside[i].news(device, counts[i][mpt::kKvOutside]);
-  return bad ? MPT_ERR_INTERNAL : in_few || in_tile ? MPT_ERR_TIMEOUT : MPT_OK;
+  const uint32_t* const counts[5] = {f, t, g, a, f4};
+  for (int i = 0; i < 5; ++i) bad |= outside[i].news(device, counts[i][mpt::kKvOutside]);
+  return bad ? MPT_ERR_INTERNAL : in_few || in_tile || in_few4 ? MPT_ERR_TIMEOUT : MPT_OK;
 }
 
 }  // extern "C"

@@ -3,7 +3,8 @@
 ``mpt.solve`` and its relatives order the chunks of prompts so that an exact-prefix cache is hit
 most.  These operators serve such prompts: rows forked from a cached prefix, new keys and values
 written into pages, attention of the new tokens over the cache, the merge of attention over parts
-of the keys, and freeing and compacting pages.  Tensors are torch CUDA tensors, passed by address;
+of the keys, and freeing and compacting pages; keys and queries turned by their positions on the
+way, and a cache that holds keys and values in 4 bits.  Tensors are torch CUDA tensors, passed by address;
 every step runs in the kernels of ``libmpt.so``.
 
 Calls enqueue on ``stream`` (a raw stream address; default: torch's current stream) and return
@@ -37,6 +38,8 @@ _CACHE = struct.Struct("@2P6q6iPqi2P")  # mpt_kv_cache
 _BOOK = struct.Struct("@Pq2i2P2i")      # mpt_kv_book
 _PAIR = struct.Struct("@2q")            # two strides
 _TWO = struct.Struct("@2P")             # two addresses
+_TURN = struct.Struct("@Pq4i3P4q")      # mpt_kv_turn
+_CACHE4 = struct.Struct("@P2q5iPqi2P")  # mpt_kv4_cache
 
 _load = _mpt.load
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
@@ -268,6 +271,228 @@ def _write(s, *args):
     status = _load().mpt_kv_write(*args, s)
     if status:
         _mpt._check(status, "mpt_kv_write")
+
+
+def _turn(rotation, positions, adjacent: bool, q, q_out, tokens: int, dim: int, dtype, index: int):
+    """The packed mpt_kv_turn."""
+    _device(rotation, *(t for t in (positions, q, q_out) if t is not None))
+    if rotation.get_device() != index:
+        raise ValueError("every tensor must be on the same CUDA device")
+    _no_grad(rotation, q, q_out)
+    shape, strides = rotation.shape, rotation.stride()
+    if len(shape) != 2 or rotation.dtype is not _F32 or (strides[1] != 1 and shape[1] > 1):
+        raise ValueError("rotation must be a 2-d float32 tensor with contiguous rows: rot / 2 cosines, rot / 2 sines")
+    rows, rot = shape
+    if positions is not None:
+        _ints(positions, "positions")
+        if len(positions) != tokens:
+            raise ValueError("positions needs one entry per token")
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out without q")
+        return _TURN.pack(rotation.data_ptr(), strides[0], rows, rot, 1 if adjacent else 0, 1,
+                          0 if positions is None else positions.data_ptr(), 0, 0, 0, 0, 0, 0)
+    qs = q.shape
+    if len(qs) != 3 or qs[0] != tokens or qs[2] != dim or q.dtype is not dtype:
+        raise ValueError("q must be [tokens, heads, head_dim] of k_new's type")
+    if q_out.shape != qs or q_out.dtype is not dtype:
+        raise ValueError("q_out must have q's shape and type")
+    _heads_strides(q, "q"), _heads_strides(q_out, "q_out")
+    a, b, _ = q.stride()
+    c, d, _ = q_out.stride()
+    return _TURN.pack(rotation.data_ptr(), strides[0], rows, rot, 1 if adjacent else 0, qs[1],
+                      0 if positions is None else positions.data_ptr(), q.data_ptr(), q_out.data_ptr(), a, b, c, d)
+
+
+def mpt_kv_write_rotated(k_new, v_new, rotation, k_pages, v_pages, page_table, q_offsets, kv_lens, *, q=None, positions=None,
+                         adjacent: bool = False, q_out=None, stream: Optional[int] = None):
+    """:func:`mpt_kv_write` with the keys turned by their positions on the way, and the queries
+    ``q`` ([tokens, heads, head_dim]) beside them; returns the turned queries (None without q).
+
+    rotation: float32[positions, rot], of each position rot / 2 cosines, then rot / 2 sines.  The
+    first rot elements of a head turn, i with i + rot / 2 (rot a multiple of 16) or, with
+    ``adjacent``, 2 i with 2 i + 1 (of 8).  positions: int32[tokens], each token's row of
+    ``rotation``; default: its position in the cache.  A token whose row is not there is dropped, its
+    query is not turned.  q_out: where the turned queries go (q itself: in place); tokens of no
+    request are not written."""
+    index = _device(k_pages, v_pages, page_table, q_offsets, kv_lens, k_new, v_new)
+    _no_grad(k_new, v_new, k_pages, v_pages)
+    cache, dtype, kv_heads, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
+    shape = k_new.shape
+    if len(shape) != 3 or shape[1] != kv_heads or shape[2] != dim or v_new.shape != shape or k_new.dtype is not dtype or v_new.dtype is not dtype:
+        raise ValueError("k_new and v_new must be [tokens, kv_heads, head_dim] of the cache's type")
+    return _run(index, stream, _write_rotated, cache, k_new, v_new, rotation, positions, adjacent, q, q_out, index)
+
+
+def _write_rotated(s, cache, k_new, v_new, rotation, positions, adjacent, q, q_out, index):
+    tokens, _, dim = k_new.shape
+    if q is not None and q_out is None:
+        q_out = _empty(q.shape, dtype=q.dtype, device=q.device)
+    turn = _turn(rotation, positions, adjacent, q, q_out, tokens, dim, k_new.dtype, index)
+    status = _load().mpt_kv_write_rotated(cache, turn, k_new.data_ptr(), _heads_strides(k_new, "k_new"), v_new.data_ptr(),
+                                          _heads_strides(v_new, "v_new"), tokens, s)
+    if status:
+        _mpt._check(status, "mpt_kv_write_rotated")
+    return q_out
+
+
+# ---------------------------------------------------------------------------
+# A cache in 4 bits
+# ---------------------------------------------------------------------------
+
+def mpt_kv4_page_bytes(page_size: int, head_dim: int) -> int:
+    """Bytes of one KV head of a page in 4 bits: pages are uint8[n_pages, kv_heads, these]."""
+    out = ctypes.c_int64()
+    _mpt._check(_load().mpt_kv4_page_bytes(int(page_size), int(head_dim), ctypes.byref(out)), "mpt_kv4_page_bytes")
+    return int(out.value)
+
+
+def _cache4(pages, page_table, q_offsets, kv_lens, dim: int) -> bytes:
+    """The packed mpt_kv4_cache of heads of `dim` elements."""
+    shape = pages.shape
+    if len(shape) != 3 or pages.dtype is not _U8:
+        raise ValueError("pages must be uint8[n_pages, kv_heads, page bytes]")
+    a, b, c = pages.stride()
+    if c != 1:
+        raise ValueError("the bytes of a page's head must be contiguous")
+    n_pages, kv_heads, size = shape
+    tile = 288 * ((dim + 31) // 32)
+    if dim < 1 or size % tile or size == 0:
+        raise ValueError("a page's head must be page_size / 8 tiles of 288 bytes per 32 elements")
+    batch, width, stride = _table(page_table, "page_table")
+    _ints(q_offsets, "q_offsets")
+    _ints(kv_lens, "kv_lens")
+    if len(q_offsets) != batch + 1 or len(kv_lens) != batch:
+        raise ValueError("q_offsets needs batch + 1 entries, kv_lens batch")
+    return _CACHE4.pack(pages.data_ptr(), a, b, n_pages, size // tile * 8, kv_heads, dim, batch, page_table.data_ptr(), stride, width,
+                        q_offsets.data_ptr(), kv_lens.data_ptr())
+
+
+def mpt_kv4_write(k_new, v_new, pages, page_table, q_offsets, kv_lens, *, rotation=None, q=None, positions=None,
+                  adjacent: bool = False, q_out=None, stream: Optional[int] = None):
+    """Write the new tokens' keys and values ([tokens, kv_heads, head_dim], bf16 or f16) as 4-bit
+    codes into ``pages`` (uint8[n_pages, kv_heads, :func:`mpt_kv4_page_bytes`]).  With ``rotation``
+    the keys are turned first, and ``q`` beside them, as by :func:`mpt_kv_write_rotated`; returns the
+    turned queries (None without q)."""
+    index = _device(pages, page_table, q_offsets, kv_lens, k_new, v_new)
+    _no_grad(k_new, v_new)
+    shape, dtype = k_new.shape, k_new.dtype
+    if len(shape) != 3 or v_new.shape != shape or v_new.dtype is not dtype or (dtype is not torch.bfloat16 and dtype is not torch.float16):
+        raise ValueError("k_new and v_new must be [tokens, kv_heads, head_dim], bfloat16 or float16")
+    cache = _cache4(pages, page_table, q_offsets, kv_lens, shape[2])
+    if shape[1] != pages.shape[1]:
+        raise ValueError("k_new and v_new must have the KV heads of pages")
+    if rotation is None and (q is not None or positions is not None or q_out is not None):
+        raise ValueError("q, positions and q_out go with a rotation")
+    return _run(index, stream, _write4, cache, k_new, v_new, rotation, positions, adjacent, q, q_out, index)
+
+
+def _write4(s, cache, k_new, v_new, rotation, positions, adjacent, q, q_out, index):
+    tokens, _, dim = k_new.shape
+    turn = None
+    if rotation is not None:
+        if q is not None and q_out is None:
+            q_out = _empty(q.shape, dtype=q.dtype, device=q.device)
+        turn = _turn(rotation, positions, adjacent, q, q_out, tokens, dim, k_new.dtype, index)
+    status = _load().mpt_kv4_write(cache, turn, _TYPES[k_new.dtype], k_new.data_ptr(), _heads_strides(k_new, "k_new"),
+                                   v_new.data_ptr(), _heads_strides(v_new, "v_new"), tokens, s)
+    if status:
+        _mpt._check(status, "mpt_kv4_write")
+    return q_out
+
+
+def mpt_kv4_read(pages, page_table, q_offsets, kv_lens, tokens: int, head_dim: int, *, dtype=torch.bfloat16, k_out=None, v_out=None,
+                 stream: Optional[int] = None):
+    """What the new tokens' codes stand for, in bf16, f16 or f32; returns (keys, values), each
+    [tokens, kv_heads, head_dim].  0 for tokens that the cache has no place for; tokens of no request
+    are not written."""
+    index = _device(pages, page_table, q_offsets, kv_lens)
+    cache = _cache4(pages, page_table, q_offsets, kv_lens, int(head_dim))
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise ValueError("dtype must be bfloat16, float16 or float32")
+    shape = (int(tokens), pages.shape[1], int(head_dim))
+    for t in (k_out, v_out):
+        if t is not None:
+            _device(pages, t)
+            if t.shape != shape or t.dtype is not dtype:
+                raise ValueError("k_out and v_out must be [tokens, kv_heads, head_dim] of dtype")
+    _no_grad(k_out, v_out)
+    return _run(index, stream, _read4, cache, kind, shape, dtype, pages.device, k_out, v_out)
+
+
+def _read4(s, cache, kind, shape, dtype, device, k_out, v_out):
+    if k_out is None:
+        k_out = _empty(shape, dtype=dtype, device=device)
+    if v_out is None:
+        v_out = _empty(shape, dtype=dtype, device=device)
+    status = _load().mpt_kv4_read(cache, kind, k_out.data_ptr(), _heads_strides(k_out, "k_out"), v_out.data_ptr(),
+                                  _heads_strides(v_out, "v_out"), shape[0], s)
+    if status:
+        _mpt._check(status, "mpt_kv4_read")
+    return k_out, v_out
+
+
+_workspace4_bytes: dict = {}
+
+
+def mpt_kv4_attend_workspace_bytes() -> int:
+    """Bytes of workspace of :func:`mpt_kv4_attend` on the current device."""
+    out = ctypes.c_size_t()
+    _mpt._check(_load().mpt_kv4_attend_workspace_bytes(ctypes.byref(out)), "mpt_kv4_attend_workspace_bytes")
+    return int(out.value)
+
+
+def mpt_kv4_attend(q, pages, page_table, q_offsets, kv_lens, *, max_q_len: int = 0, causal: bool = True,
+                   scale: Optional[float] = None, out=None, lse=None, workspace=None, stream: Optional[int] = None):
+    """:func:`mpt_kv_attend` over a cache in 4 bits (:func:`mpt_kv4_write`); returns (out, lse).
+
+    q: [tokens, heads, head_dim], bf16 or f16; pages: uint8[n_pages, kv_heads, page bytes].  Its
+    other arguments, what rows without keys get and what is not written are those of
+    :func:`mpt_kv_attend`."""
+    index = _device(q, pages, page_table, q_offsets, kv_lens)
+    _no_grad(q, out, lse)
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 3 or (dtype is not torch.bfloat16 and dtype is not torch.float16):
+        raise ValueError("q must be [tokens, heads, head_dim], bfloat16 or float16")
+    dim = shape[2]
+    cache = _cache4(pages, page_table, q_offsets, kv_lens, dim)
+    strides = _heads_strides(q, "q")
+    if out is not None:
+        _device(q, out)
+        if out.shape != shape or out.dtype is not dtype:
+            raise ValueError("out must have q's shape and type")
+        out = (out, _heads_strides(out, "out"))
+    if lse is not None:
+        _device(q, lse)
+        if lse.shape != shape[:2] or lse.dtype is not _F32 or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous float32[tokens, heads]")
+    if workspace is not None:
+        _check_workspace(workspace, index)
+    return _run(index, stream, _attend4, index, cache, q, strides, shape, dtype, max_q_len, 1 if causal else 0,
+                1.0 / math.sqrt(dim) if scale is None else scale, out, lse, workspace)
+
+
+def _attend4(s, index, cache, q, strides, shape, dtype, max_q_len, causal, scale, out, lse, workspace):
+    (tokens, heads, dim), device = shape, q.device
+    if out is None:
+        out, out_strides = _empty(shape, dtype=dtype, device=device), _PAIR.pack(heads * dim, dim)
+    else:
+        out, out_strides = out
+    if lse is None:
+        lse = _empty((tokens, heads), dtype=_F32, device=device)
+    if workspace is None:
+        size = _workspace4_bytes.get(index)
+        if size is None:
+            size = _workspace4_bytes[index] = mpt_kv4_attend_workspace_bytes()
+        workspace = _empty(size, dtype=_U8, device=device)
+    else:
+        size = workspace.numel()
+    status = _load().mpt_kv4_attend(cache, _TYPES[dtype], q.data_ptr(), strides, tokens, heads, max_q_len, causal, scale,
+                                    out.data_ptr(), out_strides, lse.data_ptr(), workspace.data_ptr(), size, s)
+    if status:
+        _mpt._check(status, "mpt_kv4_attend")
+    return out, lse
 
 
 # ---------------------------------------------------------------------------

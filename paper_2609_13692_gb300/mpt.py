@@ -48,7 +48,8 @@ EXPORTED = [
     "mpt_solve_end", "mpt_solve_resume", "mpt_set_tables", "mpt_tables32", "mpt_gather_bandwidth",
     "mpt_alu_addmin_peak", "mpt_build_info", "mpt_kv_attend_workspace_bytes", "mpt_kv_attend", "mpt_kv_merge",
     "mpt_kv_write", "mpt_kv_fork", "mpt_kv_extend", "mpt_kv_free", "mpt_kv_compact",
-    "mpt_kv_copy_pages", "mpt_kv_check",
+    "mpt_kv_copy_pages", "mpt_kv_check", "mpt_kv_write_rotated", "mpt_kv4_page_bytes", "mpt_kv4_write", "mpt_kv4_read",
+    "mpt_kv4_attend_workspace_bytes", "mpt_kv4_attend",
 ]
 
 
@@ -150,6 +151,12 @@ def load() -> ctypes.CDLL:
         "mpt_kv_compact": ([vp, vp, vp, vp, vp], ctypes.c_int),
         "mpt_kv_copy_pages": ([vp, i32, i64, i32, i64, i64, vp, vp, i32, vp], ctypes.c_int),
         "mpt_kv_check": ([vp], ctypes.c_int),
+        "mpt_kv_write_rotated": ([vp, vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
+        "mpt_kv4_page_bytes": ([i32, i32, ctypes.POINTER(i64)], ctypes.c_int),
+        "mpt_kv4_write": ([vp, vp, i32, vp, vp, vp, vp, i64, vp], ctypes.c_int),
+        "mpt_kv4_read": ([vp, i32, vp, vp, vp, vp, i64, vp], ctypes.c_int),
+        "mpt_kv4_attend_workspace_bytes": ([ctypes.POINTER(sz)], ctypes.c_int),
+        "mpt_kv4_attend": ([vp, i32, vp, vp, i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
