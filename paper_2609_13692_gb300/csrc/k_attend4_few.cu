@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
         const int col = 8 * (q * N + w);
         u[w] = valid && col < p.dim ? *(const uint4*)(at + 2 * col) : make_uint4(0, 0, 0, 0);
       }
-      const float back = query_words<N>(u, p.f16, qf[i]) * p.scale_log2;
+      const float back = kv4_scale(p.scale_log2, query_words<N>(u, p.f16, qf[i]));
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int mine = 8 * i + 2 * q + e;

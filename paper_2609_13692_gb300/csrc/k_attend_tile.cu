@@ -55,7 +55,7 @@
 // values that some row of the item must not see, blanks those that are not
 // finite, and notes the ones that other rows do see; these rows add them at the
 // item's end, key by key.
-#include "kv_internal.cuh"
+#include "kv4.cuh"
 
 namespace mpt {
 namespace {
@@ -106,6 +106,7 @@ struct TileShared {
   uint32_t tmem;
   uint32_t sent[2], asked;  // copies issued, for the block's end: tiles of keys and of values, items' queries
   int gave_up;
+  unsigned long long q_ready[2];  // cache in 4 bits: queries of a row tile
   uint32_t held[kHeldSets];
   uint32_t odd[kOddSets][9];  // 8 words of keys from the item's first ambiguous one, and whether any is set
   int64_t scratch[40];
@@ -440,7 +441,202 @@ __device__ void fill_list(const AttnParams& p, TileShared& sh) {
   __syncwarp();
 }
 
-template <int HDP, bool F16>
+// ---- the cache in 4 bits ----
+//
+// Its kernel is the same but for where the operands come from: warps 9 to 11
+// read codes and write f16 keys and values where the copies would have put
+// them, and each row's thread its own query.  Codes stand for finite values
+// whatever their bytes, so there is nothing to look for in masked ones.
+constexpr int kCodeWarps = 3;
+
+template <bool F16, bool kCodes>
+__device__ __forceinline__ uint32_t pack_as(const AttnParams& p, float lo, float hi) {
+  if (!kCodes) return pack2<F16>(lo, hi);
+  return p.f16 ? pack2<true>(lo, hi) : pack2<false>(lo, hi);
+}
+
+// A row's query into row r of its tile's operand, each 8 elements in the order
+// 0 4 1 5 2 6 3 7 that a word of codes gives (widen_codes).  bf16: times a power
+// of two, so that the largest element stays below 2 and f16 holds what is above
+// 2^-14 of it exactly; returns what takes it out again.  nullptr: zeros.
+template <int HDP>
+__device__ __forceinline__ float stage_query(const char* q, int dim, bool f16, char* to, int r) {
+  float by = 1.f, back = 1.f;
+  if (!f16 && q) {
+    uint32_t top = 0;
+#pragma unroll 8
+    for (int c = 0; c < dim; c += 8) {
+      const uint4 u = *(const uint4*)(q + 2 * c);
+      const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max(v[i] << 16 & 0x7FFFFFFFu, v[i] & 0x7FFF0000u));
+    }
+    int e = (int)(top >> 23) - 127;
+    e = top == 0 ? 0 : e < -126 ? -126 : e > 126 ? 126 : e;
+    by = __uint_as_float((uint32_t)(127 - e) << 23);
+    back = __uint_as_float((uint32_t)(127 + e) << 23);
+  }
+#pragma unroll 8
+  for (int ch = 0; ch < HDP / 8; ++ch) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (q && ch * 8 < dim) u = *(const uint4*)(q + 16 * ch);
+    uint32_t v[4] = {u.x, u.y, u.z, u.w};
+    if (!f16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = pack2<true>(__uint_as_float(v[i] << 16) * by, __uint_as_float(v[i] & 0xFFFF0000u) * by);
+    }
+    uint4 o;
+    o.x = __byte_perm(v[0], v[2], 0x5410);
+    o.y = __byte_perm(v[0], v[2], 0x7632);
+    o.z = __byte_perm(v[1], v[3], 0x5410);
+    o.w = __byte_perm(v[1], v[3], 0x7632);
+    *(uint4*)(to + (ch >> 3) * 128 * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = o;
+  }
+  return back;
+}
+
+// 16 bytes of codes (32 elements of a key, or 16 of a pair of values) with their marks.
+struct CodeChunk {
+  uint4 w;
+  uint32_t marks;
+};
+
+// By warps 9 to 11: f16 keys and values of the block's key tiles, each in its
+// slot of the ring.  A tile of 8 tokens has 8 n chunks of 16 bytes of either;
+// a warp takes tiles of 8 in turn, a lane the same chunk of each (kPer of them
+// with more than 4 groups; two tiles at once with 2).  A chunk is read as soon as the one
+// before it in its registers has been used, which is half a key tile ahead.
+template <int HDP, typename Next, typename Leave>
+__device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh, char* ring, Next next_item, Leave leave) {
+  using C = TileCfg<HDP>;
+  constexpr int kTogether = HDP == 64 ? 2 : 1, kPer = HDP == 256 ? 2 : 1;
+  constexpr int kTiles8 = kKeys / kCodeTokens / kTogether;                  // steps of all warps in half a key tile
+  constexpr int kSteps = (kTiles8 + kCodeWarps - 1) / kCodeWarps * kPer;    // of a warp
+  const int lane = threadIdx.x & 31, me = (threadIdx.x >> 5) - 9;
+  const int n = kv4_groups(p.dim);
+  int* const gave_up = &sh.gave_up;
+  const int second = kTogether == 2 ? lane >> 4 : 0, in = kTogether == 2 ? lane & 15 : lane;
+
+  // Where the lane's chunks of a tile of 8 come from and go to.  A slot has rows
+  // of 128 bytes (64 elements) with their 16-byte pieces permuted by row: piece c of
+  // row r at c ^ (r & 7).  Lanes of odd blocks of 64 elements take a chunk's halves
+  // in the other order, so that 8 lanes write to 8 places.
+  bool has[kPer], odd[kPer][2];
+  uint32_t mark_from[kPer][2], to[kPer][2];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int x = in + 32 * i;
+    has[i] = x < 8 * n;
+    const int tok = x / n, g = x - tok * n;  // of a key
+    mark_from[i][0] = kv4_key_marks(n, 0) + 2 * x;  // [token][group], as the chunks
+    odd[i][0] = g >> 1 & 1;
+    to[i][0] = (g >> 1) * kKeys * 128 + tok * 128 + ((((g & 1) << 2 | (g & 2)) ^ tok) << 4);
+    const int pair = x / (2 * n), piece4 = x - pair * 2 * n;  // of a pair of values, 4 pieces of 4 elements
+    mark_from[i][1] = kv4_value_marks(n, pair) + 4 * (piece4 >> 1);
+    odd[i][1] = piece4 >> 2 & 1;
+    to[i][1] = (piece4 >> 2) * kKeys * 128 + 2 * pair * 128 + ((((piece4 & 3) << 1 | (piece4 >> 2 & 1)) ^ 2 * pair) << 4);
+  }
+  const uint32_t from = 16 * in, values_from = kv4_value(n, 0);
+
+  // Step i, half v (0 keys, 1 values): the tile of 8 that it is about.
+  // (The warp that has one step more than the others is another for values.)
+  auto tile8 = [&](int v, int i) { return ((i / kPer) * kCodeWarps + (v ? (me + 1) % kCodeWarps : me)) * kTogether + second; };
+
+  TileItem w;
+  int k = 0;
+  uint32_t gt = 0;
+  bool ok = true;
+  // Lane b: the b-th tile of 8 of a key tile, nullptr without a page.
+  auto tile_of = [&](int j, int tiles) -> const char* {
+    const int64_t key = (int64_t)(w.e.t0 + j) * kKeys + (lane & 15) * kCodeTokens;
+    if (j >= tiles || key >= w.e.kvl) return nullptr;
+    const int id = p.table[(int64_t)w.e.req * p.table_stride + (key >> p.page_log2)];
+    if (id < 0 || id >= p.n_pages) return nullptr;
+    const int slot = (int)(key & ((1 << p.page_log2) - 1));
+    if (KV_BAD(g_tile_counts, id < p.n_pages && slot + kCodeTokens <= 1 << p.page_log2 && w.e.head < p.kv_heads)) return nullptr;
+    return p.k + (int64_t)id * p.k_page + (int64_t)w.e.head * p.k_head + (int64_t)(slot / kCodeTokens) * kv4_tile(n);
+  };
+  auto load = [&](CodeChunk& c, int v, int i, const char* tiles) {
+    const int t8 = tile8(v, i);
+    const char* at = (const char*)__shfl_sync(~0u, (unsigned long long)tiles, t8 & 15);
+    c.w = make_uint4(0, 0, 0, 0);
+    c.marks = 0;
+    if (t8 >= kKeys / kCodeTokens || !has[i % kPer] || !at) return;  // without a page: zeros
+    c.w = __ldg((const uint4*)(at + (v ? values_from : 0) + from + 512 * (i % kPer)));
+    const char* m = at + mark_from[i % kPer][v];
+    c.marks = v ? __ldg((const uint32_t*)m) : (uint32_t)__ldg((const uint16_t*)m);
+  };
+  auto store = [&](const CodeChunk& c, int v, int i, uint32_t slot_at) {
+    const int t8 = tile8(v, i);
+    if (t8 >= kKeys / kCodeTokens || !has[i % kPer]) return;
+    const uint32_t at = slot_at + to[i % kPer][v] + t8 * kCodeTokens * 128;
+    const bool swap = odd[i % kPer][v];
+    const uint32_t u[4] = {swap ? c.w.z : c.w.x, swap ? c.w.w : c.w.y, swap ? c.w.x : c.w.z, swap ? c.w.y : c.w.w};
+    uint32_t step, off;
+    if (v == 0) {
+      kv4_key_step(c.marks, step, off);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        uint32_t o[4];
+        kv4_word(u[h], step, off, o);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at ^ 16 * h), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+      }
+    } else {
+      kv4_value_step(c.marks, step, off);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t x0[4], x1[4];
+        kv4_word(u[2 * h], step, off, x0);
+        kv4_word(u[2 * h + 1], step, off, x1);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {  // the pair's tokens
+          const uint32_t sel = e ? 0x7632 : 0x5410;
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"((at ^ 16 * (h ^ e)) + 128 * e), "r"(__byte_perm(x0[0], x0[1], sel)),
+                       "r"(__byte_perm(x0[2], x0[3], sel)), "r"(__byte_perm(x1[0], x1[1], sel)), "r"(__byte_perm(x1[2], x1[3], sel))
+                       : "memory");
+        }
+      }
+    }
+  };
+
+  CodeChunk c[kSteps];
+  do {
+    w.load(p, &sh.list[k]);
+    const int tiles = w.tiles;
+    if (tiles == 0) continue;
+    const char *now = tile_of(0, tiles), *next = tile_of(1, tiles);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) load(c[i], 0, i, now);
+    for (int j = 0; j < tiles && ok; ++j, ++gt) {
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const uint32_t idx = 2 * gt + v;
+        const int s = idx % C::kSlots;
+        if (idx >= C::kSlots) ok = ok && wait_spaced<20>(&sh.empty[s], (idx / C::kSlots - 1) & 1, gave_up);
+        if (!ok) break;
+        if (v == 0 && me == 0) {
+          const unsigned held = __ballot_sync(~0u, now != nullptr) & 0xFFFFu;
+          if (lane == 0) sh.held[gt % kHeldSets] = held;
+        }
+        const uint32_t slot_at = smem_u32(ring + s * C::kSlot);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          store(c[i], v, i, slot_at);
+          load(c[i], 1 - v, i, v == 0 ? now : next);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.full[s]);
+      }
+      now = next;
+      next = tile_of(j + 2, tiles);
+    }
+  } while (ok && uniform(next_item(k)));
+  if (!ok) leave();
+}
+
+// kCodes: over the cache in 4 bits, F16 being the type of its products.
+template <int HDP, bool F16, bool kCodes>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_constant__ AttnParams p) {
   using C = TileCfg<HDP>;
   extern __shared__ char raw[];
@@ -452,14 +648,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
 
   if (tid == 0) {
     for (int s = 0; s < C::kSlots; ++s) {
-      mbar_init(&sh.full[s], 1);
+      mbar_init(&sh.full[s], kCodes ? kCodeWarps : 1);
       mbar_init(&sh.empty[s], 1);
     }
     mbar_init(&sh.q_full, 1);
     mbar_init(&sh.q_empty, 1);
+    mbar_init(&sh.q_ready[0], 4);
+    mbar_init(&sh.q_ready[1], 4);
     for (int s = 0; s < 3; ++s) {  // 2: the second score buffer with one row tile
       mbar_init(&sh.s_full[s], 1);
-      mbar_init(&sh.p_ready[s], 5);  // four warps of rows, and warp 11
+      mbar_init(&sh.p_ready[s], kCodes ? 4 : 5);  // four warps of rows, and warp 11
     }
     mbar_init(&sh.o_full[0], 1);
     mbar_init(&sh.o_full[1], 1);
@@ -506,7 +704,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     for (int i = lo; i < hi; ++i) reqs[i].x += (int)before;
     if (tid == 0) {
       sh.items = bad || all > INT32_MAX ? 0 : (int)all;  // (2^31 items: q would not fit in memory)
-      sh.stride = keys * p.kv_heads * p.dim * 4 > kNaturalBytes ? (int)gridDim.x : 1;
+      const int64_t bytes = kCodes ? 36 * kv4_groups(p.dim) : p.dim * 4;  // of a key and its value
+      sh.stride = keys * p.kv_heads * bytes > kNaturalBytes ? (int)gridDim.x : 1;
     }
     __syncthreads();
   }
@@ -599,7 +798,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
-    if (warp == 9 || warp == 10) {
+    if (kCodes && warp > 8) {
+      // ---- codes: warps 9 to 11 make f16 keys and values of them ----
+      widen_codes<HDP>(p, sh, ring, next_item, leave);
+    } else if (warp == 9 || warp == 10) {
       // ---- copies: warp 9 queries and keys, warp 10 values ----
       // Tile g of the block (over all its items) has its keys in use 2 g of the
       // ring and its values in use 2 g + 1.  A warp waits for every second use's
@@ -724,8 +926,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         w.load(p, &sh.list[k]);
         const int tiles = (int)uniform((uint32_t)w.tiles), n0 = (int)uniform((uint32_t)w.n0), n1 = (int)uniform((uint32_t)w.n1);
         if (tiles == 0) continue;
-        ok = wait_all(&sh.q_full, item & 1, gave_up) && wait_all(&sh.full[sk], phase, gave_up);
-        ++item;
+        if constexpr (kCodes) {  // bits 0 and 1 of item: phases of the row tiles' queries
+          if (n0 > 0) ok = wait_all(&sh.q_ready[0], item & 1, gave_up);
+          if (n1 > 0) ok = ok && wait_all(&sh.q_ready[1], item >> 1, gave_up);
+          item ^= (n0 > 0 ? 1 : 0) | (n1 > 0 ? 2 : 0);
+          ok = ok && wait_all(&sh.full[sk], phase, gave_up);
+        } else {
+          ok = wait_all(&sh.q_full, item & 1, gave_up) && wait_all(&sh.full[sk], phase, gave_up);
+          ++item;
+        }
         if (!ok) break;
         fence_after();
         if (elect_one()) {
@@ -735,9 +944,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           if (tiles == 1) commit(&sh.q_empty);
         }
         __syncwarp();
+        // kCodes: the phase of the values in slot `at`, which the keys in `key_slot` came before in phase `ph`
+        auto values_in = [&](int at, int key_slot, uint32_t ph) { return wait_all(&sh.full[at], at < key_slot ? ph ^ 1 : ph, gave_up); };
         if constexpr (C::kTiles == 1) {
           // The next scores are made while this tile's P is.
           int sv = after(sk, 1);
+          uint32_t v_phase = sv < sk ? phase ^ 1 : phase;
           auto step = [&] {
             if (sk + 2 >= C::kSlots) phase ^= 1;
             sk = after(sk, 2);
@@ -759,6 +971,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
             const int b = j & 1 ? 2 : 0;
             ok = wait_all(&sh.p_ready[b], ready >> b & 1, gave_up);
             ready ^= 1u << b;
+            if (kCodes) ok = ok && wait_all(&sh.full[sv], v_phase, gave_up);
             if (!ok) break;
             fence_after();
             if (elect_one()) {
@@ -768,10 +981,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
               if (j + 1 == tiles) commit(&sh.o_full[0]);
             }
             __syncwarp();
+            if (sv + 2 >= C::kSlots) v_phase ^= 1;
             sv = after(sv, 2);
             if (j + 2 < tiles) {
-              if (!C::kWatchKeys) ok = wait_all(&sh.full[sk], phase, gave_up);
+              if (!C::kWatchKeys || kCodes) ok = wait_all(&sh.full[sk], phase, gave_up);
               if (!ok) break;
+              if (kCodes) fence_after();
               if (elect_one()) {
                 scores(0, j & 1 ? 128 : 0, b, sk);
                 commit(&sh.empty[sk]);
@@ -783,10 +998,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           }
         } else {
           for (int j = 0; j < tiles; ++j) {
-            const int sv = after(sk, 1);
+            const int sv = after(sk, 1), sk0 = sk;
+            const uint32_t phase0 = phase;
             if (sk + 2 >= C::kSlots) phase ^= 1;
             sk = after(sk, 2);
             const bool more = j + 1 < tiles;
+            if constexpr (kCodes) {  // long there, mostly
+              ok = values_in(sv, sk0, phase0) && (!more || wait_all(&sh.full[sk], phase, gave_up));
+              if (!ok) break;
+            }
             // p_ready is complete once P stands, and this tile's values and the
             // next one's keys are there (warp 11 waits for those): one wait here
             if (j < n0) {
@@ -925,6 +1145,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       const int64_t first_tok = (int64_t)w.tok0 + s * p.toks;
       const bool valid = r_tok < p.toks && first_tok + r_tok < w.e.ql;
       const int tok = valid ? (int)first_tok + r_tok : 0;
+      float scale_log2 = p.scale_log2;
+      if constexpr (kCodes) {
+        // This row tile's scores of the item before have all been read here, so
+        // its queries are free.
+        if (w.count(s) > 0) {
+          const int64_t at = (int64_t)w.e.q0 + tok, head = (int64_t)w.e.head * p.group + sub;
+          const bool mine = valid && !KV_BAD(g_tile_counts, at >= 0 && at < p.tokens && head >= 0 && head < p.heads);
+          scale_log2 = kv4_scale(scale_log2, stage_query<HDP>(mine ? p.q + 2 * (at * p.q_tok + head * p.q_head) : nullptr, p.dim, p.f16,
+                                                              qbuf + s * C::kBlk * 128 * 128, r));
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.q_ready[s]);
+        }
+      }
       const int lim = valid ? w.limit(p, tok) : INT32_MAX;
       const int lim_tile = first_tok < w.e.ql ? w.limit(p, (int)first_tok) : 0;  // what every row of the tile sees
       float m = -INFINITY, l = 0.f;
@@ -968,7 +1202,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], f[c + q], f[c + 4 + q]);
 #pragma unroll
         for (int q = 0; q < 4; ++q) mx[q] = fmaxf(mx[q], f[124 + q]);
-        const float top = L<F16>::reference(fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2));
+        const float top = L<F16>::reference(fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale_log2));
         if (j == 0) {
           m = top;
         } else if (__any_sync(~0u, top - m > kLag<F16>)) {
@@ -998,7 +1232,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
         const float ref = m == -INFINITY ? 0.f : m;
         // P, rounded to the cache's type (the operand's), over S
         uint64_t sum[2] = {0, 0};  // pairs of 32-bit sums
-        const uint64_t mul = pair(p.scale_log2, p.scale_log2), off = pair(L<F16>::kLift - ref, L<F16>::kLift - ref);
+        const uint64_t mul = pair(scale_log2, scale_log2), off = pair(L<F16>::kLift - ref, L<F16>::kLift - ref);
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
           uint32_t x[16];
@@ -1024,7 +1258,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       if (!ok) break;
       gt += w.tiles;
       const uint32_t* odd = nullptr;
-      if (w.tiles > 0) odd = sh.odd[item++ % kOddSets];
+      if (!kCodes && w.tiles > 0) odd = sh.odd[item++ % kOddSets];
       if (w.count(s) > 0) {
         ok = wait_all(&sh.o_full[s], done & 1, gave_up);
         ++done;
@@ -1050,7 +1284,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = 0.f;
           }
-          if (extra && valid) {
+          if (!kCodes && extra && valid) {
             // seen keys whose values were blanked for the other rows
             const char* q = p.q + 2 * (tok_at * p.q_tok + head * p.q_head);
             for (int a = 0; a < 256; ++a) {
@@ -1080,7 +1314,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           if (whole) {
             uint32_t v[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = pack2<F16>(o[2 * e] * scale, o[2 * e + 1] * scale);
+            for (int e = 0; e < 16; ++e) v[e] = pack_as<F16, kCodes>(p, o[2 * e] * scale, o[2 * e + 1] * scale);
             if (inside && p.wide) {  // whole 32-byte sectors
 #pragma unroll
               for (int e = 0; e < 2; ++e)
@@ -1105,7 +1339,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
           part[C::kRows * HDP + C::kRows + s * 128 + r] = l;
         }
       }
-      if (w.count(s) > 0) {  // the notes are read
+      if (!kCodes && w.count(s) > 0) {  // the notes are read
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.odd_read[(item - 1) % kOddSets]);
       }
@@ -1124,12 +1358,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   // and the last queries.  They land before the block ends.
   if ((warp == 9 || warp == 10) && *(volatile int*)gave_up) {
     if (tid == 9 * 32) atomicAdd(&g_tile_counts[kKvGaveUp], 1u);
+    if (!kCodes) {
     const uint32_t v = warp - 9, n = sh.sent[v], last = (C::kSlots + 1) / 2;
     for (uint32_t k = n > last ? n - last : 0; k < n; ++k) {
       const uint32_t idx = 2 * k + v;
       wait_landed(&sh.full[idx % C::kSlots], (idx / C::kSlots) & 1);
     }
     if (v == 0 && sh.asked > 0) wait_landed(&sh.q_full, (sh.asked - 1) & 1);
+    }
   }
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
@@ -1138,7 +1374,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
 // (c, 32 rows), a lane per row, a warp per eighth of the columns.  (Four times the
 // blocks for a quarter of the columns each: 1 us less where 20 parts of 8 items
 // are joined, 20 us more where 152 items of 2 parts are.)
-template <int HDP, bool F16>
+template <int HDP, bool F16, bool kCodes>
 __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant__ AttnParams p) {
   wait_for_primary();
   const int4 d = p.desc[blockIdx.x];
@@ -1182,29 +1418,29 @@ __global__ void __launch_bounds__(256) k_attend_tile_join(const __grid_constant_
     const int col = warp * kCols + c;
     if (col >= p.dim) break;
     uint4 v;
-    v.x = pack2<F16>(acc[c] * inv, acc[c + 1] * inv);
-    v.y = pack2<F16>(acc[c + 2] * inv, acc[c + 3] * inv);
-    v.z = pack2<F16>(acc[c + 4] * inv, acc[c + 5] * inv);
-    v.w = pack2<F16>(acc[c + 6] * inv, acc[c + 7] * inv);
+    v.x = pack_as<F16, kCodes>(p, acc[c] * inv, acc[c + 1] * inv);
+    v.y = pack_as<F16, kCodes>(p, acc[c + 2] * inv, acc[c + 3] * inv);
+    v.z = pack_as<F16, kCodes>(p, acc[c + 4] * inv, acc[c + 5] * inv);
+    v.w = pack_as<F16, kCodes>(p, acc[c + 6] * inv, acc[c + 7] * inv);
     *(uint4*)(p.out + 2 * (tok * p.out_tok + head * p.out_head + col)) = v;
   }
   if (p.lse && warp == 0) p.lse[tok * p.heads + head] = L<F16>::lse(top, sum);
 }
 
-template <int HDP, bool F16>
+template <int HDP, bool F16, bool kCodes = false>
 cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream) {
   using C = TileCfg<HDP>;
   // the warpgroups' shares have to fit the registers of the launch, or they would wait for ever
   static const cudaError_t fits = [] {
     cudaFuncAttributes a;
-    const cudaError_t e = cudaFuncGetAttributes(&a, k_attend_tile<HDP, F16>);
+    const cudaError_t e = cudaFuncGetAttributes(&a, k_attend_tile<HDP, F16, kCodes>);
     return e != cudaSuccess ? e : a.numRegs * 3 >= C::kRoleRegs + 2 * C::kRowRegs ? cudaSuccess : cudaErrorInvalidConfiguration;
   }();
   if (fits != cudaSuccess) return fits;
   static std::atomic<uint64_t> allowed;
-  cudaError_t e = kv_allow_smem(k_attend_tile<HDP, F16>, C::kSmem, device, allowed);
+  cudaError_t e = kv_allow_smem(k_attend_tile<HDP, F16, kCodes>, C::kSmem, device, allowed);
   if (e != cudaSuccess) return e;
-  k_attend_tile<HDP, F16><<<sms, kThreads, C::kSmem, stream>>>(p);
+  k_attend_tile<HDP, F16, kCodes><<<sms, kThreads, C::kSmem, stream>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(sms, C::kRows / 32);
@@ -1215,13 +1451,24 @@ cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream
   at.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_attend_tile_join<HDP, F16>, p);
+  return cudaLaunchKernelEx(&cfg, k_attend_tile_join<HDP, F16, kCodes>, p);
 }
 
 }  // namespace
 
+// Floats of the partial results (after the blocks' descriptions).
+static size_t tile_parts(int sms) { return (size_t)sms * 2 * (256 * 128 + 2 * 256); }
+
+size_t attend4_tile_workspace(int sms) { return attn4_part_offset(sms) + tile_parts(sms) * sizeof(float); }
+
+cudaError_t launch_attend4_tile(const AttnParams& p, int sms, int device, cudaStream_t stream) {
+  if (p.dim <= 64) return launch<64, true, true>(p, sms, device, stream);
+  if (p.dim <= 128) return launch<128, true, true>(p, sms, device, stream);
+  return launch<256, true, true>(p, sms, device, stream);
+}
+
 size_t attend_tile_workspace(int sms) {  // a slot has as much room for 128 rows of 256 columns as for 256 of 128
-  return (size_t)sms * kFewPerSm * sizeof(int4) + 256 + (size_t)sms * 2 * (256 * 128 + 2 * 256) * sizeof(float);
+  return (size_t)sms * kFewPerSm * sizeof(int4) + 256 + tile_parts(sms) * sizeof(float);
 }
 
 cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int device, cudaStream_t stream) {

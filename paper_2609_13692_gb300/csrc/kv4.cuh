@@ -70,4 +70,11 @@ __device__ __forceinline__ void kv4_value_step(uint32_t marks, uint32_t& step, u
   kv4_marks(__byte_perm(marks, 0, 0x4140), __byte_perm(marks, 0, 0x4342), step, off);
 }
 
+// The scale of a row's scores once its power of two is back in it, between the
+// smallest and the largest normal number: 0 times a masked score, or infinity
+// times one of 0, would be NaN.
+__device__ __forceinline__ float kv4_scale(float scale, float back) {
+  return fminf(fmaxf(scale * back, 1.17549435e-38f), 3.40282347e38f);
+}
+
 }  // namespace mpt

@@ -271,6 +271,8 @@ cudaError_t attend4_few_counts(cudaStream_t stream, uint32_t* counts);
 // the ring of slots).
 constexpr int kTileBatch = 8192;
 size_t attend_tile_workspace(int sms);
+size_t attend4_tile_workspace(int sms);
+cudaError_t launch_attend4_tile(const AttnParams& p, int sms, int device, cudaStream_t stream);
 cudaError_t launch_attend_tile(const AttnParams& p, bool f16, int sms, int device, cudaStream_t stream);
 cudaError_t attend_tile_counts(cudaStream_t stream, uint32_t* counts);
 

@@ -163,7 +163,10 @@ mpt_status check_new(const void* k, const int64_t* k_stride, const void* v, cons
   return MPT_OK;
 }
 
-size_t attend4_workspace(int sms) { return attend4_few_workspace(sms); }
+size_t attend4_workspace(int sms) {
+  const size_t few = attend4_few_workspace(sms), tile = attend4_tile_workspace(sms);
+  return few > tile ? few : tile;
+}
 
 size_t attend_workspace(int sms) {
   const size_t few = attend_few_workspace(sms), tile = attend_tile_workspace(sms);
@@ -395,8 +398,13 @@ mpt_status mpt_kv4_attend(const mpt_kv4_cache* c, int32_t type, const void* q, c
   p.f16 = type == MPT_KV_F16;
   p.scale_log2 = scale * 1.4426950408889634f;
   const int64_t most = max_q_len > 0 ? max_q_len : tokens <= c->batch ? 1 : 129;
+  p.toks = 128 / p.group;
+  p.item_toks = p.toks * (p.dim > 128 ? 1 : 2);
+  p.wide = p.dim % 16 == 0 && mpt::aligned(out, 32) && (heads == 1 || p.out_head % 16 == 0) && (tokens == 1 || p.out_tok % 16 == 0);
   p.box = c->page_size < 64 ? c->page_size : 64;
-  const cudaError_t e = mpt::launch_attend4_few(p, most * p.group < 16 ? (int)(most * p.group) : 16, sms, device, (cudaStream_t)stream);
+  const bool tile = most * p.group > 16 && c->batch <= mpt::kTileBatch;
+  const cudaError_t e = tile ? mpt::launch_attend4_tile(p, sms, device, (cudaStream_t)stream)
+                             : mpt::launch_attend4_few(p, most * p.group < 16 ? (int)(most * p.group) : 16, sms, device, (cudaStream_t)stream);
   return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 
