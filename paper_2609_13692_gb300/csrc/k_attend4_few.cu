@@ -25,8 +25,7 @@ namespace {
 
 __device__ uint32_t g_few4_counts[kKvCounts];
 
-constexpr int kKeys = 64;  // of a stage
-constexpr int kWarps = 4;  // of products, 16 keys of a stage each; one more copies
+constexpr int kWarps = 4;  // of products; one more copies
 constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kLag = 4;    // scores may exceed a row's reference by 2^kLag
 using L = Lift<true, kLag>;
@@ -36,8 +35,10 @@ template <int N, int kR>
 struct Few4Cfg {
   static constexpr int kRows = 8 * kR, kCols = 32 * N;
   static constexpr int kPerSm = kR == 1 ? (N <= 2 ? 4 : N <= 4 ? 3 : 2) : N <= 2 ? 3 : 2;
+  static constexpr int kGroups = N <= 4 ? 2 : 1;  // of 16 keys, a warp takes of a stage
+  static constexpr int kKeys = 16 * kGroups * kWarps;
   static constexpr int kStage = kKeys / kCodeTokens * kv4_tile(N);
-  static constexpr int kStages = N <= 2 ? 8 : N <= 4 ? 6 : 4;
+  static constexpr int kStages = N <= 2 ? 4 : N == 3 ? 4 : N == 4 ? 3 : 4;
   static constexpr int kPad = kCols + 4;  // row of the joining buffer, in floats
   static constexpr int kBuf = kRows * kPad * 4;
   static constexpr int kMl = kWarps * 2 * kRows * 4;
@@ -50,6 +51,13 @@ __device__ __forceinline__ void mma(float* c, uint32_t a0, uint32_t a1, uint32_t
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same from zero.
+__device__ __forceinline__ void mma_first(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t r;
@@ -104,12 +112,16 @@ template <int kRows>
 __device__ __forceinline__ int row_tiles(const AttnParams& p, const AttnReq& r) {
   return (int)(((int64_t)r.ql * p.group + kRows - 1) / kRows);
 }
-__device__ __forceinline__ int tiles_of(int n) { return n < 1 ? 0 : (n - 1) / kKeys + 1; }
+template <int kKeys>
+__device__ __forceinline__ int tiles_of(int n) {
+  return n < 1 ? 0 : (n - 1) / kKeys + 1;
+}
+template <int kKeys>
 __device__ __forceinline__ int key_tiles(const AttnReq& r) {
-  const int n = tiles_of(r.kvl);
+  const int n = tiles_of<kKeys>(r.kvl);
   return n < 1 ? 1 : n;
 }
-template <int kRows>
+template <int kRows, int kKeys>
 __device__ __forceinline__ Few4Item few_item(const AttnParams& p, const AttnReq& r, int req, int64_t item, int rt) {
   Few4Item it;
   it.req = req;
@@ -118,7 +130,7 @@ __device__ __forceinline__ Few4Item few_item(const AttnParams& p, const AttnReq&
   const int64_t left = (int64_t)r.ql * p.group - it.row0;
   it.rows = left < kRows ? (int)left : kRows;
   it.r = r;
-  it.tiles = tiles_of(attn_limit(p, r, (it.row0 + it.rows - 1) / p.group));
+  it.tiles = tiles_of<kKeys>(attn_limit(p, r, (it.row0 + it.rows - 1) / p.group));
   return it;
 }
 __device__ __forceinline__ bool few_inside(const AttnParams& p, const Few4Item& x, int row) {
@@ -164,7 +176,7 @@ __device__ __forceinline__ float query_words(const uint4* raw, bool f16, uint32_
 template <int N, int kR>
 __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_few(const __grid_constant__ AttnParams p) {
   using C = Few4Cfg<N, kR>;
-  constexpr int kRows = C::kRows;
+  constexpr int kRows = C::kRows, kKeys = C::kKeys, kGroups = C::kGroups;
   extern __shared__ char raw[];
   char* ring = (char*)(((uintptr_t)raw + 127) & ~(uintptr_t)127);
   float* bufs = (float*)(ring + C::kStages * C::kStage);
@@ -188,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
   const AttnRange range = attn_range<kThreads>(p.batch, blockIdx.x, gridDim.x, scratch, [&](int i) -> int64_t {
     if (attn_falls(p, i)) return -1;
     const AttnReq r = attn_req(p, i);
-    return (int64_t)p.kv_heads * row_tiles<kRows>(p, r) * key_tiles(r);
+    return (int64_t)p.kv_heads * row_tiles<kRows>(p, r) * key_tiles<kKeys>(r);
   });
   if (tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (range.begin >= range.end) return;
@@ -196,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
 
   int req = range.req;
   AttnReq r = attn_req(p, req);
-  int rt = row_tiles<kRows>(p, r), cost = key_tiles(r);
+  int rt = row_tiles<kRows>(p, r), cost = key_tiles<kKeys>(r);
   int64_t item = range.off / cost;
   int t0 = (int)(range.off % cost);
   int64_t left = range.end - range.begin;
@@ -209,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
         if (++req >= p.batch) return false;
         r = attn_req(p, req);
         rt = row_tiles<kRows>(p, r);
-        cost = key_tiles(r);
+        cost = key_tiles<kKeys>(r);
       } while (rt == 0);
     }
     return left > 0;
@@ -217,12 +229,12 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
 
   if (warp == kWarps) {
     // ---- copies: a page's part of a stage is contiguous ----
-    const int box = p.box, per = kKeys / box;  // keys of a copy; copies of a stage
+    const int box = p.box < kKeys ? p.box : kKeys, per = kKeys / box;  // keys of a copy; copies of a stage
     const uint32_t bytes = (uint32_t)(box / kCodeTokens * kv4_tile(N));
     bool ok = true;
     uint32_t done = 0;
     do {
-      const Few4Item x = few_item<kRows>(p, r, req, item, rt);
+      const Few4Item x = few_item<kRows, kKeys>(p, r, req, item, rt);
       const int seg = (int)(left < cost - t0 ? left : cost - t0);
       const int last = t0 + seg < x.tiles ? t0 + seg : x.tiles;
       const int32_t* row = p.table + (int64_t)req * p.table_stride;
@@ -268,11 +280,11 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
 
   // ---- products ----
   const int g = lane >> 2, q = lane & 3;
-  const uint32_t ring_at = smem_u32(ring) + warp * 2 * kv4_tile(N);  // this warp's two tiles of a stage
+  const uint32_t ring_at = smem_u32(ring) + warp * 2 * kGroups * kv4_tile(N);  // this warp's tiles of a stage
   const uint32_t k_at = kv4_key(N, g) + q * 4 * N, v_at = kv4_value(N, q) + g * 4 * N;
-  uint32_t it = 0;  // stages used so far
+  uint32_t s = 0, phase = 0;  // the stage at hand
   for (;;) {
-    const Few4Item x = few_item<kRows>(p, r, req, item, rt);
+    const Few4Item x = few_item<kRows, kKeys>(p, r, req, item, rt);
     const int seg = (int)(left < cost - t0 ? left : cost - t0);
     const int last = t0 + seg < x.tiles ? t0 + seg : x.tiles;
     const bool starts = t0 == 0, ends = t0 + seg == cost;
@@ -300,9 +312,12 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
         lim[i][e] = mine < x.rows ? attn_limit(p, r, (x.row0 + mine) / p.group) : 0;
       }
     }
-    const int lim_lo = attn_limit(p, r, x.row0 / p.group);  // what every valid row sees
+    // what every valid row sees, and what any does
+    const int lim_lo = attn_limit(p, r, x.row0 / p.group), lim_hi = attn_limit(p, r, (x.row0 + x.rows - 1) / p.group);
 
-    float o[kR][2 * N][4], m[kR][2], l[kR][2];
+    // Of each row: the running maximum (a reference that lags behind it), the sum,
+    // what a score's exponent is less by, and the score above which the reference grows.
+    float o[kR][2 * N][4], m[kR][2], l[kR][2], off[kR][2], most[kR][2];
 #pragma unroll
     for (int i = 0; i < kR; ++i) {
 #pragma unroll
@@ -311,116 +326,138 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
         for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
       m[i][0] = m[i][1] = -INFINITY;
       l[i][0] = l[i][1] = 0.f;
+      off[i][0] = off[i][1] = L::kLift;
+      most[i][0] = most[i][1] = -INFINITY;
     }
 
-    for (int t = t0; t < last; ++t, ++it) {
-      const int s = it % C::kStages;
+    for (int t = t0; t < last; ++t) {
       // having given up, the block still ends in order
-      (void)__all_sync(~0u, wait_bar(&full[s], (it / C::kStages) & 1, &gave_up, g_few4_counts));
-      const uint32_t a_at = ring_at + s * C::kStage, b_at = a_at + kv4_tile(N);
-
-      // S^T = K Q^T for 16 keys: rows g (first tile) and g + 8 (second)
-      float sc[kR][2][4];
+      (void)__all_sync(~0u, wait_bar(&full[s], phase, &gave_up, g_few4_counts));
+      const uint32_t at = ring_at + s * C::kStage;
+      const int key0 = t * kKeys + 16 * kGroups * warp;
+      if (key0 < lim_hi) {
+        // S^T = K Q^T, 16 keys at a time: rows g (a tile of 8) and g + 8 (the next)
+        float sc[kGroups][kR][4];
 #pragma unroll
-      for (int i = 0; i < kR; ++i)
+        for (int u = 0; u < kGroups; ++u) {
+          const uint32_t a_at = at + 2 * u * kv4_tile(N), b_at = a_at + kv4_tile(N);
+          float half[kR][4];  // every second product, so that a chain is half as long
+          uint32_t wa[N], wb[N], sa, oa, sb, ob;
+          load_words<N>(wa, a_at + k_at);
+          load_words<N>(wb, b_at + k_at);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[i][0][e] = sc[i][1][e] = 0.f;
-      {
-        uint32_t wa[N], wb[N], sa, oa, sb, ob;
-        load_words<N>(wa, a_at + k_at);
-        load_words<N>(wb, b_at + k_at);
+          for (int w = 0; w < N; ++w) {
+            // the group of word q N + w: the same for all of a lane's words where N is 1, 2 or 4
+            if (w == 0 || (N == 8 && w == 4) || (N & (N - 1)) != 0) {
+              const uint32_t mk = kv4_key_marks(N, g) + 2 * ((q * N + w) >> 2);
+              kv4_key_step(load_u16(a_at + mk), sa, oa);
+              kv4_key_step(load_u16(b_at + mk), sb, ob);
+            }
+            uint32_t a[4], b[4];
+            kv4_word(wa[w], sa, oa, a);
+            kv4_word(wb[w], sb, ob, b);
 #pragma unroll
-        for (int w = 0; w < N; ++w) {
-          // the group of word q N + w: the same for all of a lane's words where N is 1, 2 or 4
-          if (w == 0 || (N == 8 && w == 4) || (N & (N - 1)) != 0) {
-            const uint32_t mk = kv4_key_marks(N, g) + 2 * ((q * N + w) >> 2);
-            kv4_key_step(load_u16(a_at + mk), sa, oa);
-            kv4_key_step(load_u16(b_at + mk), sb, ob);
-          }
-          uint32_t a[4], b[4];
-          kv4_word(wa[w], sa, oa, a);
-          kv4_word(wb[w], sb, ob, b);
-#pragma unroll
-          for (int i = 0; i < kR; ++i) {
-            mma(sc[i][0], a[0], b[0], a[1], b[1], qf[i][2 * w][0], qf[i][2 * w][1]);
-            mma(sc[i][1], a[2], b[2], a[3], b[3], qf[i][2 * w + 1][0], qf[i][2 * w + 1][1]);
-          }
-        }
-      }
-      const uint32_t held = there[s];
-      const bool partly = lim_lo - t * kKeys < kKeys || held != 0xFFu;
-      bool grows = false;
-#pragma unroll
-      for (int i = 0; i < kR; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = (sc[i][0][e] + sc[i][1][e]) * by[i][e & 1];
-          if (partly) {
-            const int key = 16 * warp + g + 8 * (e >> 1);
-            if (t * kKeys + key >= lim[i][e & 1] || !(held >> (key >> 3) & 1u)) v = -INFINITY;
-          }
-          sc[i][0][e] = v;
-          grows |= v > m[i][e & 1] + kLag;
-        }
-      if (__any_sync(~0u, grows)) {
-#pragma unroll
-        for (int i = 0; i < kR; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float mx = fmaxf(sc[i][0][e], sc[i][0][2 + e]);
-            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
-            const float mn = L::reference(fmaxf(m[i][e], mx));
-            const float alpha = ex2(m[i][e] - (mn == -INFINITY ? 0.f : mn));
-            m[i][e] = mn;
-            l[i][e] *= alpha;
-#pragma unroll
-            for (int n = 0; n < 2 * N; ++n) {
-              o[i][n][e] *= alpha;
-              o[i][n][2 + e] *= alpha;
+            for (int i = 0; i < kR; ++i) {
+              if (w == 0) {
+                mma_first(sc[u][i], a[0], b[0], a[1], b[1], qf[i][2 * w][0], qf[i][2 * w][1]);
+                mma_first(half[i], a[2], b[2], a[3], b[3], qf[i][2 * w + 1][0], qf[i][2 * w + 1][1]);
+              } else {
+                mma(sc[u][i], a[0], b[0], a[1], b[1], qf[i][2 * w][0], qf[i][2 * w][1]);
+                mma(half[i], a[2], b[2], a[3], b[3], qf[i][2 * w + 1][0], qf[i][2 * w + 1][1]);
+              }
             }
           }
-      }
-      uint32_t pb[kR][2];
 #pragma unroll
-      for (int i = 0; i < kR; ++i) {
-        float v[4];
+          for (int i = 0; i < kR; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float ref = m[i][e & 1] == -INFINITY ? 0.f : m[i][e & 1];
-          v[e] = ex2(sc[i][0][e] + (L::kLift - ref));
+            for (int e = 0; e < 4; ++e) sc[u][i][e] += half[i][e];
         }
-        l[i][0] += v[0] + v[2];
-        l[i][1] += v[1] + v[3];
-        pb[i][0] = transpose8(pack_f16(v[0], v[1]));
-        pb[i][1] = transpose8(pack_f16(v[2], v[3]));
-      }
-
-      // O^T += V^T P^T: rows are elements, 4 (N g + w) on from the word's
-      {
-        uint32_t wa[N], wb[N], sa, oa, sb, ob;
-        load_words<N>(wa, a_at + v_at);
-        load_words<N>(wb, b_at + v_at);
+        const uint32_t held = there[s] >> 2 * kGroups * warp & ((1u << 2 * kGroups) - 1);
+        if (lim_lo - key0 < 16 * kGroups || held != (1u << 2 * kGroups) - 1) {
 #pragma unroll
-        for (int w = 0; w < N; ++w) {
-          if (w == 0 || (N & (N - 1)) != 0) {
-            const uint32_t mk = kv4_value_marks(N, q) + 4 * ((N * g + w) >> 3);
-            kv4_value_step(load_u32(a_at + mk), sa, oa);
-            kv4_value_step(load_u32(b_at + mk), sb, ob);
-          }
-          uint32_t a[4], b[4];
-          kv4_word(wa[w], sa, oa, a);
-          kv4_word(wb[w], sb, ob, b);
+          for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+            for (int i = 0; i < kR; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (key0 + 16 * u + g + 8 * (e >> 1) >= lim[i][e & 1] || !(held >> (2 * u + (e >> 1)) & 1u)) sc[u][i][e] = -INFINITY;
+        }
+        bool grows = false;
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+          for (int i = 0; i < kR; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) grows |= sc[u][i][e] > most[i][e & 1];
+        if (__any_sync(~0u, grows)) {
+#pragma unroll
+          for (int i = 0; i < kR; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float mx = fmaxf(sc[0][i][e], sc[0][i][2 + e]);
+#pragma unroll
+              for (int u = 1; u < kGroups; ++u) mx = fmaxf(mx, fmaxf(sc[u][i][e], sc[u][i][2 + e]));
+              mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
+              mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
+              mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
+              const float mn = L::reference(fmaxf(m[i][e], mx * by[i][e])), safe = mn == -INFINITY ? 0.f : mn;
+              const float alpha = ex2(m[i][e] - safe);
+              m[i][e] = mn;
+              off[i][e] = L::kLift - safe;
+              most[i][e] = (mn + kLag) / by[i][e];
+              l[i][e] *= alpha;
+#pragma unroll
+              for (int n = 0; n < 2 * N; ++n) {
+                o[i][n][e] *= alpha;
+                o[i][n][2 + e] *= alpha;
+              }
+            }
+        }
+        uint32_t pb[kGroups][kR][2];
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u)
 #pragma unroll
           for (int i = 0; i < kR; ++i) {
-            mma(o[i][2 * w], a[0], a[1], b[0], b[1], pb[i][0], pb[i][1]);
-            mma(o[i][2 * w + 1], a[2], a[3], b[2], b[3], pb[i][0], pb[i][1]);
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = ex2(fmaf(sc[u][i][e], by[i][e & 1], off[i][e & 1]));
+            l[i][0] += v[0] + v[2];
+            l[i][1] += v[1] + v[3];
+            pb[u][i][0] = transpose8(pack_f16(v[0], v[1]));
+            pb[u][i][1] = transpose8(pack_f16(v[2], v[3]));
+          }
+
+        // O^T += V^T P^T: rows are elements, 4 (N g + w) on from the word's
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+          const uint32_t a_at = at + 2 * u * kv4_tile(N), b_at = a_at + kv4_tile(N);
+          uint32_t wa[N], wb[N], sa, oa, sb, ob;
+          load_words<N>(wa, a_at + v_at);
+          load_words<N>(wb, b_at + v_at);
+#pragma unroll
+          for (int w = 0; w < N; ++w) {
+            if (w == 0 || (N & (N - 1)) != 0) {
+              const uint32_t mk = kv4_value_marks(N, q) + 4 * ((N * g + w) >> 3);
+              kv4_value_step(load_u32(a_at + mk), sa, oa);
+              kv4_value_step(load_u32(b_at + mk), sb, ob);
+            }
+            uint32_t a[4], b[4];
+            kv4_word(wa[w], sa, oa, a);
+            kv4_word(wb[w], sb, ob, b);
+#pragma unroll
+            for (int i = 0; i < kR; ++i) {
+              mma(o[i][2 * w], a[0], a[1], b[0], b[1], pb[u][i][0], pb[u][i][1]);
+              mma(o[i][2 * w + 1], a[2], a[3], b[2], b[3], pb[u][i][0], pb[u][i][1]);
+            }
           }
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty[s]);
+      if (++s == C::kStages) {
+        s = 0;
+        phase ^= 1;
+      }
     }
 
     // ---- join the warps ----

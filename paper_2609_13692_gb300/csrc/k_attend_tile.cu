@@ -63,7 +63,9 @@ namespace {
 __device__ uint32_t g_tile_counts[kKvCounts];
 
 constexpr int kKeys = 128;     // keys of a tile
-constexpr int kThreads = 384;
+constexpr int kCodeWarps = 7;  // cache in 4 bits: warps that widen codes
+template <bool kCodes>
+constexpr int kThreads = kCodes ? 512 : 384;
 constexpr int kOddSets = 4;    // items whose notes are kept apart
 constexpr int kList = 32;      // items listed at a time
 constexpr int kHeldSets = 16;  // key tiles whose page marks are kept apart
@@ -89,8 +91,12 @@ struct TileCfg {
   // Registers a thread: of the four warps without rows, and of the rows' eight.
   // (Of 88 with 208 and 72 with 216: 2,048 tokens over 10,000 keys, heads of 64,
   // 200 and 180 us; 28 ragged chunks, heads of 96, 372 and 383.)
-  static constexpr int kRoleRegs = HDP == 64 ? 72 : 88, kRowRegs = HDP == 64 ? 216 : 208;
-  static_assert(kRoleRegs + 2 * kRowRegs <= 3 * 168);
+  // (The cache in 4 bits has eight warps without rows.)
+  template <bool kCodes>
+  static constexpr int kRoleRegs = kCodes || HDP == 64 ? 72 : 88;
+  template <bool kCodes>
+  static constexpr int kRowRegs = kCodes ? 184 : HDP == 64 ? 216 : 208;
+  static_assert(kRoleRegs<false> + 2 * kRowRegs<false> <= 3 * 168 && 2 * kRoleRegs<true> + 2 * kRowRegs<true> <= 4 * 128);
   static constexpr int kSmem = 1024 + kQ + kSlots * kSlot + 2048;
 };
 
@@ -144,7 +150,10 @@ __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parit
 __device__ __forceinline__ void mbar_arrive_n(unsigned long long* bar, uint32_t n) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
 }
-__device__ __forceinline__ void bar_all() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
+template <bool kCodes>
+__device__ __forceinline__ void bar_all() {
+  asm volatile("bar.sync 1, %0;" ::"n"(kThreads<kCodes>) : "memory");
+}
 
 // The same for the warps that have time: polls take issue slots that the rows'
 // arithmetic needs.  (4,096 tokens over 20,480 keys: 797 us with warp 11's polls
@@ -443,12 +452,10 @@ __device__ void fill_list(const AttnParams& p, TileShared& sh) {
 
 // ---- the cache in 4 bits ----
 //
-// Its kernel is the same but for where the operands come from: warps 9 to 11
+// Its kernel is the same but for where the operands come from: warps 9 to 15
 // read codes and write f16 keys and values where the copies would have put
 // them, and each row's thread its own query.  Codes stand for finite values
 // whatever their bytes, so there is nothing to look for in masked ones.
-constexpr int kCodeWarps = 3;
-
 template <bool F16, bool kCodes>
 __device__ __forceinline__ uint32_t pack_as(const AttnParams& p, float lo, float hi) {
   if (!kCodes) return pack2<F16>(lo, hi);
@@ -501,7 +508,7 @@ struct CodeChunk {
   uint32_t marks;
 };
 
-// By warps 9 to 11: f16 keys and values of the block's key tiles, each in its
+// By warps 9 to 15: f16 keys and values of the block's key tiles, each in its
 // slot of the ring.  A tile of 8 tokens has 8 n chunks of 16 bytes of either;
 // a warp takes tiles of 8 in turn, a lane the same chunk of each (kPer of them
 // with more than 4 groups; two tiles at once with 2).  A chunk is read as soon as the one
@@ -539,8 +546,8 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
   const uint32_t from = 16 * in, values_from = kv4_value(n, 0);
 
   // Step i, half v (0 keys, 1 values): the tile of 8 that it is about.
-  // (The warp that has one step more than the others is another for values.)
-  auto tile8 = [&](int v, int i) { return ((i / kPer) * kCodeWarps + (v ? (me + 1) % kCodeWarps : me)) * kTogether + second; };
+  // (The warps that have one step more than the others are others for values.)
+  auto tile8 = [&](int v, int i) { return ((i / kPer) * kCodeWarps + (v ? (me + 2) % kCodeWarps : me)) * kTogether + second; };
 
   TileItem w;
   int k = 0;
@@ -637,7 +644,7 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
 
 // kCodes: over the cache in 4 bits, F16 being the type of its products.
 template <int HDP, bool F16, bool kCodes>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __grid_constant__ AttnParams p) {
   using C = TileCfg<HDP>;
   extern __shared__ char raw[];
   char* base = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
@@ -671,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   // The requests, in the room of the ring: first item, new tokens, keys, pairs.
   int4* const reqs = (int4*)ring;
   {
-    const int per = (p.batch + kThreads - 1) / kThreads, lo = min(tid * per, p.batch), hi = min(lo + per, p.batch);
+    const int per = (p.batch + kThreads<kCodes> - 1) / kThreads<kCodes>, lo = min(tid * per, p.batch), hi = min(lo + per, p.batch);
     int64_t sum = 0, keys = 0;  // items and keys
     bool bad = false;
     for (int i = lo; i < hi; ++i) {
@@ -696,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     bad = __syncthreads_or(bad);
     int64_t before = inc - sum, all = 0;
     keys = 0;
-    for (int w = 0; w < kThreads / 32; ++w) {
+    for (int w = 0; w < kThreads<kCodes> / 32; ++w) {
       if (w < warp) before += sh.scratch[w];
       all += sh.scratch[w];
       keys += sh.scratch[16 + w];
@@ -724,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
     const int4 r = reqs[at_req];
     return pair_cost(p, r.y, r.z, (item - r.x) % r.w);
   };
-  const AttnRange range = attn_range<kThreads>((int)gridDim.x, blockIdx.x, gridDim.x, sh.scratch, [&](int c) -> int64_t {
+  const AttnRange range = attn_range<kThreads<kCodes>>((int)gridDim.x, blockIdx.x, gridDim.x, sh.scratch, [&](int c) -> int64_t {
     int64_t sum = 0;
     const int64_t end = stride > 1 ? items : min((int64_t)items, (int64_t)(c + 1) * run);
     for (int64_t i = stride > 1 ? c : (int64_t)c * run; i < end; i += stride) sum += cost_of((int)i);
@@ -765,7 +772,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   __syncthreads();  // the requests are done with: the ring is free
 
   // rows that no copy fills (whole tokens only in a tile) stay 0
-  for (int e = tid; e < C::kQ / 16; e += kThreads) ((uint4*)qbuf)[e] = make_uint4(0, 0, 0, 0);
+  for (int e = tid; e < C::kQ / 16; e += kThreads<kCodes>) ((uint4*)qbuf)[e] = make_uint4(0, 0, 0, 0);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)) : "memory");
@@ -781,25 +788,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
   auto next_item = [&](int& k) -> bool {
     if (++k < sh.count) return true;
     if (!sh.more) return false;
-    bar_all();
+    bar_all<kCodes>();
     if (warp == 11) fill_list(p, sh);
-    bar_all();
+    bar_all<kCodes>();
     k = 0;
     return true;
   };
   // A role that has given up still meets the others.
   auto leave = [&] {
     while (sh.more) {
-      bar_all();
+      bar_all<kCodes>();
       if (warp == 11) fill_list(p, sh);
-      bar_all();
+      bar_all<kCodes>();
     }
   };
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::template kRoleRegs<kCodes>));
     if (kCodes && warp > 8) {
-      // ---- codes: warps 9 to 11 make f16 keys and values of them ----
+      // ---- codes: warps 9 to 15 make f16 keys and values of them ----
       widen_codes<HDP>(p, sh, ring, next_item, leave);
     } else if (warp == 9 || warp == 10) {
       // ---- copies: warp 9 queries and keys, warp 10 values ----
@@ -1132,7 +1139,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tile(const __grid_consta
       if (!ok) leave();
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRowRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::template kRowRegs<kCodes>));
     // ---- one row per thread ----
     TileItem w;
     int k = 0;
@@ -1434,13 +1441,13 @@ cudaError_t launch(const AttnParams& p, int sms, int device, cudaStream_t stream
   static const cudaError_t fits = [] {
     cudaFuncAttributes a;
     const cudaError_t e = cudaFuncGetAttributes(&a, k_attend_tile<HDP, F16, kCodes>);
-    return e != cudaSuccess ? e : a.numRegs * 3 >= C::kRoleRegs + 2 * C::kRowRegs ? cudaSuccess : cudaErrorInvalidConfiguration;
+    return e != cudaSuccess ? e : a.numRegs * (kThreads<kCodes> / 128) >= (kCodes ? 2 : 1) * C::template kRoleRegs<kCodes> + 2 * C::template kRowRegs<kCodes> ? cudaSuccess : cudaErrorInvalidConfiguration;
   }();
   if (fits != cudaSuccess) return fits;
   static std::atomic<uint64_t> allowed;
   cudaError_t e = kv_allow_smem(k_attend_tile<HDP, F16, kCodes>, C::kSmem, device, allowed);
   if (e != cudaSuccess) return e;
-  k_attend_tile<HDP, F16, kCodes><<<sms, kThreads, C::kSmem, stream>>>(p);
+  k_attend_tile<HDP, F16, kCodes><<<sms, kThreads<kCodes>, C::kSmem, stream>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(sms, C::kRows / 32);

@@ -401,7 +401,7 @@ mpt_status mpt_kv4_attend(const mpt_kv4_cache* c, int32_t type, const void* q, c
   p.toks = 128 / p.group;
   p.item_toks = p.toks * (p.dim > 128 ? 1 : 2);
   p.wide = p.dim % 16 == 0 && mpt::aligned(out, 32) && (heads == 1 || p.out_head % 16 == 0) && (tokens == 1 || p.out_tok % 16 == 0);
-  p.box = c->page_size < 64 ? c->page_size : 64;
+  p.box = c->page_size;
   const bool tile = most * p.group > 16 && c->batch <= mpt::kTileBatch;
   const cudaError_t e = tile ? mpt::launch_attend4_tile(p, sms, device, (cudaStream_t)stream)
                              : mpt::launch_attend4_few(p, most * p.group < 16 ? (int)(most * p.group) : 16, sms, device, (cudaStream_t)stream);
