@@ -350,8 +350,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
             // the group of word q N + w: the same for all of a lane's words where N is 1, 2 or 4
             if (w == 0 || (N == 8 && w == 4) || (N & (N - 1)) != 0) {
               const uint32_t mk = kv4_key_marks(N, g) + 2 * ((q * N + w) >> 2);
-              kv4_key_step(load_u16(a_at + mk), sa, oa);
-              kv4_key_step(load_u16(b_at + mk), sb, ob);
+              kv4_key_steps(load_u16(a_at + mk), load_u16(b_at + mk), sa, oa, sb, ob);
             }
             uint32_t a[4], b[4];
             kv4_word(wa[w], sa, oa, a);

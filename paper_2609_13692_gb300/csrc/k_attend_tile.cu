@@ -321,6 +321,10 @@ __device__ __forceinline__ void store32(void* to, const uint32_t* v) {
 // (Natural order and columns: 28 requests of up to 700 tokens over 6,000 keys of
 // 24 heads, 380 MB: 541 and 488 us; 4,096 tokens over 20,480 keys of 8 heads,
 // 84 MB: 785 and 840 us, the blocks reading the same keys at the same time.)
+// The cache in 4 bits is always taken in columns: besides, they mix items of two
+// row tiles with those of one among the blocks (28 requests of up to 700 tokens
+// over 700 to 6,000 keys, 24 heads on 8 of 96: 678 and 507 us; of 128: 719 and
+// 520; 4,096 tokens over 20,480 keys: 968 and 969).
 constexpr int64_t kNaturalBytes = 100ll << 20;  // of 126 MB of L2
 __device__ __forceinline__ int pairs_of(const AttnParams& p, int ql) {
   return (int)(((int64_t)ql + p.item_toks - 1) / p.item_toks);
@@ -468,13 +472,18 @@ __device__ __forceinline__ uint32_t pack_as(const AttnParams& p, float lo, float
 // 2^-14 of it exactly; returns what takes it out again.  nullptr: zeros.
 template <int HDP>
 __device__ __forceinline__ float stage_query(const char* q, int dim, bool f16, char* to, int r) {
+  uint4 u[HDP / 8];  // all loads are in flight together
+#pragma unroll
+  for (int c = 0; c < HDP / 8; ++c) {
+    u[c] = make_uint4(0, 0, 0, 0);
+    if (q && c * 8 < dim) u[c] = __ldg((const uint4*)(q + 16 * c));
+  }
   float by = 1.f, back = 1.f;
-  if (!f16 && q) {
+  if (!f16) {
     uint32_t top = 0;
-#pragma unroll 8
-    for (int c = 0; c < dim; c += 8) {
-      const uint4 u = *(const uint4*)(q + 2 * c);
-      const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int c = 0; c < HDP / 8; ++c) {
+      const uint32_t v[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = max(top, max(v[i] << 16 & 0x7FFFFFFFu, v[i] & 0x7FFF0000u));
     }
@@ -483,11 +492,9 @@ __device__ __forceinline__ float stage_query(const char* q, int dim, bool f16, c
     by = __uint_as_float((uint32_t)(127 - e) << 23);
     back = __uint_as_float((uint32_t)(127 + e) << 23);
   }
-#pragma unroll 8
-  for (int ch = 0; ch < HDP / 8; ++ch) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (q && ch * 8 < dim) u = *(const uint4*)(q + 16 * ch);
-    uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int c = 0; c < HDP / 8; ++c) {
+    uint32_t v[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
     if (!f16) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = pack2<true>(__uint_as_float(v[i] << 16) * by, __uint_as_float(v[i] & 0xFFFF0000u) * by);
@@ -497,7 +504,7 @@ __device__ __forceinline__ float stage_query(const char* q, int dim, bool f16, c
     o.y = __byte_perm(v[0], v[2], 0x7632);
     o.z = __byte_perm(v[1], v[3], 0x5410);
     o.w = __byte_perm(v[1], v[3], 0x7632);
-    *(uint4*)(to + (ch >> 3) * 128 * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = o;
+    *(uint4*)(to + (c >> 3) * 128 * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = o;
   }
   return back;
 }
@@ -711,8 +718,7 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
     for (int i = lo; i < hi; ++i) reqs[i].x += (int)before;
     if (tid == 0) {
       sh.items = bad || all > INT32_MAX ? 0 : (int)all;  // (2^31 items: q would not fit in memory)
-      const int64_t bytes = kCodes ? 36 * kv4_groups(p.dim) : p.dim * 4;  // of a key and its value
-      sh.stride = keys * p.kv_heads * bytes > kNaturalBytes ? (int)gridDim.x : 1;
+      sh.stride = kCodes || keys * p.kv_heads * p.dim * 4 > kNaturalBytes ? (int)gridDim.x : 1;
     }
     __syncthreads();
   }
@@ -1147,6 +1153,21 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
     const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + s * 128 + lanes, t_o = tmem + 256 + s * 128 + lanes;
     uint32_t scored = 0, done = 0, item = 0, gt = 0, steps = 0;  // scored: phases of this row tile's buffer and of buffer 2
     bool ok = true;
+    // kCodes: an item's queries for this row tile; returns the row's scale.  Where
+    // the row has read the last scores of the item before, its queries are free.
+    auto stage = [&](const TileItem& x) -> float {
+      if (x.count(s) == 0) return p.scale_log2;
+      const int64_t t = (int64_t)x.tok0 + s * p.toks + r_tok, at = x.e.q0 + t, head = (int64_t)x.e.head * p.group + sub;
+      const bool mine = r_tok < p.toks && t < x.e.ql && !KV_BAD(g_tile_counts, at >= 0 && at < p.tokens && head >= 0 && head < p.heads);
+      const float back =
+          stage_query<HDP>(mine ? p.q + 2 * (at * p.q_tok + head * p.q_head) : nullptr, p.dim, p.f16, qbuf + s * C::kBlk * 128 * 128, r);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.q_ready[s]);
+      return kv4_scale(p.scale_log2, back);
+    };
+    bool staged = false;
+    float scale_next = 0.f;
     do {
       w.load(p, &sh.list[k]);
       const int64_t first_tok = (int64_t)w.tok0 + s * p.toks;
@@ -1154,17 +1175,8 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
       const int tok = valid ? (int)first_tok + r_tok : 0;
       float scale_log2 = p.scale_log2;
       if constexpr (kCodes) {
-        // This row tile's scores of the item before have all been read here, so
-        // its queries are free.
-        if (w.count(s) > 0) {
-          const int64_t at = (int64_t)w.e.q0 + tok, head = (int64_t)w.e.head * p.group + sub;
-          const bool mine = valid && !KV_BAD(g_tile_counts, at >= 0 && at < p.tokens && head >= 0 && head < p.heads);
-          scale_log2 = kv4_scale(scale_log2, stage_query<HDP>(mine ? p.q + 2 * (at * p.q_tok + head * p.q_head) : nullptr, p.dim, p.f16,
-                                                              qbuf + s * C::kBlk * 128 * 128, r));
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.q_ready[s]);
-        }
+        scale_log2 = staged ? scale_next : stage(w);
+        staged = false;
       }
       const int lim = valid ? w.limit(p, tok) : INT32_MAX;
       const int lim_tile = first_tok < w.e.ql ? w.limit(p, (int)first_tok) : 0;  // what every row of the tile sees
@@ -1263,6 +1275,16 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
         if (lane == 0) mbar_arrive(&sh.p_ready[buf]);
       }
       if (!ok) break;
+      if constexpr (kCodes) {
+        // The next item's queries before this one's output, so that its first
+        // scores are made meanwhile.
+        if (k + 1 < sh.count) {
+          TileItem next;
+          next.load(p, &sh.list[k + 1]);
+          scale_next = stage(next);
+          staged = true;
+        }
+      }
       gt += w.tiles;
       const uint32_t* odd = nullptr;
       if (!kCodes && w.tiles > 0) odd = sh.odd[item++ % kOddSets];

@@ -65,6 +65,24 @@ __device__ __forceinline__ void kv4_marks(uint32_t steps, uint32_t offsets, uint
 __device__ __forceinline__ void kv4_key_step(uint32_t marks, uint32_t& step, uint32_t& off) {
   kv4_marks(__byte_perm(marks, 0, 0x4040), __byte_perm(marks, 0, 0x4141), step, off);
 }
+// Of two keys' groups at once.
+__device__ __forceinline__ uint32_t kv4_low(uint32_t x) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tmov.b32 %0, {l, l};\n\t}" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t kv4_high(uint32_t x) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tmov.b32 %0, {h, h};\n\t}" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ void kv4_key_steps(uint32_t marks_a, uint32_t marks_b, uint32_t& step_a, uint32_t& off_a, uint32_t& step_b,
+                                              uint32_t& off_b) {
+  uint32_t step, off;
+  // (of 16 bits each: bytes 2 and 3 are 0)
+  kv4_marks(__byte_perm(marks_a, marks_b, 0x2420), __byte_perm(marks_a, marks_b, 0x2521), step, off);
+  step_a = kv4_low(step), off_a = kv4_low(off), step_b = kv4_high(step), off_b = kv4_high(off);
+}
 // Of a pair of values' group, low half the even token.  `marks`: its four bytes.
 __device__ __forceinline__ void kv4_value_step(uint32_t marks, uint32_t& step, uint32_t& off) {
   kv4_marks(__byte_perm(marks, 0, 0x4140), __byte_perm(marks, 0, 0x4342), step, off);
