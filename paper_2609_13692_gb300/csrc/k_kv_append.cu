@@ -119,16 +119,32 @@ __device__ __forceinline__ void turn(const Turn& u, bool adjacent, bool first, c
   }
 }
 
+// x / y as a division rounds it, with inv = 1 / y rounded to nearest: one
+// correction of the product gives the nearest quotient (Markstein, 1990), but
+// where it is below the normal numbers, which no step or code depends on.
+__device__ __forceinline__ float quotient(float x, float y, float inv) {
+  const float q = __fmul_rn(x, inv);
+  return __fmaf_rn(__fmaf_rn(-q, y, x), inv, q);
+}
+
 // Codes of a group of 32 elements, 8 a lane: the lane's two pieces, and in every
 // lane the group's marks (step | offset << 8).  `has`: the lane has elements.
 __device__ __forceinline__ uint32_t encode(float* f, bool has, int lane, uint32_t& marks) {
-  float lo = INFINITY, hi = -INFINITY;
+  float lo = f[0], hi = f[0], odd = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float x = f[i] == f[i] ? f[i] : 0.f;
-    f[i] = fminf(fmaxf(x, -kv4_most), kv4_most);
     lo = fminf(lo, f[i]);
     hi = fmaxf(hi, f[i]);
+    odd = __fmaf_rn(f[i], 0.f, odd);  // NaN from then on, if f[i] is that or an infinity
+  }
+  if (__any_sync(~0u, odd != 0.f || lo < -kv4_most || hi > kv4_most)) {
+    lo = INFINITY, hi = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f[i] = fminf(fmaxf(f[i] == f[i] ? f[i] : 0.f, -kv4_most), kv4_most);
+      lo = fminf(lo, f[i]);
+      hi = fmaxf(hi, f[i]);
+    }
   }
   if (!has) lo = INFINITY, hi = -INFINITY;
 #pragma unroll
@@ -137,29 +153,25 @@ __device__ __forceinline__ uint32_t encode(float* f, bool has, int lane, uint32_
     hi = fmaxf(hi, __shfl_xor_sync(~0u, hi, d));
   }
   const float own = __shfl_sync(~0u, f[0], lane & ~3);  // the group's first element
-  float step = fmaxf(fmaxf(__fdiv_rn(__fsub_rn(hi, lo), 15.f), __fdiv_rn(fmaxf(hi, -lo), 120.f)), 0x1p-18f);
+  float step = fmaxf(fmaxf(quotient(__fsub_rn(hi, lo), 15.f, 1.f / 15.f), quotient(fmaxf(hi, -lo), 120.f, 1.f / 120.f)), 0x1p-18f);
   step = __uint_as_float((__float_as_uint(step) + 0xFFFFFu) & ~0xFFFFFu);
-  const float inv = __frcp_rn(step), z = rintf(__fdiv_rn(lo, step));
-  marks = ((__float_as_uint(step * 16.f) >> 20) - ((127 - 15) << 3)) | (uint32_t)((int)z + 128) << 8;
+  const float inv = __frcp_rn(step);
+  // Added to 1.5 2^23, a quotient is rounded to a whole number that stands in the sum's last bits.
+  auto whole = [&](float x) { return __float_as_int(__fadd_rn(quotient(x, step, inv), 0x1.8p23f)); };
+  const int z = whole(lo);
+  marks = ((__float_as_uint(step * 16.f) >> 20) - ((127 - 15) << 3)) | (uint32_t)(z - __float_as_int(0x1.8p23f) + 128) << 8;
   uint32_t piece[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = has ? f[i] : own;
-    // x / step rounded as a division is: with the inverse rounded to nearest,
-    // one correction of the product gives the nearest quotient (Markstein)
-    const float q = __fmul_rn(x, inv);
-    const float c = fminf(fmaxf(__fsub_rn(rintf(__fmaf_rn(__fmaf_rn(-q, step, x), inv, q)), z), 0.f), 15.f);
-    piece[i >> 2] |= (uint32_t)(int)c << 4 * (i & 3);
-  }
+  for (int i = 0; i < 8; ++i)  // never below z: x is at least lo, and rounding keeps that
+    piece[i >> 2] += (uint32_t)min(whole(has ? f[i] : own) - z, 15) << 4 * (i & 3);
 #pragma unroll
   for (int i = 0; i < 2; ++i) piece[i] = (piece[i] << 6 | piece[i] >> 10) & 0xFFFFu;
   return piece[0] | piece[1] << 16;
 }
 
-constexpr int kAtOnce = 4;  // steps whose loads are in flight together
-
 template <bool F16, bool kCodes>
-__global__ void __launch_bounds__(128) k_kv_append(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(128, 8) k_kv_append(const __grid_constant__ AppendParams p) {
+  constexpr int kAtOnce = kCodes ? 2 : 4;  // steps whose loads are in flight together
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int64_t t = warp / p.parts;
@@ -198,83 +210,88 @@ __global__ void __launch_bounds__(128) k_kv_append(const __grid_constant__ Appen
     }
   }
 
-  // steps: of the queries, then of the keys, then of the values
-  const int nq = p.q ? (p.q_heads + heads - 1) / heads : 0, nk = (p.kv_heads + heads - 1) / heads;
-  const int steps = page >= 0 ? nq + 2 * nk : nq;
-  const int n = kv4_groups(p.dim);
-  for (int base = part; base < steps; base += p.parts * kAtOnce) {
-    uint4 x[kAtOnce];
+  // A step takes `heads` heads of the queries, the keys or the values; a token's
+  // steps are dealt out to its parts in that order.  take(x, head, here) for the
+  // lane's 8 elements of each; all lanes of the warp come to it together.
+  auto stream = [&](const char* base, int64_t tok, int64_t stride, int count, int before, auto take) {
+    const uint4* from = (const uint4*)base + t * tok + which * stride + sub;
+    const int n = (count + heads - 1) / heads;
+    const int skip = before % p.parts;
+    for (int j = part >= skip ? part - skip : part - skip + p.parts; j < n; j += kAtOnce * p.parts) {
+      uint4 x[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const int st = base + i * p.parts;
-      x[i] = make_uint4(0, 0, 0, 0);
-      if (st >= steps) continue;
-      const int kind = st < nq ? 0 : st < nq + nk ? 1 : 2, head = (st - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * heads + which;
-      const uint4* from = kind == 0   ? (const uint4*)p.q + t * p.q_tok + head * p.q_head
-                          : kind == 1 ? (const uint4*)p.k_new + t * p.k_new_tok + head * p.k_new_head
-                                      : (const uint4*)p.v_new + t * p.v_new_tok + head * p.v_new_head;
-      if (has && head < (kind == 0 ? p.q_heads : p.kv_heads)) x[i] = from[sub];
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int k = j + i * p.parts;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (has && k * heads + which < count) x[i] = from[(int64_t)(k * heads) * stride];
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int k = j + i * p.parts;
+        if (k >= n) break;
+        take(x[i], k * heads + which, k * heads + which < count);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const int st = base + i * p.parts;
-      if (st >= steps) break;  // the warp's lanes agree
-      const int kind = st < nq ? 0 : st < nq + nk ? 1 : 2, head = (st - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * heads + which;
-      const bool here = head < (kind == 0 ? p.q_heads : p.kv_heads);
+    return n;
+  };
+  int before = 0;
+  if (p.q) {
+    uint4* const to = (uint4*)p.q_out + t * p.q_out_tok + sub;
+    before = stream(p.q, p.q_tok, p.q_head, p.q_heads, 0, [&](const uint4& x, int head, bool here) {
       float f[8];
-      if (kind == 2) {
-        if (!kCodes) {
-          if (has && here) ((uint4*)p.v + page * p.v_page + slot * p.v_slot + head * p.v_head)[sub] = x[i];
-          continue;
-        }
-        widen<F16>(x[i], f);
-      } else {
-        turn<F16>(u, p.adjacent, first, x[i], f);
-        if (kind == 0) {
-          if (has && here) ((uint4*)p.q_out + t * p.q_out_tok + head * p.q_out_head)[sub] = u.on ? narrow<F16>(f) : x[i];
-          continue;
-        }
-        if (!kCodes) {
-          if (has && here) ((uint4*)p.k + page * p.k_page + slot * p.k_slot + head * p.k_head)[sub] = u.on ? narrow<F16>(f) : x[i];
-          continue;
-        }
-      }
-      if constexpr (kCodes) {
-        uint32_t marks;
-        const uint32_t w = encode(f, has, lane, marks);
-        if (!here || sub >= 4 * n) continue;
-        char* tile = p.pages + page * p.page_bytes + head * p.head_bytes + (slot >> 3) * kv4_tile(n);
-        const int tok = slot & 7, g = sub >> 2;
-        if (kind == 1) {
-          *(uint32_t*)(tile + kv4_key(n, tok) + sub * 4) = w;
-          if ((sub & 3) == 0) *(uint16_t*)(tile + kv4_key_marks(n, tok) + g * 2) = (uint16_t)marks;
-        } else {
-          uint16_t* to = (uint16_t*)(tile + kv4_value(n, tok >> 1)) + sub * 4 + (tok & 1);
-          to[0] = (uint16_t)w;
-          to[2] = (uint16_t)(w >> 16);
-          if ((sub & 3) == 0) {
-            uint8_t* m = (uint8_t*)tile + kv4_value_marks(n, tok >> 1) + g * 4 + (tok & 1);
-            m[0] = (uint8_t)marks;
-            m[2] = (uint8_t)(marks >> 8);
-          }
-        }
-      }
-    }
+      turn<F16>(u, p.adjacent, first, x, f);
+      if (has && here) to[head * p.q_out_head] = u.on ? narrow<F16>(f) : x;
+    });
   }
-}
-
-// (c + z) s of a piece's four elements.
-__device__ __forceinline__ void decode(uint32_t piece, uint32_t step_byte, uint32_t offset_byte, float* f) {
-  const float s = __half2float(__ushort_as_half((unsigned short)(min(step_byte, 222u) << 7))) * 0.0625f;
-  const float z = (float)((int)offset_byte - 128);
-  const uint32_t c = (piece >> 6 | piece << 10) & 0xFFFFu;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = ((float)(c >> 4 * i & 15u) + z) * s;
+  if (page < 0) return;
+  if constexpr (!kCodes) {
+    uint4* const k = (uint4*)p.k + page * p.k_page + slot * p.k_slot + sub;
+    uint4* const v = (uint4*)p.v + page * p.v_page + slot * p.v_slot + sub;
+    before += stream(p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+      float f[8];
+      turn<F16>(u, p.adjacent, first, x, f);
+      if (has && here) k[head * p.k_head] = u.on ? narrow<F16>(f) : x;
+    });
+    stream(p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+      if (has && here) v[head * p.v_head] = x;
+    });
+  } else {
+    const int n = kv4_groups(p.dim), tok = (int)slot & 7, g = sub >> 2;
+    const bool writes = sub < 4 * n;
+    char* const tile = p.pages + page * p.page_bytes + (slot >> 3) * kv4_tile(n);
+    before += stream(p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+      float f[8];
+      uint32_t marks;
+      turn<F16>(u, p.adjacent, first, x, f);
+      const uint32_t w = encode(f, has, lane, marks);
+      if (!here || !writes) return;
+      char* const to = tile + head * p.head_bytes;
+      *(uint32_t*)(to + kv4_key(n, tok) + sub * 4) = w;
+      if ((sub & 3) == 0) *(uint16_t*)(to + kv4_key_marks(n, tok) + g * 2) = (uint16_t)marks;
+    });
+    stream(p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+      float f[8];
+      uint32_t marks;
+      widen<F16>(x, f);
+      const uint32_t w = encode(f, has, lane, marks);
+      if (!here || !writes) return;
+      char* const to = tile + head * p.head_bytes;
+      uint16_t* const v = (uint16_t*)(to + kv4_value(n, tok >> 1)) + sub * 4 + (tok & 1);
+      v[0] = (uint16_t)w;
+      v[2] = (uint16_t)(w >> 16);
+      if ((sub & 3) == 0) {
+        uint8_t* const m = (uint8_t*)to + kv4_value_marks(n, tok >> 1) + g * 4 + (tok & 1);
+        m[0] = (uint8_t)marks;
+        m[2] = (uint8_t)(marks >> 8);
+      }
+    });
+  }
 }
 
 // kType: of the output.  A warp a token (or a part of its heads), 8 elements a lane.
 template <int kType>
 __global__ void __launch_bounds__(128) k_kv4_read(const __grid_constant__ AppendParams p) {
+  constexpr int kAtOnce = 4;  // steps whose loads are in flight together
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int64_t t = warp / p.parts;
@@ -287,40 +304,59 @@ __global__ void __launch_bounds__(128) k_kv4_read(const __grid_constant__ Append
   const int64_t slot = at.pos & ((1 << p.page_log2) - 1);
   if (KV_BAD(g_append_counts, page < 0 || (t < p.tokens && at.pos >= 0 && at.pos < (int64_t)p.width << p.page_log2 && page < p.n_pages)))
     return;
-  const int nk = (p.kv_heads + heads - 1) / heads, n = kv4_groups(p.dim), tok = (int)slot & 7, g = sub >> 2;
   if (sub * 8 >= p.dim) return;
-#pragma unroll 4
-  for (int st = part; st < 2 * nk; st += p.parts) {
-    const bool value = st >= nk;
-    const int head = (st - (value ? nk : 0)) * heads + which;
-    if (head >= p.kv_heads) continue;
-    float f[8];
-    if (page >= 0) {
-      const char* tile = p.pages + page * p.page_bytes + head * p.head_bytes + (slot >> 3) * kv4_tile(n);
-      uint32_t a, b, s, z;
-      if (!value) {
-        const uint32_t w = *(const uint32_t*)(tile + kv4_key(n, tok) + sub * 4);
-        const uint32_t m = *(const uint16_t*)(tile + kv4_key_marks(n, tok) + g * 2);
-        a = w & 0xFFFFu, b = w >> 16, s = m & 0xFFu, z = m >> 8;
-      } else {
-        const uint16_t* w = (const uint16_t*)(tile + kv4_value(n, tok >> 1)) + sub * 4 + (tok & 1);
-        const uint8_t* m = (const uint8_t*)tile + kv4_value_marks(n, tok >> 1) + g * 4 + (tok & 1);
-        a = w[0], b = w[2], s = m[0], z = m[2];
-      }
-      decode(a, s, z, f);
-      decode(b, s, z, f + 4);
-    } else {
+  const int nk = (p.kv_heads + heads - 1) / heads, n = kv4_groups(p.dim), tok = (int)slot & 7, g = sub >> 2;
+  const char* const tile = p.pages + (int64_t)page * p.page_bytes + (slot >> 3) * kv4_tile(n);
+  const uint32_t half = tok & 1 ? 0x7632 : 0x5410;
+  for (int st = part; st < 2 * nk; st += kAtOnce * p.parts) {
+    // A value's pieces stand beside those of the other token of its pair.
+    uint2 w[kAtOnce];
+    uint32_t m[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = 0.f;
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int k = st + i * p.parts, head = (k < nk ? k : k - nk) * heads + which;
+      w[i] = make_uint2(0, 0);
+      m[i] = 0;
+      if (page < 0 || k >= 2 * nk || head >= p.kv_heads) continue;
+      const char* from = tile + head * p.head_bytes;
+      if (k < nk) {
+        w[i].x = *(const uint32_t*)(from + kv4_key(n, tok) + sub * 4);
+        m[i] = *(const uint16_t*)(from + kv4_key_marks(n, tok) + g * 2);
+      } else {
+        w[i] = *(const uint2*)(from + kv4_value(n, tok >> 1) + sub * 8);
+        m[i] = *(const uint32_t*)(from + kv4_value_marks(n, tok >> 1) + g * 4);
+      }
     }
-    const int64_t out = value ? t * p.v_new_tok + head * p.v_new_head : t * p.k_new_tok + head * p.k_new_head;  // 8 elements each
-    char* to = (char*)(value ? p.v_new : p.k_new);
-    if (kType == MPT_KV_F32) {
-      float4* o = (float4*)to + 2 * (out + sub);
-      o[0] = make_float4(f[0], f[1], f[2], f[3]);
-      o[1] = make_float4(f[4], f[5], f[6], f[7]);
-    } else {
-      ((uint4*)to)[out + sub] = narrow<kType == MPT_KV_F16>(f);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int k = st + i * p.parts, head = (k < nk ? k : k - nk) * heads + which;
+      if (k >= 2 * nk || head >= p.kv_heads) continue;
+      const bool value = k >= nk;
+      const uint32_t word = value ? __byte_perm(w[i].x, w[i].y, half) : w[i].x;
+      const uint32_t marks = value ? m[i] >> 8 * (tok & 1) & 0xFFu | (m[i] >> 8 * (tok & 1) & 0xFF0000u) >> 8 : m[i];
+      uint32_t step, off, o[4];
+      kv4_key_step(marks, step, off);
+      kv4_word(word, step, off, o);  // (e, e + 4)
+      const int64_t out = value ? t * p.v_new_tok + head * p.v_new_head : t * p.k_new_tok + head * p.k_new_head;  // 8 elements each
+      char* const to = (char*)(value ? p.v_new : p.k_new);
+      if (kType == MPT_KV_F16) {
+        ((uint4*)to)[out + sub] = make_uint4(__byte_perm(o[0], o[1], 0x5410), __byte_perm(o[2], o[3], 0x5410), __byte_perm(o[0], o[1], 0x7632),
+                                             __byte_perm(o[2], o[3], 0x7632));
+        continue;
+      }
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[e] = __half2float(__ushort_as_half((unsigned short)o[e]));
+        f[4 + e] = __half2float(__ushort_as_half((unsigned short)(o[e] >> 16)));
+      }
+      if (kType == MPT_KV_F32) {
+        float4* const o4 = (float4*)to + 2 * (out + sub);
+        o4[0] = make_float4(f[0], f[1], f[2], f[3]);
+        o4[1] = make_float4(f[4], f[5], f[6], f[7]);
+      } else {
+        ((uint4*)to)[out + sub] = narrow<false>(f);
+      }
     }
   }
 }
