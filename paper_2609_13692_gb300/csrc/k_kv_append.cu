@@ -15,6 +15,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "kv4.cuh"
 #include "kv_pages.cuh"
 
@@ -170,8 +172,7 @@ __device__ __forceinline__ uint32_t encode(float* f, bool has, int lane, uint32_
 }
 
 template <bool F16, bool kCodes>
-__global__ void __launch_bounds__(128, 8) k_kv_append(const __grid_constant__ AppendParams p) {
-  constexpr int kAtOnce = kCodes ? 2 : 4;  // steps whose loads are in flight together
+__global__ void __launch_bounds__(128, kCodes ? 7 : 8) k_kv_append(const __grid_constant__ AppendParams p) {
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int64_t t = warp / p.parts;
@@ -212,11 +213,13 @@ __global__ void __launch_bounds__(128, 8) k_kv_append(const __grid_constant__ Ap
 
   // A step takes `heads` heads of the queries, the keys or the values; a token's
   // steps are dealt out to its parts in that order.  take(x, head, here) for the
-  // lane's 8 elements of each; all lanes of the warp come to it together.
-  auto stream = [&](const char* base, int64_t tok, int64_t stride, int count, int before, auto take) {
+  // lane's 8 elements of each; all lanes of the warp come to it together.  The
+  // loads of at_once steps are in flight together.
+  auto stream = [&](auto at_once, const char* base, int64_t tok, int64_t stride, int count, int before, auto take) {
     const uint4* from = (const uint4*)base + t * tok + which * stride + sub;
     const int n = (count + heads - 1) / heads;
     const int skip = before % p.parts;
+    constexpr int kAtOnce = decltype(at_once)::value;
     for (int j = part >= skip ? part - skip : part - skip + p.parts; j < n; j += kAtOnce * p.parts) {
       uint4 x[kAtOnce];
 #pragma unroll
@@ -237,7 +240,7 @@ __global__ void __launch_bounds__(128, 8) k_kv_append(const __grid_constant__ Ap
   int before = 0;
   if (p.q) {
     uint4* const to = (uint4*)p.q_out + t * p.q_out_tok + sub;
-    before = stream(p.q, p.q_tok, p.q_head, p.q_heads, 0, [&](const uint4& x, int head, bool here) {
+    before = stream(std::integral_constant<int, 4>(), p.q, p.q_tok, p.q_head, p.q_heads, 0, [&](const uint4& x, int head, bool here) {
       float f[8];
       turn<F16>(u, p.adjacent, first, x, f);
       if (has && here) to[head * p.q_out_head] = u.on ? narrow<F16>(f) : x;
@@ -247,19 +250,19 @@ __global__ void __launch_bounds__(128, 8) k_kv_append(const __grid_constant__ Ap
   if constexpr (!kCodes) {
     uint4* const k = (uint4*)p.k + page * p.k_page + slot * p.k_slot + sub;
     uint4* const v = (uint4*)p.v + page * p.v_page + slot * p.v_slot + sub;
-    before += stream(p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    before += stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       float f[8];
       turn<F16>(u, p.adjacent, first, x, f);
       if (has && here) k[head * p.k_head] = u.on ? narrow<F16>(f) : x;
     });
-    stream(p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       if (has && here) v[head * p.v_head] = x;
     });
   } else {
     const int n = kv4_groups(p.dim), tok = (int)slot & 7, g = sub >> 2;
     const bool writes = sub < 4 * n;
     char* const tile = p.pages + page * p.page_bytes + (slot >> 3) * kv4_tile(n);
-    before += stream(p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    before += stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       float f[8];
       uint32_t marks;
       turn<F16>(u, p.adjacent, first, x, f);
@@ -269,7 +272,7 @@ __global__ void __launch_bounds__(128, 8) k_kv_append(const __grid_constant__ Ap
       *(uint32_t*)(to + kv4_key(n, tok) + sub * 4) = w;
       if ((sub & 3) == 0) *(uint16_t*)(to + kv4_key_marks(n, tok) + g * 2) = (uint16_t)marks;
     });
-    stream(p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       float f[8];
       uint32_t marks;
       widen<F16>(x, f);

@@ -46,7 +46,7 @@ _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_get
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-_current_device = torch.cuda.current_device
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _empty, _U8, _F32 = torch.empty, torch.uint8, torch.float32
 
 
@@ -107,7 +107,7 @@ def _cache(k_pages, v_pages, page_table, q_offsets, kv_lens):
     batch, width, stride = _table(page_table, "page_table")
     _ints(q_offsets, "q_offsets")
     _ints(kv_lens, "kv_lens")
-    if len(q_offsets) != batch + 1 or len(kv_lens) != batch:
+    if q_offsets.shape[0] != batch + 1 or kv_lens.shape[0] != batch:
         raise ValueError("q_offsets needs batch + 1 entries, kv_lens batch")
     n_pages, page_size, kv_heads, dim = shape
     return _CACHE.pack(k_pages.data_ptr(), v_pages.data_ptr(), kp, ks, kh, vp, vs, vh, _TYPES[dtype], n_pages, page_size,
@@ -275,9 +275,9 @@ def _write(s, *args):
 
 def _turn(rotation, positions, adjacent: bool, q, q_out, tokens: int, dim: int, dtype, index: int):
     """The packed mpt_kv_turn."""
-    _device(rotation, *(t for t in (positions, q, q_out) if t is not None))
-    if rotation.get_device() != index:
-        raise ValueError("every tensor must be on the same CUDA device")
+    for t in (rotation, positions, q, q_out):
+        if t is not None and t.get_device() != index:
+            raise ValueError("every tensor must be on the same CUDA device")
     _no_grad(rotation, q, q_out)
     shape, strides = rotation.shape, rotation.stride()
     if len(shape) != 2 or rotation.dtype is not _F32 or (strides[1] != 1 and shape[1] > 1):
@@ -285,7 +285,7 @@ def _turn(rotation, positions, adjacent: bool, q, q_out, tokens: int, dim: int, 
     rows, rot = shape
     if positions is not None:
         _ints(positions, "positions")
-        if len(positions) != tokens:
+        if positions.shape[0] != tokens:
             raise ValueError("positions needs one entry per token")
     if q is None:
         if q_out is not None:
@@ -297,9 +297,10 @@ def _turn(rotation, positions, adjacent: bool, q, q_out, tokens: int, dim: int, 
         raise ValueError("q must be [tokens, heads, head_dim] of k_new's type")
     if q_out.shape != qs or q_out.dtype is not dtype:
         raise ValueError("q_out must have q's shape and type")
-    _heads_strides(q, "q"), _heads_strides(q_out, "q_out")
-    a, b, _ = q.stride()
-    c, d, _ = q_out.stride()
+    a, b, e = q.stride()
+    c, d, f = q_out.stride()
+    if (e != 1 or f != 1) and q.numel() > 0:
+        raise ValueError("q and q_out must have contiguous heads")
     return _TURN.pack(rotation.data_ptr(), strides[0], rows, rot, 1 if adjacent else 0, qs[1],
                       0 if positions is None else positions.data_ptr(), q.data_ptr(), q_out.data_ptr(), a, b, c, d)
 
@@ -362,7 +363,7 @@ def _cache4(pages, page_table, q_offsets, kv_lens, dim: int) -> bytes:
     batch, width, stride = _table(page_table, "page_table")
     _ints(q_offsets, "q_offsets")
     _ints(kv_lens, "kv_lens")
-    if len(q_offsets) != batch + 1 or len(kv_lens) != batch:
+    if q_offsets.shape[0] != batch + 1 or kv_lens.shape[0] != batch:
         raise ValueError("q_offsets needs batch + 1 entries, kv_lens batch")
     return _CACHE4.pack(pages.data_ptr(), a, b, n_pages, size // tile * 8, kv_heads, dim, batch, page_table.data_ptr(), stride, width,
                         q_offsets.data_ptr(), kv_lens.data_ptr())
