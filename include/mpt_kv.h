@@ -170,7 +170,8 @@ mpt_status mpt_kv_write_rotated(const mpt_kv_cache* cache, const mpt_kv_turn* tu
  * the step's byte the upper bits of 16 s as a positive f16 (5 of exponent, 3 of
  * mantissa), the offset's z + 128.  Missing elements of the last group are
  * written as its first one is.  What reads a step's byte takes those above 222
- * (16 s = 7168) for 222, so no bytes stand for an infinity or a NaN.
+ * (16 s = 7168) for 222, so no bytes stand for an infinity or a NaN; where an
+ * offset is below -120, which no write makes, attention rounds (c + z) s to f16.
  * ------------------------------------------------------------------------- */
 typedef struct mpt_kv4_cache {
   void* pages;       /* device, 16-byte aligned */

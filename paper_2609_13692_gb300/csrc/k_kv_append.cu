@@ -336,29 +336,26 @@ __global__ void __launch_bounds__(128) k_kv4_read(const __grid_constant__ Append
       if (k >= 2 * nk || head >= p.kv_heads) continue;
       const bool value = k >= nk;
       const uint32_t word = value ? __byte_perm(w[i].x, w[i].y, half) : w[i].x;
-      const uint32_t marks = value ? m[i] >> 8 * (tok & 1) & 0xFFu | (m[i] >> 8 * (tok & 1) & 0xFF0000u) >> 8 : m[i];
-      uint32_t step, off, o[4];
-      kv4_key_step(marks, step, off);
-      kv4_word(word, step, off, o);  // (e, e + 4)
-      const int64_t out = value ? t * p.v_new_tok + head * p.v_new_head : t * p.k_new_tok + head * p.k_new_head;  // 8 elements each
-      char* const to = (char*)(value ? p.v_new : p.k_new);
-      if (kType == MPT_KV_F16) {
-        ((uint4*)to)[out + sub] = make_uint4(__byte_perm(o[0], o[1], 0x5410), __byte_perm(o[2], o[3], 0x5410), __byte_perm(o[0], o[1], 0x7632),
-                                             __byte_perm(o[2], o[3], 0x7632));
-        continue;
-      }
+      const uint32_t marks = value ? m[i] >> 8 * (tok & 1) : m[i];  // the step's byte the lowest
+      // c + z in f16, then times the step in 32 bits: exact whatever bytes are there
+      const uint32_t offset = value ? marks >> 16 & 0xFFu : marks >> 8, z = hadd2((offset | offset << 16) | 0x64006400u, 0xE490E490u);
+      const float step = __half2float(__ushort_as_half((unsigned short)(min(marks & 0xFFu, 222u) << 7))) * 0.0625f;
+      const uint32_t at[4] = {word, word >> 4, __byte_perm(word, 0, 0x2301), word << 4};
       float f[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f[e] = __half2float(__ushort_as_half((unsigned short)o[e]));
-        f[4 + e] = __half2float(__ushort_as_half((unsigned short)(o[e] >> 16)));
+      for (int e = 0; e < 4; ++e) {  // elements e and e + 4
+        const uint32_t o = hadd2(kv4_code_bits(at[e]), z);
+        f[e] = __half2float(__ushort_as_half((unsigned short)o)) * step;
+        f[4 + e] = __half2float(__ushort_as_half((unsigned short)(o >> 16))) * step;
       }
+      const int64_t out = value ? t * p.v_new_tok + head * p.v_new_head : t * p.k_new_tok + head * p.k_new_head;  // 8 elements each
+      char* const to = (char*)(value ? p.v_new : p.k_new);
       if (kType == MPT_KV_F32) {
         float4* const o4 = (float4*)to + 2 * (out + sub);
         o4[0] = make_float4(f[0], f[1], f[2], f[3]);
         o4[1] = make_float4(f[4], f[5], f[6], f[7]);
       } else {
-        ((uint4*)to)[out + sub] = narrow<false>(f);
+        ((uint4*)to)[out + sub] = narrow<kType == MPT_KV_F16>(f);
       }
     }
   }
