@@ -20,8 +20,8 @@ constexpr float kv4_most = 3360.f;  // of a value: its step's byte is then 222 a
 // A word of two pieces as four pairs of f16: (c + z) s of the i-th element of
 // the low piece and of the high one.  Rotated left by six bits, a piece has its
 // first code at bits 6 to 9 of 16, where under the exponent of 16 it reads as
-// 16 + c; the others come there by a shift of four, by exchanging the bytes, and
-// by a shift of four the other way.  (16 + c) s + (z - 16) s is then one fused
+// 16 + c; the last comes there by a shift of four, the third by exchanging the
+// bytes, the second by both.  (16 + c) s + (z - 16) s is then one fused
 // operation on both halves, and every term is a whole number below 2^11 of
 // step's last place: exact.
 __device__ __forceinline__ uint32_t kv4_code_bits(uint32_t x) {
@@ -50,9 +50,10 @@ __device__ __forceinline__ uint32_t hmin2(uint32_t a, uint32_t b) {
   return r;
 }
 __device__ __forceinline__ void kv4_word(uint32_t w, uint32_t step, uint32_t off, uint32_t* v) {
+  const uint32_t x = __byte_perm(w, 0, 0x2301);
   v[0] = hfma2(kv4_code_bits(w), step, off);
-  v[1] = hfma2(kv4_code_bits(w >> 4), step, off);
-  v[2] = hfma2(kv4_code_bits(__byte_perm(w, 0, 0x2301)), step, off);
+  v[1] = hfma2(kv4_code_bits(x << 4), step, off);
+  v[2] = hfma2(kv4_code_bits(x), step, off);
   v[3] = hfma2(kv4_code_bits(w << 4), step, off);
 }
 // s and (z - 16) s, two at a time, from the bytes of 16 s (at bits 0 and 16 of
