@@ -63,7 +63,6 @@ namespace {
 __device__ uint32_t g_tile_counts[kKvCounts];
 
 constexpr int kKeys = 128;     // keys of a tile
-constexpr int kCodeWarps = 7;  // cache in 4 bits: warps that widen codes
 template <bool kCodes>
 constexpr int kThreads = kCodes ? 512 : 384;
 constexpr int kOddSets = 4;    // items whose notes are kept apart
@@ -96,6 +95,8 @@ struct TileCfg {
   static constexpr int kRoleRegs = kCodes || HDP == 64 ? 72 : 88;
   template <bool kCodes>
   static constexpr int kRowRegs = kCodes ? 184 : HDP == 64 ? 216 : 208;
+  // Warps that widen codes: 9 to 15, and those of the absent row tile.
+  static constexpr int kCodeWarps = kTiles == 1 ? 11 : 7;
   static_assert(kRoleRegs<false> + 2 * kRowRegs<false> <= 3 * 168 && 2 * kRoleRegs<true> + 2 * kRowRegs<true> <= 4 * 128);
   static constexpr int kSmem = 1024 + kQ + kSlots * kSlot + 2048;
 };
@@ -515,18 +516,21 @@ struct CodeChunk {
   uint32_t marks;
 };
 
-// By warps 9 to 15: f16 keys and values of the block's key tiles, each in its
+// By kCodeWarps warps: f16 keys and values of the block's key tiles, each in its
 // slot of the ring.  A tile of 8 tokens has 8 n chunks of 16 bytes of either;
-// a warp takes tiles of 8 in turn, a lane the same chunk of each (kPer of them
-// with more than 4 groups; two tiles at once with 2).  A chunk is read as soon as the one
+// a warp takes tiles of 8 in turn (half of one with more than 4 groups, two at
+// once with 2), a lane the same chunk of each.  A chunk is read as soon as the one
 // before it in its registers has been used, which is half a key tile ahead.
+// (2,048 tokens over 10,000 keys of 32 heads of 256 on 8: the four warps of the
+// absent row tile among them, 1.50 -> FIG ms.)
 template <int HDP, typename Next, typename Leave>
-__device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh, char* ring, Next next_item, Leave leave) {
+__device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh, char* ring, int me, Next next_item, Leave leave) {
   using C = TileCfg<HDP>;
+  constexpr int kCodeWarps = C::kCodeWarps;
   constexpr int kTogether = HDP == 64 ? 2 : 1, kPer = HDP == 256 ? 2 : 1;
-  constexpr int kTiles8 = kKeys / kCodeTokens / kTogether;                  // steps of all warps in half a key tile
-  constexpr int kSteps = (kTiles8 + kCodeWarps - 1) / kCodeWarps * kPer;    // of a warp
-  const int lane = threadIdx.x & 31, me = (threadIdx.x >> 5) - 9;
+  constexpr int kUnits = kKeys / kCodeTokens / kTogether * kPer;       // steps of all warps in half a key tile
+  constexpr int kSteps = (kUnits + kCodeWarps - 1) / kCodeWarps;       // of a warp
+  const int lane = threadIdx.x & 31;
   const int n = kv4_groups(p.dim);
   int* const gave_up = &sh.gave_up;
   const int second = kTogether == 2 ? lane >> 4 : 0, in = kTogether == 2 ? lane & 15 : lane;
@@ -536,7 +540,7 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
   // row r at c ^ (r & 7).  Lanes of odd blocks of 64 elements take a chunk's halves
   // in the other order, so that 8 lanes write to 8 places.
   bool has[kPer], odd[kPer][2];
-  uint32_t mark_from[kPer][2], to[kPer][2];
+  uint32_t mark_from[kPer][2], to[kPer][2];  // (the second index is known where they are used, the first chosen)
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int x = in + 32 * i;
@@ -552,9 +556,10 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
   }
   const uint32_t from = 16 * in, values_from = kv4_value(n, 0);
 
-  // Step i, half v (0 keys, 1 values): the tile of 8 that it is about.
+  // Step i, half v (0 keys, 1 values): the tile of 8 that it is about, and which of the lane's chunks.
   // (The warps that have one step more than the others are others for values.)
-  auto tile8 = [&](int v, int i) { return ((i / kPer) * kCodeWarps + (v ? (me + 2) % kCodeWarps : me)) * kTogether + second; };
+  auto unit = [&](int v, int i) { return i * kCodeWarps + (v ? (me + 2) % kCodeWarps : me); };
+  auto tile8 = [&](int u) { return u / kPer * kTogether + second; };
 
   TileItem w;
   int k = 0;
@@ -571,20 +576,20 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
     return p.k + (int64_t)id * p.k_page + (int64_t)w.e.head * p.k_head + (int64_t)(slot / kCodeTokens) * kv4_tile(n);
   };
   auto load = [&](CodeChunk& c, int v, int i, const char* tiles) {
-    const int t8 = tile8(v, i);
+    const int x = unit(v, i), t8 = tile8(x), which = x % kPer;
     const char* at = (const char*)__shfl_sync(~0u, (unsigned long long)tiles, t8 & 15);
     c.w = make_uint4(0, 0, 0, 0);
     c.marks = 0;
-    if (t8 >= kKeys / kCodeTokens || !has[i % kPer] || !at) return;  // without a page: zeros
-    c.w = __ldg((const uint4*)(at + (v ? values_from : 0) + from + 512 * (i % kPer)));
-    const char* m = at + mark_from[i % kPer][v];
+    if (t8 >= kKeys / kCodeTokens || !has[which] || !at) return;  // without a page: zeros
+    c.w = __ldg((const uint4*)(at + (v ? values_from : 0) + from + 512 * which));
+    const char* m = at + mark_from[which][v];
     c.marks = v ? __ldg((const uint32_t*)m) : (uint32_t)__ldg((const uint16_t*)m);
   };
   auto store = [&](const CodeChunk& c, int v, int i, uint32_t slot_at) {
-    const int t8 = tile8(v, i);
-    if (t8 >= kKeys / kCodeTokens || !has[i % kPer]) return;
-    const uint32_t at = slot_at + to[i % kPer][v] + t8 * kCodeTokens * 128;
-    const bool swap = odd[i % kPer][v];
+    const int x = unit(v, i), t8 = tile8(x), which = x % kPer;
+    if (t8 >= kKeys / kCodeTokens || !has[which]) return;
+    const uint32_t at = slot_at + to[which][v] + t8 * kCodeTokens * 128;
+    const bool swap = odd[which][v];
     const uint32_t u[4] = {swap ? c.w.z : c.w.x, swap ? c.w.w : c.w.y, swap ? c.w.x : c.w.z, swap ? c.w.y : c.w.w};
     uint32_t step, off;
     if (v == 0) {
@@ -662,7 +667,7 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
 
   if (tid == 0) {
     for (int s = 0; s < C::kSlots; ++s) {
-      mbar_init(&sh.full[s], kCodes ? kCodeWarps : 1);
+      mbar_init(&sh.full[s], kCodes ? C::kCodeWarps : 1);
       mbar_init(&sh.empty[s], 1);
     }
     mbar_init(&sh.q_full, 1);
@@ -809,11 +814,14 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
     }
   };
 
-  if (warp >= 8) {
+  if (kCodes && C::kTiles == 1 && warp >= 4 && warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::template kRowRegs<kCodes>));
+    widen_codes<HDP>(p, sh, ring, warp + 3, next_item, leave);
+  } else if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::template kRoleRegs<kCodes>));
     if (kCodes && warp > 8) {
       // ---- codes: warps 9 to 15 make f16 keys and values of them ----
-      widen_codes<HDP>(p, sh, ring, next_item, leave);
+      widen_codes<HDP>(p, sh, ring, warp - 9, next_item, leave);
     } else if (warp == 9 || warp == 10) {
       // ---- copies: warp 9 queries and keys, warp 10 values ----
       // Tile g of the block (over all its items) has its keys in use 2 g of the
