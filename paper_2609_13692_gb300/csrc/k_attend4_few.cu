@@ -13,8 +13,24 @@
 // words of values pairs of tokens.  P^T comes from S^T by a transposition of
 // 8 x 8 matrices across lanes.
 //
-// Bound: 36 bytes a key and group of 32 elements, read once; and issue slots:
-// about 13 operations per 8 codes, 270 a warp for 16 keys of 128 elements.
+// Bound: 36 bytes a key and group of 32 elements, read once; and, before that,
+// issue slots: 11 operations for 8 codes, three of them to align a piece's codes,
+// about 310 a warp for 16 keys of 128 elements with all that is not codes.  So a
+// warp takes 32 keys at once where the accumulators leave room (waits, maxima and
+// votes are shared by them: three requests of 100,001 to 131,072 keys 100 -> 90 us),
+// the maximum of a row is looked for only when a score is above its reference by
+// more than 2^kLag, and one warp of five copies (a page's part of a stage is
+// contiguous, so a copy is up to 18 KB).
+//
+// Measured (one GB300, 8 KV heads of 128): the three requests 88 us, 4.5 TB/s; one
+// of 1,000,000 keys 244 us, 4.7 TB/s, 0.71 of the copy rate; 28 of 2,000 to 6,000
+// 40 us, 13 of them start, end and join; one of 777 9.4 us, launches and a chain of
+// dependent reads.  28 requests of heads of 64, 96 and 256: 29, 38 and 73 us.
+//
+// Tried and slower: a ring for each warp, filled by itself, four blocks of four
+// warps an SM (the three requests 97 us: a fifth more operations), two blocks of
+// five an SM (95), fewer or more stages (no different), left shifts as products on
+// the other pipe (no different).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

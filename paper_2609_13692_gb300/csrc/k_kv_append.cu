@@ -10,8 +10,16 @@
 // shuffle brings it; so a head may be written where it was read.
 //
 // Bound: the memory.  What is turned is read and written once, and codes are
-// 4.5 bits an element; the arithmetic of the codes (a quotient, its rounding and
-// the packing: about 15 operations an element) hides behind it.
+// 4.5 bits an element.  A token's chain of reads (request, page, cosines, values)
+// is long, so what counts is how many warps are there to hide it: eight blocks of
+// four an SM, which 64 registers allow, are worth more than more loads in flight in
+// each (33,600 tokens of 32 query and 8 KV heads of 128, turned: 151 us with 88
+// registers, 180 with 92 and loads that run ahead, 119 with 64; of codes, seven
+// blocks and two steps at once).  The arithmetic of the codes, about 12 operations
+// an element, does not hide whole: without it the write takes 10 us less.
+//
+// Measured (one GB300): the turned write 119 us, 6.5 TB/s, 0.97 of the copy rate;
+// as codes 137 us, 4.9 TB/s; codes read back 36 us, 4.5 TB/s; 28 tokens 3.0 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
