@@ -118,6 +118,35 @@ __device__ __forceinline__ uint32_t load_u32(uint32_t at) {
   return r;
 }
 
+// Bounded wait of a whole warp: false once the block has given up, or after four
+// seconds (which it then counts).  The hardware holds the warp for up to a
+// microsecond at each look: looks take issue slots that the products need.
+__device__ __forceinline__ bool look(unsigned long long* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(1000)
+      : "memory");
+  return __all_sync(~0u, ok != 0);
+}
+__device__ __noinline__ bool wait_longer(unsigned long long* bar, uint32_t parity, int* gave_up) {
+  const unsigned long long start = now_ns();
+  for (;;) {
+    if (look(bar, parity)) return true;
+    bool over = *(volatile int*)gave_up != 0;
+    if (!over && now_ns() - start > 4000000000ull) {
+      over = true;
+      *(volatile int*)gave_up = 1;
+      if ((threadIdx.x & 31) == 0) atomicAdd(&g_few4_counts[kKvGaveUp], 1u);
+    }
+    if (__any_sync(~0u, over)) return false;
+  }
+}
+__device__ __forceinline__ bool wait_warp(unsigned long long* bar, uint32_t parity, int* gave_up) {
+  return look(bar, parity) || wait_longer(bar, parity, gave_up);
+}
+
 // One item: rows of one KV head of one request.
 struct Few4Item {
   int req, head, row0, rows;  // rows: valid ones
@@ -199,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
   float* ml = (float*)((char*)bufs + C::kBuf);  // [kWarps][2][kRows]
   unsigned long long* full = (unsigned long long*)((char*)ml + C::kMl);
   unsigned long long* empty = full + C::kStages;
-  uint32_t* there = (uint32_t*)(empty + C::kStages);  // per stage: which groups of 8 keys the cache holds
+  uint32_t* there = (uint32_t*)(empty + C::kStages);  // per stage: which copies the cache holds
   int64_t* scratch = (int64_t*)((char*)full + C::kStages * 24);
   __shared__ int gave_up;
 
@@ -247,8 +276,9 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
     // ---- copies: a page's part of a stage is contiguous ----
     const int box = p.box < kKeys ? p.box : kKeys, per = kKeys / box;  // keys of a copy; copies of a stage
     const uint32_t bytes = (uint32_t)(box / kCodeTokens * kv4_tile(N));
+    const unsigned all = per == 32 ? ~0u : (1u << per) - 1;
     bool ok = true;
-    uint32_t done = 0;
+    uint32_t done = 0, s = 0, phase = 0;  // stages filled; the next one, and how often the ring has been
     do {
       const Few4Item x = few_item<kRows, kKeys>(p, r, req, item, rt);
       const int seg = (int)(left < cost - t0 ? left : cost - t0);
@@ -262,20 +292,18 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
       };
       int next = page_of(t0);
       for (int t = t0; t < last; ++t, ++done) {
-        const int s = done % C::kStages;
         const int id = next;
         next = page_of(t + 1);
         if (done >= C::kStages) {
-          ok = __all_sync(~0u, wait_bar(&empty[s], (done / C::kStages - 1) & 1, &gave_up, g_few4_counts) && *(volatile int*)&gave_up == 0);
+          ok = wait_warp(&empty[s], phase ^ 1, &gave_up) && *(volatile int*)&gave_up == 0;
+          ok = __all_sync(~0u, ok);
           if (!ok) break;
         }
         const int slot = (t * kKeys) & ((1 << p.page_log2) - 1);  // of pages larger than a stage
         const bool bad = KV_BAD(g_few4_counts, id < 0 || (id < p.n_pages && x.head < p.kv_heads && slot + box <= 1 << p.page_log2 && lane < per));
         const unsigned held = __ballot_sync(~0u, id >= 0 && !bad);
         if (lane == 0) {
-          uint32_t m = 0;
-          for (int g = 0; g < kKeys / kCodeTokens; ++g) m |= (held >> (g * kCodeTokens / box) & 1u) << g;
-          there[s] = m;
+          there[s] = held == all ? ~0u : held;  // a bit per copy, all of them where none is missing
           mbar_arrive_expect_tx(&full[s], bytes * __popc(held));
         }
         __syncwarp();
@@ -286,6 +314,10 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
                        "r"(smem_u32(&full[s]))
                        : "memory");
         __syncwarp();
+        if (++s == C::kStages) {
+          s = 0;
+          phase ^= 1;
+        }
       }
       if (!ok || !next_item(seg)) break;
     } while (true);
@@ -348,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
 
     for (int t = t0; t < last; ++t) {
       // having given up, the block still ends in order
-      (void)__all_sync(~0u, wait_bar(&full[s], phase, &gave_up, g_few4_counts));
+      (void)wait_warp(&full[s], phase, &gave_up);
       const uint32_t at = ring_at + s * C::kStage;
       const int key0 = t * kKeys + 16 * kGroups * warp;
       if (key0 < lim_hi) {
@@ -387,15 +419,18 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
 #pragma unroll
             for (int e = 0; e < 4; ++e) sc[u][i][e] += half[i][e];
         }
-        const uint32_t held = there[s] >> 2 * kGroups * warp & ((1u << 2 * kGroups) - 1);
-        if (lim_lo - key0 < 16 * kGroups || held != (1u << 2 * kGroups) - 1) {
+        const uint32_t held = there[s];
+        if (lim_lo - key0 < 16 * kGroups || held != ~0u) {
+          const int shift = __ffs(p.box < kKeys ? p.box : kKeys) - 1;  // keys of a copy, a power of two
 #pragma unroll
           for (int u = 0; u < kGroups; ++u)
 #pragma unroll
             for (int i = 0; i < kR; ++i)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (key0 + 16 * u + g + 8 * (e >> 1) >= lim[i][e & 1] || !(held >> (2 * u + (e >> 1)) & 1u)) sc[u][i][e] = -INFINITY;
+                if (key0 + 16 * u + g + 8 * (e >> 1) >= lim[i][e & 1] ||
+                    !(held >> ((16 * kGroups * warp + 16 * u + 8 * (e >> 1)) >> shift) & 1u))
+                  sc[u][i][e] = -INFINITY;
         }
         bool grows = false;
 #pragma unroll
