@@ -60,6 +60,12 @@ struct Few4Cfg {
   static constexpr int kMl = kWarps * 2 * kRows * 4;
   static constexpr int kSmem = 128 + kStages * kStage + kBuf + kMl + kStages * 24 + 320;
   static constexpr int kSlot = kRows * kCols + 2 * kRows;  // floats of a partial result
+  // What an item costs beside its key tiles (queries, first copies, the join of
+  // the warps: 3 us), in their time.  It is counted before them, as units of the
+  // line without work, or the blocks with the short requests would be the last
+  // (150 requests of 300 to 5,000 keys, 16 heads of 64: 154 us without, 146, 139,
+  // 137 and 138 with 1 to 4; 8 heads of 128, 32 query heads: 181, 165 and 162 with 1, 3 and 4).
+  static constexpr int kItem = 3;
 };
 
 __device__ __forceinline__ void mma(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -245,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
   const AttnRange range = attn_range<kThreads>(p.batch, blockIdx.x, gridDim.x, scratch, [&](int i) -> int64_t {
     if (attn_falls(p, i)) return -1;
     const AttnReq r = attn_req(p, i);
-    return (int64_t)p.kv_heads * row_tiles<kRows>(p, r) * key_tiles<kKeys>(r);
+    return (int64_t)p.kv_heads * row_tiles<kRows>(p, r) * (key_tiles<kKeys>(r) + C::kItem);
   });
   if (tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (range.begin >= range.end) return;
@@ -253,20 +259,22 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
 
   int req = range.req;
   AttnReq r = attn_req(p, req);
-  int rt = row_tiles<kRows>(p, r), cost = key_tiles<kKeys>(r);
+  int rt = row_tiles<kRows>(p, r);
+  int cost = key_tiles<kKeys>(r) + C::kItem;
   int64_t item = range.off / cost;
-  int t0 = (int)(range.off % cost);
+  int u0 = (int)(range.off % cost);  // the item's first unit here
   int64_t left = range.end - range.begin;
+  auto first_tile = [](int u) { return u > C::kItem ? u - C::kItem : 0; };
   auto next_item = [&](int seg) -> bool {
     left -= seg;
-    t0 = 0;
+    u0 = 0;
     if (++item == (int64_t)p.kv_heads * rt) {
       item = 0;
       do {
         if (++req >= p.batch) return false;
         r = attn_req(p, req);
         rt = row_tiles<kRows>(p, r);
-        cost = key_tiles<kKeys>(r);
+        cost = key_tiles<kKeys>(r) + C::kItem;
       } while (rt == 0);
     }
     return left > 0;
@@ -281,8 +289,8 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
     uint32_t done = 0, s = 0, phase = 0;  // stages filled; the next one, and how often the ring has been
     do {
       const Few4Item x = few_item<kRows, kKeys>(p, r, req, item, rt);
-      const int seg = (int)(left < cost - t0 ? left : cost - t0);
-      const int last = t0 + seg < x.tiles ? t0 + seg : x.tiles;
+      const int seg = (int)(left < cost - u0 ? left : cost - u0);
+      const int t0 = first_tile(u0), end = first_tile(u0 + seg), last = end < x.tiles ? end : x.tiles;
       const int32_t* row = p.table + (int64_t)req * p.table_stride;
       auto page_of = [&](int t) -> int {  // lane b: the page of the b-th copy
         const int64_t key = (int64_t)t * kKeys + lane * box;
@@ -333,9 +341,13 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
   uint32_t s = 0, phase = 0;  // the stage at hand
   for (;;) {
     const Few4Item x = few_item<kRows, kKeys>(p, r, req, item, rt);
-    const int seg = (int)(left < cost - t0 ? left : cost - t0);
-    const int last = t0 + seg < x.tiles ? t0 + seg : x.tiles;
-    const bool starts = t0 == 0, ends = t0 + seg == cost;
+    const int seg = (int)(left < cost - u0 ? left : cost - u0);
+    if (u0 + seg <= C::kItem) {  // the block ends before the item's key tiles begin
+      if (!next_item(seg)) break;
+      continue;
+    }
+    const int t0 = first_tile(u0), end = first_tile(u0 + seg), last = end < x.tiles ? end : x.tiles;
+    const bool starts = t0 == 0, ends = u0 + seg == cost;
 
     // query row 8 i + g of this lane's fragments; rows 8 i + 2 q + e of its scores
     uint32_t qf[kR][2 * N][2];
@@ -600,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
       }
     }
     if (starts && !ends && tid == 0) {
-      const int64_t first = range.end - seg;  // the item's first unit
+      const int64_t first = range.end - seg - u0;  // the item's first unit
       p.desc[blockIdx.x] = make_int4(r.q0, x.row0, x.head | x.rows << 16, attn_block_of(range, first + cost - 1) - (int)blockIdx.x + 1);
     }
     bar_consumers();
