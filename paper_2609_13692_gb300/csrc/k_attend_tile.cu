@@ -340,6 +340,11 @@ __device__ __forceinline__ int pair_cost(const AttnParams& p, int ql, int kvl, i
   return lim <= kKeys ? 1 : (lim - 1) / kKeys + 1;
 }
 
+// The cache in 4 bits: what an item costs beside its key tiles, in their time,
+// counted before them as units of the line without work.
+template <bool kCodes>
+constexpr int kItem = kCodes ? 4 : 0;
+
 // What a role needs of an entry.
 struct TileItem {
   TileEntry e;
@@ -369,8 +374,9 @@ struct TileItem {
 };
 
 // By one warp: the next entries of the block's list, from `item` on (its first
-// t0 key tiles are another block's), `left` key tiles in all.  Lane k finds the
+// t0 units are another block's), `left` units in all.  Lane k finds the
 // k-th item; the requests are gone through 32 at a time.
+template <bool kCodes>
 __device__ void fill_list(const AttnParams& p, TileShared& sh) {
   const int lane = threadIdx.x & 31, n = sh.stride;
   const int items = sh.items;
@@ -414,7 +420,7 @@ __device__ void fill_list(const AttnParams& p, TileShared& sh) {
       e.head = local / np;
       e.pair = local % np;
       e.q0 = q0, e.ql = ql, e.kvl = kvl;
-      cost = pair_cost(p, ql, kvl, e.pair);
+      cost = pair_cost(p, ql, kvl, e.pair) + kItem<kCodes>;
       found = true;
     }
     start = total;
@@ -435,15 +441,22 @@ __device__ void fill_list(const AttnParams& p, TileShared& sh) {
     if (__ballot_sync(~0u, bad) & ((2u << lane) - 1u)) e.seg = 0;
   }
   const int n_used = __popc(__ballot_sync(~0u, e.seg > 0));  // a run from lane 0
+  const int64_t taken = inc - mine + e.seg;
+  int count = n_used;
+  if (kCodes) {  // from units to key tiles; the last item may have none of them here
+    const int end = e.t0 + e.seg - kItem<kCodes>;
+    e.t0 = e.t0 > kItem<kCodes> ? e.t0 - kItem<kCodes> : 0;
+    e.seg = e.seg > 0 && end > e.t0 ? end - e.t0 : 0;
+    count = __popc(__ballot_sync(~0u, e.seg > 0));
+  }
   __syncwarp();
   if (e.seg > 0) sh.list[lane] = e;
   const int last = n_used > 0 ? n_used - 1 : 0;
   if (lane == last) {
-    const int64_t taken = inc - mine + e.seg;
-    sh.count = n_used;
+    sh.count = count;
     sh.left = left - taken;
     sh.more = n_used == kList && left > taken;
-    if (kBoundsChecked && n_used == 0) {  // a list has an entry: one without rows
+    if ((kBoundsChecked || kCodes) && count == 0) {  // a list has an entry: one without rows
       sh.list[0] = {0, 0, 0, 0, 0, 0, 1, 0};
       sh.count = 1;
     }
@@ -754,7 +767,7 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
       else hi = mid - 1;
     }
     const int4 r = reqs[at_req];
-    return pair_cost(p, r.y, r.z, (item - r.x) % r.w);
+    return pair_cost(p, r.y, r.z, (item - r.x) % r.w) + kItem<kCodes>;
   };
   const AttnRange range = attn_range<kThreads<kCodes>>((int)gridDim.x, blockIdx.x, gridDim.x, sh.scratch, [&](int c) -> int64_t {
     int64_t sum = 0;
@@ -792,7 +805,7 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
       sh.left = range.end - range.begin;
     }
     __syncwarp();
-    fill_list(p, sh);
+    fill_list<kCodes>(p, sh);
   }
   __syncthreads();  // the requests are done with: the ring is free
 
@@ -814,7 +827,7 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
     if (++k < sh.count) return true;
     if (!sh.more) return false;
     bar_all<kCodes>();
-    if (warp == 11) fill_list(p, sh);
+    if (warp == 11) fill_list<kCodes>(p, sh);
     bar_all<kCodes>();
     k = 0;
     return true;
@@ -823,7 +836,7 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
   auto leave = [&] {
     while (sh.more) {
       bar_all<kCodes>();
-      if (warp == 11) fill_list(p, sh);
+      if (warp == 11) fill_list<kCodes>(p, sh);
       bar_all<kCodes>();
     }
   };
