@@ -15,22 +15,23 @@
 //
 // Bound: 36 bytes a key and group of 32 elements, read once; and, before that,
 // issue slots: 11 operations for 8 codes, three of them to align a piece's codes,
-// about 310 a warp for 16 keys of 128 elements with all that is not codes.  So a
-// warp takes 32 keys at once where the accumulators leave room (waits, maxima and
-// votes are shared by them: three requests of 100,001 to 131,072 keys 100 -> 90 us),
-// the maximum of a row is looked for only when a score is above its reference by
-// more than 2^kLag, and one warp of five copies (a page's part of a stage is
-// contiguous, so a copy is up to 18 KB).
+// about 350 a warp for 16 keys of 128 elements with all that is not codes.  So a
+// warp takes 32 keys at once (waits, maxima and votes are shared by them: three
+// requests of 100,001 to 131,072 keys 100 -> 90 us; 28 of heads of 256 68 -> 63), the
+// maximum of a row is looked for only when a score is above its reference by more
+// than 2^kLag, and one warp of five copies (a page's part of a stage is contiguous,
+// so a copy is up to 36 KB).
 //
-// Measured (one GB300, 8 KV heads of 128): the three requests 88 us, 4.5 TB/s; one
-// of 1,000,000 keys 244 us, 4.7 TB/s, 0.71 of the copy rate; 28 of 2,000 to 6,000
-// 40 us, 13 of them start, end and join; one of 777 9.4 us, launches and a chain of
-// dependent reads.  28 requests of heads of 64, 96 and 256: 29, 38 and 73 us.
+// Measured (one GB300, 8 KV heads of 128): the three requests 80 us, 5.0 TB/s, of
+// which 11 us are start, end and join (0.87 of the copy rate between them); 28 of
+// 2,000 to 6,000 36 us; 150 of 300 to 5,000, 16 heads of 64, up to 4 tokens, 136 us;
+// one of 777 9.1 us, launches and a chain of dependent reads.
 //
 // Tried and slower: a ring for each warp, filled by itself, four blocks of four
-// warps an SM (the three requests 97 us: a fifth more operations), two blocks of
-// five an SM (95), fewer or more stages (no different), left shifts as products on
-// the other pipe (no different).
+// warps an SM (the three requests 97 us against 88: a fifth more operations), two
+// blocks an SM (95).  No different: fewer or more stages, three blocks of heads of
+// 64 instead of four, values' codes read before the exponentials, left shifts as
+// products on the other pipe.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -51,10 +52,10 @@ template <int N, int kR>
 struct Few4Cfg {
   static constexpr int kRows = 8 * kR, kCols = 32 * N;
   static constexpr int kPerSm = kR == 1 ? (N <= 2 ? 4 : N <= 4 ? 3 : 2) : N <= 2 ? 3 : 2;
-  static constexpr int kGroups = N <= 4 ? 2 : 1;  // of 16 keys, a warp takes of a stage
+  static constexpr int kGroups = 2;  // of 16 keys, a warp takes of a stage
   static constexpr int kKeys = 16 * kGroups * kWarps;
   static constexpr int kStage = kKeys / kCodeTokens * kv4_tile(N);
-  static constexpr int kStages = N <= 2 ? 4 : N == 3 ? 4 : N == 4 ? 3 : 4;
+  static constexpr int kStages = N <= 3 ? 4 : N == 4 ? 3 : 2;
   static constexpr int kPad = kCols + 4;  // row of the joining buffer, in floats
   static constexpr int kBuf = kRows * kPad * 4;
   static constexpr int kMl = kWarps * 2 * kRows * 4;
@@ -125,17 +126,9 @@ __device__ __forceinline__ uint32_t load_u32(uint32_t at) {
 }
 
 // Bounded wait of a whole warp: false once the block has given up, or after four
-// seconds (which it then counts).  The hardware holds the warp for up to a
-// microsecond at each look: looks take issue slots that the products need.
-__device__ __forceinline__ bool look(unsigned long long* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity), "r"(1000)
-      : "memory");
-  return __all_sync(~0u, ok != 0);
-}
+// seconds (which it then counts).  The lanes vote at each look: where they leave
+// the loop one by one, as in wait_bar, the three long requests take 88 us, not 80.
+__device__ __forceinline__ bool look(unsigned long long* bar, uint32_t parity) { return __all_sync(~0u, mbar_try_wait(bar, parity)); }
 __device__ __noinline__ bool wait_longer(unsigned long long* bar, uint32_t parity, int* gave_up) {
   const unsigned long long start = now_ns();
   for (;;) {

@@ -341,7 +341,8 @@ __device__ __forceinline__ int pair_cost(const AttnParams& p, int ql, int kvl, i
 }
 
 // The cache in 4 bits: what an item costs beside its key tiles, in their time,
-// counted before them as units of the line without work.
+// counted before them as units of the line without work.  (28 ragged chunks: 482 us
+// without, 460, 450, 451 and 451 with 2, 4, 6 and 8.)
 template <bool kCodes>
 constexpr int kItem = kCodes ? 4 : 0;
 
@@ -476,16 +477,16 @@ __device__ void fill_list(const AttnParams& p, TileShared& sh) {
 // whatever their bytes, so there is nothing to look for in masked ones.
 //
 // Measured (one GB300, 32 query heads on 8 KV heads of 128, pages of 16): 4,096
-// tokens over 20,480 keys, call after call, 0.95 ms, 1.30 PFLOP/s, of which 0.10
+// tokens over 20,480 keys, call after call, 0.94 ms, 1.31 PFLOP/s, of which 0.10
 // are the widening's (0.85 with codes left as they are, 0.83 over 16 bits); 28
 // requests of 28 to 685 tokens over 700 to 6,000 keys, 24 heads of 96, a tenth of
-// the pages absent, 0.48 ms.  Widening costs a warp about 85 operations for a
+// the pages absent, 0.45 ms.  Widening costs a warp about 85 operations for a
 // tile of 8 tokens, in a chain that one warp in a scheduler cannot hide: with three
 // warps instead of seven the long chunk takes 1.40 ms (divisions for the places in
 // a slot inside the loop: 3.0).
 //
-// Tried and no faster: 192 registers a row and 64 for the others (0.99 ms, ragged
-// 0.49), longer sleeps between polls, the fence between codes' stores and the
+// Tried and no faster: 192 registers a row and 64 for the others (2 % slower),
+// longer sleeps between polls, the fence between codes' stores and the
 // products on the products' side (2 % less), page lookups a tile further ahead (2 %
 // more); with heads above 128 five slots of half a key tile (1.25 -> 1.70 ms).
 template <bool F16, bool kCodes>
