@@ -402,7 +402,11 @@ mpt_status mpt_kv4_attend(const mpt_kv4_cache* c, int32_t type, const void* q, c
   p.item_toks = p.toks * (p.dim > 128 ? 1 : 2);
   p.wide = p.dim % 16 == 0 && mpt::aligned(out, 32) && (heads == 1 || p.out_head % 16 == 0) && (tokens == 1 || p.out_tok % 16 == 0);
   p.box = c->page_size;
-  const bool tile = most * p.group > 16 && c->batch <= mpt::kTileBatch;
+  // Up to 32 rows per KV head the smaller kernel's two items of 16 are faster than
+  // one tile of 128 rows (32 rows, smaller and larger kernel: 20,480 keys 27 and
+  // 37 us, 3,000 keys 16 and 25, 28 requests of 2,000 to 6,000 96 and 127; 64 rows:
+  // 40 and 38, 17 and 25, 175 and 126).
+  const bool tile = most * p.group > 32 && c->batch <= mpt::kTileBatch;
   const cudaError_t e = tile ? mpt::launch_attend4_tile(p, sms, device, (cudaStream_t)stream)
                              : mpt::launch_attend4_few(p, most * p.group < 16 ? (int)(most * p.group) : 16, sms, device, (cudaStream_t)stream);
   return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
