@@ -57,7 +57,7 @@ struct Few4Cfg {
   static constexpr int kStage = kKeys / kCodeTokens * kv4_tile(N);
   static constexpr int kStages = N <= 3 ? 4 : N == 4 ? 3 : 2;
   static constexpr int kPad = kCols + 4;  // row of the joining buffer, in floats
-  static constexpr int kBuf = kRows * kPad * 4;
+  static constexpr int kBuf = kWarps * kRows * kPad * 4;
   static constexpr int kMl = kWarps * 2 * kRows * 4;
   static constexpr int kSmem = 128 + kStages * kStage + kBuf + kMl + kStages * 24 + 320;
   static constexpr int kSlot = kRows * kCols + 2 * kRows;  // floats of a partial result
@@ -528,43 +528,17 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
           ml[(warp * 2 + 1) * kRows + 8 * i + 2 * q + e] = l[i][e];
         }
       }
+    // Each warp's outputs beside one another, against its own maxima; a warp
+    // without a key in a row has 0 there.
+#pragma unroll
+    for (int w = 0; w < N; ++w)
+#pragma unroll
+      for (int i = 0; i < kR; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          *(float4*)(bufs + (warp * kRows + 8 * i + 2 * q + e) * C::kPad + 4 * (N * g + w)) =
+              make_float4(o[i][2 * w][e], o[i][2 * w][2 + e], o[i][2 * w + 1][e], o[i][2 * w + 1][2 + e]);
     bar_consumers();
-    float f[kR][2];
-#pragma unroll
-    for (int i = 0; i < kR; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * 2 * kRows + 8 * i + 2 * q + e]);
-        f[i][e] = ex2(m[i][e] - (top == -INFINITY ? 0.f : top));
-      }
-    // A warp without a key in a row adds nothing (f = 0, its o is 0).  The warps
-    // add one after the other into one buffer, the first half of the words in
-    // the order 3, 2, 1, 0 and the second in 2, 3, 0, 1, two warps at a time.
-#pragma unroll
-    for (int round = 0; round < 4; ++round) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (warp != (half == 0 ? 3 - round : (round + 2) & 3)) continue;
-#pragma unroll
-        for (int w = half == 0 ? 0 : (N + 1) / 2; w < (half == 0 ? (N + 1) / 2 : N); ++w)
-#pragma unroll
-          for (int i = 0; i < kR; ++i)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float4* at = (float4*)(bufs + (8 * i + 2 * q + e) * C::kPad + 4 * (N * g + w));
-              float4 v = make_float4(o[i][2 * w][e] * f[i][e], o[i][2 * w][2 + e] * f[i][e], o[i][2 * w + 1][e] * f[i][e],
-                                     o[i][2 * w + 1][2 + e] * f[i][e]);
-              if (round > 0) {
-                const float4 z = *at;
-                v.x += z.x, v.y += z.y, v.z += z.z, v.w += z.w;
-              }
-              *at = v;
-            }
-      }
-      bar_consumers();
-    }
     const bool whole = starts && ends;
     const int slot = blockIdx.x * 2 + (starts ? 1 : 0);
     const bool outside = KV_BAD(g_few4_counts, x.rows >= 1 && x.rows <= kRows && few_inside(p, x, x.row0) && few_inside(p, x, x.row0 + x.rows - 1) &&
@@ -578,9 +552,17 @@ __global__ void __launch_bounds__(kThreads, Few4Cfg<N, kR>::kPerSm) k_attend4_fe
       for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * 2 * kRows + row]);
       const float safe = top == -INFINITY ? 0.f : top;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) sum += ml[(w * 2 + 1) * kRows + row] * ex2(ml[w * 2 * kRows + row] - safe);
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; i += 4) *(float4*)(v + i) = *(const float4*)(bufs + row * C::kPad + col + i);
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = ex2(ml[w * 2 * kRows + row] - safe);
+        sum = fmaf(ml[(w * 2 + 1) * kRows + row], f, sum);
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+          const float4 z = *(const float4*)(bufs + (w * kRows + row) * C::kPad + col + i);
+          v[i] = fmaf(f, z.x, v[i]), v[i + 1] = fmaf(f, z.y, v[i + 1]), v[i + 2] = fmaf(f, z.z, v[i + 2]), v[i + 3] = fmaf(f, z.w, v[i + 3]);
+        }
+      }
       if (whole) {
         const int abs = x.row0 + row;
         const int64_t tok = r.q0 + abs / p.group, head = (int64_t)x.head * p.group + abs % p.group;
