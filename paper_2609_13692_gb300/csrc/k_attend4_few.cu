@@ -25,11 +25,12 @@
 // Measured (one GB300, 8 KV heads of 128): the three requests 80 us, 5.0 TB/s, of
 // which 11 us are start, end and join (0.87 of the copy rate between them); 28 of
 // 2,000 to 6,000 36 us; 150 of 300 to 5,000, 16 heads of 64, up to 4 tokens, 136 us;
-// one of 777 9.1 us, launches and a chain of dependent reads.
+// one of 777 8.8 us, launches and a chain of dependent reads.
 //
 // Tried and slower: a ring for each warp, filled by itself, four blocks of four
 // warps an SM (the three requests 97 us against 88: a fifth more operations), two
-// blocks an SM (95).  No different: fewer or more stages, three blocks of heads of
+// blocks an SM (95), an item's queries read before the item before is joined (80 ->
+// 88: registers).  No different: fewer or more stages, three blocks of heads of
 // 64 instead of four, values' codes read before the exponentials, left shifts as
 // products on the other pipe.
 #include <cuda_bf16.h>
