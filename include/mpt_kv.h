@@ -137,7 +137,8 @@ typedef struct mpt_kv_turn {
   int32_t heads;            /* of q, 1 to 2^17 */
   const int32_t* positions; /* device [tokens], or NULL */
   const void* q;            /* device, the type of the keys, [tokens][heads][head_dim], or NULL */
-  void* q_out;              /* q turned; q itself (with its strides), or no overlap with it */
+  void* q_out;              /* q turned; q itself (with its strides), or no overlap with it; none with
+                             * the new keys and values (INVALID_ARG) or the cache */
   int64_t q_stride[2];      /* elements between tokens and heads, multiples of 8 */
   int64_t q_out_stride[2];
 } mpt_kv_turn;
@@ -203,7 +204,9 @@ mpt_status mpt_kv4_write(const mpt_kv4_cache* cache, const mpt_kv_turn* turn, in
  * `type`: BF16, F16 or F32) back out of their pages, for a request that is
  * handed to another cache or a check.  0 where the cache has no place for a
  * token; rows of no request are not written.
- *   k_out, v_out: device [tokens][kv_heads][head_dim], strides as in mpt_kv_write.
+ *   k_out, v_out: device [tokens][kv_heads][head_dim], strides as in mpt_kv_write;
+ *   they must not overlap one another (INVALID_ARG) or the pages; parts of one
+ *   tensor may interleave.
  * Errors: INVALID_ARG, TOO_LARGE, CUDA. */
 mpt_status mpt_kv4_read(const mpt_kv4_cache* cache, int32_t type, void* k_out, const int64_t* k_stride, void* v_out,
                         const int64_t* v_stride, int64_t tokens, void* stream);

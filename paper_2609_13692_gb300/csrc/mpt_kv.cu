@@ -4,6 +4,7 @@
 #include <cstring>
 
 #include "kv4.cuh"
+#include "kv_overlap.h"
 #include "kv_pages.cuh"
 #include "kv_report.h"
 
@@ -131,6 +132,20 @@ mpt_status check_turn(const mpt_kv_turn* u, int32_t dim, int64_t tokens) {
   if (u->q == u->q_out && ((tokens > 1 && u->q_stride[0] != u->q_out_stride[0]) || (u->heads > 1 && u->q_stride[1] != u->q_out_stride[1])))
     return MPT_ERR_INVALID_ARG;
   return MPT_OK;
+}
+
+HeadRuns head_runs(const void* at, const int64_t* stride, int64_t tokens, int32_t heads, int32_t dim, int bytes) {
+  return {(uintptr_t)at, (int64_t)dim * bytes, {tokens, heads}, {stride[0] * bytes, stride[1] * bytes}};
+}
+
+// Turned queries may be written where they were read, but nowhere else over what
+// other warps still read.
+bool turn_overlaps(const mpt_kv_turn& u, int32_t dim, const void* k, const int64_t* k_stride, const void* v, const int64_t* v_stride,
+                   int64_t tokens, int32_t kv_heads) {
+  if (!u.q) return false;
+  const HeadRuns out = head_runs(u.q_out, u.q_out_stride, tokens, u.heads, dim, 2);
+  return (u.q != u.q_out && heads_overlap(out, head_runs(u.q, u.q_stride, tokens, u.heads, dim, 2))) ||
+         heads_overlap(out, head_runs(k, k_stride, tokens, kv_heads, dim, 2)) || heads_overlap(out, head_runs(v, v_stride, tokens, kv_heads, dim, 2));
 }
 
 // What the writes with a turn, the writes of codes and their reads share.
@@ -309,6 +324,7 @@ mpt_status mpt_kv_write_rotated(const mpt_kv_cache* c, const mpt_kv_turn* turn, 
   if (st == MPT_OK) st = mpt::check_turn(turn, c->head_dim, tokens);
   if (st == MPT_OK) st = mpt::check_new(k_new, k_stride, v_new, v_stride, tokens, c->kv_heads);
   if (st != MPT_OK || tokens == 0 || c->batch == 0) return st;
+  if (mpt::turn_overlaps(*turn, c->head_dim, k_new, k_stride, v_new, v_stride, tokens, c->kv_heads)) return MPT_ERR_INVALID_ARG;
   mpt::AppendParams p;
   mpt::fill_append(p, *c, turn, k_new, k_stride, v_new, v_stride, tokens, log2);
   p.k = (char*)c->k, p.v = (char*)c->v;
@@ -333,6 +349,7 @@ mpt_status mpt_kv4_write(const mpt_kv4_cache* c, const mpt_kv_turn* turn, int32_
   if (st == MPT_OK && turn) st = mpt::check_turn(turn, c->head_dim, tokens);
   if (st == MPT_OK) st = mpt::check_new(k_new, k_stride, v_new, v_stride, tokens, c->kv_heads);
   if (st != MPT_OK || tokens == 0 || c->batch == 0) return st;
+  if (turn && mpt::turn_overlaps(*turn, c->head_dim, k_new, k_stride, v_new, v_stride, tokens, c->kv_heads)) return MPT_ERR_INVALID_ARG;
   mpt::AppendParams p;
   mpt::fill_append(p, *c, turn, k_new, k_stride, v_new, v_stride, tokens, log2);
   p.pages = (char*)c->pages, p.page_bytes = c->stride[0], p.head_bytes = c->stride[1];
@@ -347,6 +364,10 @@ mpt_status mpt_kv4_read(const mpt_kv4_cache* c, int32_t type, void* k_out, const
   if (st == MPT_OK && type != MPT_KV_BF16 && type != MPT_KV_F16 && type != MPT_KV_F32) st = MPT_ERR_INVALID_ARG;
   if (st == MPT_OK) st = mpt::check_new(k_out, k_stride, v_out, v_stride, tokens, c->kv_heads);
   if (st != MPT_OK || tokens == 0 || c->batch == 0) return st;
+  const int bytes = type == MPT_KV_F32 ? 4 : 2;
+  if (mpt::heads_overlap(mpt::head_runs(k_out, k_stride, tokens, c->kv_heads, c->head_dim, bytes),
+                         mpt::head_runs(v_out, v_stride, tokens, c->kv_heads, c->head_dim, bytes)))
+    return MPT_ERR_INVALID_ARG;
   mpt::AppendParams p;
   mpt::fill_append(p, *c, nullptr, k_out, k_stride, v_out, v_stride, tokens, log2);
   p.pages = (char*)c->pages, p.page_bytes = c->stride[0], p.head_bytes = c->stride[1];

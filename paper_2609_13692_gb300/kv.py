@@ -314,8 +314,8 @@ def mpt_kv_write_rotated(k_new, v_new, rotation, k_pages, v_pages, page_table, q
     first rot elements of a head turn, i with i + rot / 2 (rot a multiple of 16) or, with
     ``adjacent``, 2 i with 2 i + 1 (of 8).  positions: int32[tokens], each token's row of
     ``rotation``; default: its position in the cache.  A token whose row is not there is dropped, its
-    query is not turned.  q_out: where the turned queries go (q itself: in place); tokens of no
-    request are not written."""
+    query is not turned.  q_out: where the turned queries go (q itself: in place, else memory that
+    q, k_new and v_new have no part of); tokens of no request are not written."""
     index = _device(k_pages, v_pages, page_table, q_offsets, kv_lens, k_new, v_new)
     _no_grad(k_new, v_new, k_pages, v_pages)
     cache, dtype, kv_heads, dim = _cache(k_pages, v_pages, page_table, q_offsets, kv_lens)
@@ -405,8 +405,8 @@ def _write4(s, cache, k_new, v_new, rotation, positions, adjacent, q, q_out, ind
 def mpt_kv4_read(pages, page_table, q_offsets, kv_lens, tokens: int, head_dim: int, *, dtype=torch.bfloat16, k_out=None, v_out=None,
                  stream: Optional[int] = None):
     """What the new tokens' codes stand for, in bf16, f16 or f32; returns (keys, values), each
-    [tokens, kv_heads, head_dim].  0 for tokens that the cache has no place for; tokens of no request
-    are not written."""
+    [tokens, kv_heads, head_dim] (k_out, v_out: where they go, without overlap).  0 for tokens that
+    the cache has no place for; tokens of no request are not written."""
     index = _device(pages, page_table, q_offsets, kv_lens)
     cache = _cache4(pages, page_table, q_offsets, kv_lens, int(head_dim))
     kind = _TYPES.get(dtype)
