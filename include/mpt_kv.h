@@ -217,9 +217,11 @@ mpt_status mpt_kv4_attend_workspace_bytes(size_t* bytes);
 
 /* mpt_kv_attend over a cache in 4 bits; q and out are `type` (BF16 or F16).
  * Keys and values enter the products as the f16 values that their codes stand
- * for, queries as f16 (bf16 ones times a power of two of their row, which is
- * exact down to 2^-24 of the row's largest), probabilities as f16 at 2^11 times
- * their size at least.  Errors: as mpt_kv_attend. */
+ * for, queries as f16, probabilities as f16 at 2^11 times their size at least.
+ * A row of bf16 queries is first divided by the power of two 2^e that its largest
+ * element is in [2^e, 2^(e+1)) of: elements of 2^(e-17) and more stay as they
+ * are, smaller ones are off by up to 2^(e-25) (an error of the score of up to
+ * scale 2^(e-25) sum |k|).  Errors: as mpt_kv_attend. */
 mpt_status mpt_kv4_attend(const mpt_kv4_cache* cache, int32_t type, const void* q, const int64_t* q_stride,
                           int64_t tokens, int32_t heads, int32_t max_q_len, int32_t causal, float scale, void* out,
                           const int64_t* out_stride, float* lse, void* workspace, size_t workspace_bytes,

@@ -11,7 +11,10 @@
 // layout is that operand's: a lane's words of a key hold the pairs (e, e + 4) of
 // elements of its own, in an order that the query's fragments follow, and its
 // words of values pairs of tokens.  P^T comes from S^T by a transposition of
-// 8 x 8 matrices across lanes.
+// 8 x 8 matrices across lanes.  It is f16, as the product asks for beside exact
+// values: 11 bits of each probability, which is the only rounding besides the
+// output's (against 64 bits 2.9e-4 of f16 outputs, where 32-bit probabilities
+// leave 2.1e-4; of bf16 ones 1.67e-3 and 1.66e-3).
 //
 // Bound: 36 bytes a key and group of 32 elements, read once; and, before that,
 // issue slots: 11 operations for 8 codes, three of them to align a piece's codes,
@@ -182,9 +185,10 @@ __device__ __forceinline__ bool few_inside(const AttnParams& p, const Few4Item& 
   return attn_inside(p, x.req, x.head, x.r.q0, x.r.ql, x.r.kvl) && row >= 0 && row / p.group < x.r.ql;
 }
 
-// A query row's part of a lane as f16, and (bf16) the power of two that was
-// taken out of it: 2^-e with the row's largest element below 2^(e + 1), so that
-// nothing overflows and what f16 cannot hold is below 2^-24 of that element.
+// A query row's part of a lane as f16, the type of the other operand (bf16 would
+// round what codes stand for), and (bf16) the power of two 2^e that was taken out
+// of it, the row's largest element being below 2^(e + 1): nothing overflows.  Of
+// bf16's 8 bits f16 holds all down to 2^-17 of 2^e, and what is below to 2^-25 of it.
 template <int N>
 __device__ __forceinline__ float query_words(const uint4* raw, bool f16, uint32_t (*qf)[2]) {
   float back = 1.f, by = 1.f;

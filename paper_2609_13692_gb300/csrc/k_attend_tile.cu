@@ -496,9 +496,9 @@ __device__ __forceinline__ uint32_t pack_as(const AttnParams& p, float lo, float
 }
 
 // A row's query into row r of its tile's operand, each 8 elements in the order
-// 0 4 1 5 2 6 3 7 that a word of codes gives (widen_codes).  bf16: times a power
-// of two, so that the largest element stays below 2 and f16 holds what is above
-// 2^-14 of it exactly; returns what takes it out again.  nullptr: zeros.
+// 0 4 1 5 2 6 3 7 that a word of codes gives (widen_codes).  bf16: divided by the
+// power of two 2^e that leaves the largest element in [1, 2), so that f16 holds what
+// is at least 2^-17 exactly and the rest to 2^-25; returns 2^e.  nullptr: zeros.
 template <int HDP>
 __device__ __forceinline__ float stage_query(const char* q, int dim, bool f16, char* to, int r) {
   uint4 u[HDP / 8];  // all loads are in flight together
