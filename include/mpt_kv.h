@@ -26,9 +26,14 @@
  *   - Request i owns the new tokens q_offsets[i] .. q_offsets[i+1] - 1 of the
  *     packed token axis and kv_lens[i] tokens of the cache, the new ones the
  *     last among them; its token at position p lies on page
- *     page_table[i * table_stride + p / page_size], slot p % page_size.  Read
- *     lengths are clamped to what the table and the token axis hold
- *     (0 <= kv_lens[i] <= table_width * page_size).
+ *     page_table[i * table_stride + p / page_size], slot p % page_size.
+ *   - Attention clamps lengths to what the table and the token axis hold
+ *     (0 <= kv_lens[i] <= table_width * page_size, offsets from 0 to tokens) and
+ *     takes positions from the clamped ones.  Writes, and codes read back, take
+ *     lengths as they are: token t of request i stands at kv_lens[i] -
+ *     (q_offsets[i+1] - q_offsets[i]) + t - q_offsets[i], and one whose position
+ *     the table does not have is dropped.  The two differ only where a length
+ *     or an offset reaches past the tensors.
  *   - A page id outside [0, n_pages) is a page that the cache does not hold
  *     (-1 by convention): its keys are masked, writes to it are dropped.
  */
