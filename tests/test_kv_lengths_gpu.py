@@ -15,6 +15,20 @@ I32 = dict(dtype=torch.int32)
 BEYOND = [0, 1, 41, 44]
 
 
+@pytest.mark.parametrize("last", [50, 64, 2 ** 31 - 1])
+@pytest.mark.parametrize("hint", [1, 40])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_attention_clamps_offsets(kv, dim, hint, last):  # noqa: F811
+    """The last offset beyond the tokens: as the number of tokens itself, in every row."""
+    c = make(21, [1, 40, 3, 5], [60, 64, 9, 30], 4, 2, dim, 16, BF16)
+    assert c["at"].tolist() == BEYOND + [49]
+    want = kv.mpt_kv4_attend(*args(c), max_q_len=hint)
+    got = kv.mpt_kv4_attend(*args(c)[:3], torch.tensor(BEYOND + [last], **I32, device="cuda"), c["lens"], max_q_len=hint)
+    kv.mpt_kv_check()
+    assert not bool(torch.isneginf(want[1]).any())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("last,lens", [(50, [60, 64, 9, 30]), (60, [60, 64, 9, 30]), (49, [60, 85, 9, 90]), (2 ** 31 - 1, [60, 64, 9, 2 ** 31 - 1])])
 def test_writes_take_lengths_as_they_are(kv, last, lens):  # noqa: F811
     """Token t of request i stands at kv_lens[i] - (q_offsets[i + 1] - q_offsets[i]) + its place there, whatever the
