@@ -423,10 +423,18 @@ mpt_status mpt_kv4_attend(const mpt_kv4_cache* c, int32_t type, const void* q, c
   p.item_toks = p.toks * (p.dim > 128 ? 1 : 2);
   p.wide = p.dim % 16 == 0 && mpt::aligned(out, 32) && (heads == 1 || p.out_head % 16 == 0) && (tokens == 1 || p.out_tok % 16 == 0);
   p.box = c->page_size;
-  // Up to 32 rows per KV head the smaller kernel's two items of 16 are faster than
-  // one tile of 128 rows (32 rows, smaller and larger kernel: 20,480 keys 27 and
-  // 37 us, 3,000 keys 16 and 25, 28 requests of 2,000 to 6,000 96 and 127; 64 rows:
-  // 40 and 38, 17 and 25, 175 and 126).
+  // Up to 32 rows per KV head the smaller kernel is faster than one tile of 128
+  // rows, although its items of 16 rows (8, with heads above 128) widen each code
+  // two to four times.  Smaller and larger kernel, us, 8 KV heads, one token's heads
+  // four rows:
+  //                       28 of 2,000 to 6,000 keys     one of 20,480
+  //   heads of             64       128       256         128       256
+  //   16 rows           38  101   59  126  118  358     23  37    31  95
+  //   32 rows           62  101  101  127  219  370     28  38    48  98
+  //   48 rows           86  101  142  128  320  371     34  38    64  99
+  //   64 rows          109  101  184  128  422  379     41  39    81 100
+  // (Heads of 160 and 192 cross where those of 256 do.)  One of 3,000 keys is
+  // the smaller one's at all of these.
   const bool tile = most * p.group > 32 && c->batch <= mpt::kTileBatch;
   const cudaError_t e = tile ? mpt::launch_attend4_tile(p, sms, device, (cudaStream_t)stream)
                              : mpt::launch_attend4_few(p, most * p.group < 16 ? (int)(most * p.group) : 16, sms, device, (cudaStream_t)stream);
