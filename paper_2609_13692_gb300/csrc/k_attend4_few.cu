@@ -181,7 +181,7 @@ __device__ __forceinline__ Few4Item few_item(const AttnParams& p, const AttnReq&
   it.tiles = tiles_of<kKeys>(attn_limit(p, r, (it.row0 + it.rows - 1) / p.group));
   return it;
 }
-__device__ __forceinline__ bool few_inside(const AttnParams& p, const Few4Item& x, int row) {
+[[maybe_unused]] __device__ __forceinline__ bool few_inside(const AttnParams& p, const Few4Item& x, int row) {
   return attn_inside(p, x.req, x.head, x.r.q0, x.r.ql, x.r.kvl) && row >= 0 && row / p.group < x.r.ql;
 }
 

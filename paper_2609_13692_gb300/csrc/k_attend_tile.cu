@@ -589,12 +589,8 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
   auto unit = [&](int v, int i) { return i * kCodeWarps + (v ? (me + 2) % kCodeWarps : me); };
   auto tile8 = [&](int u) { return u / kPer * kTogether + second; };
 
-  TileItem w;
-  int k = 0;
-  uint32_t gt = 0;
-  bool ok = true;
   // Lane b: the b-th tile of 8 of a key tile, nullptr without a page.
-  auto tile_of = [&](int j, int tiles) -> const char* {
+  auto tile_of = [&](const TileItem& w, int j, int tiles) -> const char* {
     const int64_t key = (int64_t)(w.e.t0 + j) * kKeys + (lane & 15) * kCodeTokens;
     if (j >= tiles || key >= w.e.kvl) return nullptr;
     const int id = p.table[(int64_t)w.e.req * p.table_stride + (key >> p.page_log2)];
@@ -647,11 +643,15 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
   };
 
   CodeChunk c[kSteps];
+  TileItem w;
+  int k = 0;
+  uint32_t gt = 0;
+  bool ok = true;
   do {
     w.load(p, &sh.list[k]);
     const int tiles = w.tiles;
     if (tiles == 0) continue;
-    const char *now = tile_of(0, tiles), *next = tile_of(1, tiles);
+    const char *now = tile_of(w, 0, tiles), *next = tile_of(w, 1, tiles);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) load(c[i], 0, i, now);
     for (int j = 0; j < tiles && ok; ++j, ++gt) {
@@ -676,7 +676,7 @@ __device__ __forceinline__ void widen_codes(const AttnParams& p, TileShared& sh,
         if (lane == 0) mbar_arrive(&sh.full[s]);
       }
       now = next;
-      next = tile_of(j + 2, tiles);
+      next = tile_of(w, j + 2, tiles);
     }
   } while (ok && uniform(next_item(k)));
   if (!ok) leave();
@@ -1424,12 +1424,12 @@ __global__ void __launch_bounds__(kThreads<kCodes>, 1) k_attend_tile(const __gri
   if ((warp == 9 || warp == 10) && *(volatile int*)gave_up) {
     if (tid == 9 * 32) atomicAdd(&g_tile_counts[kKvGaveUp], 1u);
     if (!kCodes) {
-    const uint32_t v = warp - 9, n = sh.sent[v], last = (C::kSlots + 1) / 2;
-    for (uint32_t k = n > last ? n - last : 0; k < n; ++k) {
-      const uint32_t idx = 2 * k + v;
-      wait_landed(&sh.full[idx % C::kSlots], (idx / C::kSlots) & 1);
-    }
-    if (v == 0 && sh.asked > 0) wait_landed(&sh.q_full, (sh.asked - 1) & 1);
+      const uint32_t v = warp - 9, n = sh.sent[v], last = (C::kSlots + 1) / 2;
+      for (uint32_t k = n > last ? n - last : 0; k < n; ++k) {
+        const uint32_t idx = 2 * k + v;
+        wait_landed(&sh.full[idx % C::kSlots], (idx / C::kSlots) & 1);
+      }
+      if (v == 0 && sh.asked > 0) wait_landed(&sh.q_full, (sh.asked - 1) & 1);
     }
   }
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));

@@ -258,19 +258,19 @@ __global__ void __launch_bounds__(128, kCodes ? 7 : 8) k_kv_append(const __grid_
   if constexpr (!kCodes) {
     uint4* const k = (uint4*)p.k + page * p.k_page + slot * p.k_slot + sub;
     uint4* const v = (uint4*)p.v + page * p.v_page + slot * p.v_slot + sub;
-    before += stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    before += stream(std::integral_constant<int, 4>(), p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       float f[8];
       turn<F16>(u, p.adjacent, first, x, f);
       if (has && here) k[head * p.k_head] = u.on ? narrow<F16>(f) : x;
     });
-    stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    stream(std::integral_constant<int, 4>(), p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       if (has && here) v[head * p.v_head] = x;
     });
   } else {
     const int n = kv4_groups(p.dim), tok = (int)slot & 7, g = sub >> 2;
     const bool writes = sub < 4 * n;
     char* const tile = p.pages + page * p.page_bytes + (slot >> 3) * kv4_tile(n);
-    before += stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    before += stream(std::integral_constant<int, 2>(), p.k_new, p.k_new_tok, p.k_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       float f[8];
       uint32_t marks;
       turn<F16>(u, p.adjacent, first, x, f);
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(128, kCodes ? 7 : 8) k_kv_append(const __grid_
       *(uint32_t*)(to + kv4_key(n, tok) + sub * 4) = w;
       if ((sub & 3) == 0) *(uint16_t*)(to + kv4_key_marks(n, tok) + g * 2) = (uint16_t)marks;
     });
-    stream(std::integral_constant<int, kCodes ? 2 : 4>(), p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
+    stream(std::integral_constant<int, 2>(), p.v_new, p.v_new_tok, p.v_new_head, p.kv_heads, before, [&](const uint4& x, int head, bool here) {
       float f[8];
       uint32_t marks;
       widen<F16>(x, f);
