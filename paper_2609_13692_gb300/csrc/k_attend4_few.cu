@@ -25,10 +25,11 @@
 // than 2^kLag, and one warp of five copies (a page's part of a stage is contiguous,
 // so a copy is up to 36 KB).
 //
-// Measured (one GB300, 8 KV heads of 128): the three requests 80 us, 5.0 TB/s, of
-// which 11 us are start, end and join (0.87 of the copy rate between them); 28 of
-// 2,000 to 6,000 36 us; 150 of 300 to 5,000, 16 heads of 64, up to 4 tokens, 136 us;
-// one of 777 8.8 us, launches and a chain of dependent reads.
+// Measured (GB300, 8 KV heads of 128; from the fastest GPU to the slowest): the
+// three requests 80 to 88 us, 5.0 TB/s on the fastest, of which 11 us are start, end
+// and join (0.87 of the copy rate between them); 28 of 2,000 to 6,000 36 to 40 us; 150
+// of 300 to 5,000, 16 heads of 64, up to 4 tokens, 136 us; one of 777 9.0 to 9.5 us,
+// launches and a chain of dependent reads.
 //
 // Tried and slower: a ring for each warp, filled by itself, four blocks of four
 // warps an SM (the three requests 97 us against 88: a fifth more operations), two

@@ -13,7 +13,7 @@
 // 4.5 bits an element.  A token's chain of reads (request, page, cosines, values)
 // is long, so what counts is how many warps are there to hide it: eight blocks of
 // four an SM, which 64 registers allow, are worth more than more loads in flight in
-// each (33,600 tokens of 32 query and 8 KV heads of 128, turned: 151 us with 88
+// each (31,175 tokens of 32 query and 8 KV heads of 128, turned: 151 us with 88
 // registers, 180 with 92 and loads that run ahead, 119 with 64; of codes, seven
 // blocks and two steps at once).  The arithmetic of the codes, about 12 operations
 // an element, does not hide whole: without it the write takes 10 us less.
