@@ -49,7 +49,7 @@ extern "C" {
 /* Element types. */
 #define MPT_KV_BF16 0
 #define MPT_KV_F16 1
-#define MPT_KV_F32 2 /* mpt_kv_merge only */
+#define MPT_KV_F32 2 /* mpt_kv_merge and mpt_kv4_read only */
 
 /* One layer's cache and the requests of one step. */
 typedef struct mpt_kv_cache {
